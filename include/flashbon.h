@@ -278,6 +278,9 @@ enum {
   FB_K_EMBED,         /* patch embedding */
   FB_K_HEAD,          /* head + Euler update */
   FB_K_SMALL,         /* timestep embedding, modulation, conversions */
+  FB_K_SANDWICH,      /* norms around a block, gate, scaled residual, expert combination */
+  FB_K_ROUTE,         /* router: top-k experts, rows sorted by expert */
+  FB_K_EXPERT,        /* products grouped by expert */
   FB_K_COUNT
 };
 typedef struct fb_kstat {
@@ -339,6 +342,139 @@ fb_status fb_op_gemm(fb_model* m, int M, int N, int K, const void* A, const void
 fb_status fb_op_attention(fb_model* m, const void* Q, int ldq, const void* K, int ldk,
                           const void* V, int ldv, void* O, int ldo, int batch, int Lq,
                           int Lkv, int kv_batch_rows, int heads, int head_dim, int impl);
+
+/* ---- mixture-of-experts feed-forward between two norms ---------------------------
+ * (an engineering entry point: the paper's f_theta is a black box, and DiT variants whose
+ * feed-forward is a mixture of experts, or whose blocks have a norm on both sides, need
+ * these next to the calls above.) Inference only, like the rest of the library. The op
+ * calls follow the single-op ones: DEVICE pointers, enqueued on the model's stream (on the
+ * SMs of its budget), waited for. A matrix is row-major with a row stride in elements (ld*),
+ * which may exceed its width; elements behind the width are neither read nor written.
+ * Inputs and outputs do not overlap unless said so. fb_set_op_repeat applies. */
+enum { FB_BF16 = 0, FB_F32 = 1 };                              /* element types */
+enum { FB_NORM_NONE = 0, FB_NORM_RMS = 1, FB_NORM_LAYER = 2 }; /* norms over a row */
+/* Activations. The gated ones take 2 n weight rows, the n gate rows before the n up rows:
+ * silu(gate) * up, gelu(gate) * up. GELU is the tanh form. */
+enum { FB_ACT_NONE = 0, FB_ACT_GELU = 1, FB_ACT_SWIGLU = 2, FB_ACT_GEGLU = 3 };
+
+/* fb_op_sandwich_norm: the norm behind a block, its gate, the scaled residual and the norm
+ * before the next block, for each of `rows` rows r of `dim` elements (group g = r /
+ * group_rows, or 0 with group_rows = 0):
+ *   y  = row r of y                           (parts = 0), or
+ *   y  = sum_j weight[r][j] * y[slot[r][j]]   (parts >= 1; slot -1 adds nothing and its
+ *                                              weight is not used)
+ *   u  = Post(y) * post_w + post_b            (NULL: 1 and 0)
+ *   h' = resid_scale * h + gate[g] * u        (gate NULL: 1; y NULL: h' = resid_scale * h)
+ *   a  = Pre(h') * (mul_base + mul[g]) + add[g]   (mul, add NULL: 0)
+ * with RMSNorm x / sqrt(mean(x^2) + eps) or LayerNorm (x - mean) / sqrt(var + eps). All
+ * arithmetic is fp32; h' (type of h) and a are rounded as they are stored, and a is formed
+ * from h' before that. h_out NULL: h' is not stored; it may be h (same stride). a NULL: no
+ * second norm (pre is then ignored). y: bf16 or fp32 [y_rows][dim]; slot and weight:
+ * [rows][parts]; gate, mul, add: fp32 rows of stride ldm; post_w, post_b: fp32 [dim].
+ * FB_EINVAL for dim outside [1, FB_SANDWICH_MAX_DIM], parts outside [0,
+ * FB_SANDWICH_MAX_PARTS], strides below dim, rows missing from y, an unknown type or norm,
+ * nothing to write, or a slot >= y_rows (found on the device: the outputs are then not
+ * usable). rows = 0 does nothing. */
+#define FB_SANDWICH_MAX_DIM 16384
+#define FB_SANDWICH_MAX_PARTS 16
+typedef struct fb_sandwich {
+  int rows, dim;
+  const void* h;
+  int h_type;
+  int64_t ldh;
+  const void* y;
+  int y_type, y_rows, parts;
+  int64_t ldy;
+  const int32_t* slot;
+  const float* weight;
+  int post;
+  float post_eps;
+  const float *post_w, *post_b, *gate;
+  float resid_scale;
+  void* h_out;
+  int64_t ldho;
+  int pre;
+  float pre_eps, mul_base;
+  const float *mul, *add;
+  void* a;
+  int a_type;
+  int64_t lda;
+  int group_rows;
+  int64_t ldm;
+} fb_sandwich;
+fb_status fb_op_sandwich_norm(fb_model* m, const fb_sandwich* s);
+
+/* fb_op_route: the router. logits [tokens][experts] (bf16 or fp32) -> for each token its
+ * top_k experts by falling logit (ties: the lower expert) in expert[token][0..], their
+ * softmax weights over all experts (renorm != 0: over the chosen ones) in weight, and the
+ * (token, expert) pairs sorted by expert, tokens rising within one: pairs offsets[e] ..
+ * offsets[e + 1] - 1 are expert e's, token[i] is pair i's token and slot[token][j] the pair
+ * of a token's j-th expert. Pairs are the rows that fb_op_expert_gemm takes. A NaN or -inf
+ * logit is never chosen and has weight 0 (+inf counts as the largest finite value). valid
+ * [tokens] or NULL: tokens with valid = 0 (padding) go nowhere and their logits are not
+ * used. Where a token has fewer experts, its last entries are expert -1, weight 0, slot -1,
+ * and token[offsets[experts] ..] is -1. expert, weight, slot: [tokens][top_k]; token:
+ * [tokens * top_k]; offsets: [experts + 1]. FB_EINVAL for experts outside [1,
+ * FB_ROUTE_MAX_EXPERTS], top_k outside [1, min(experts, FB_ROUTE_MAX_TOP_K)] or tokens
+ * outside [0, FB_ROUTE_MAX_PAIRS / top_k]. */
+#define FB_ROUTE_MAX_EXPERTS 512
+#define FB_ROUTE_MAX_TOP_K 16
+#define FB_ROUTE_MAX_PAIRS (1 << 26)
+typedef struct fb_route {
+  int tokens, experts, top_k;
+  const void* logits;
+  int logits_type;
+  int64_t ldl;
+  const uint8_t* valid;
+  int renorm;
+  int32_t* expert;
+  float* weight;
+  int32_t *slot, *token, *offsets;
+} fb_route;
+fb_status fb_op_route(fb_model* m, const fb_route* r);
+
+/* fb_op_expert_gemm: matrix products grouped by expert. Rows offsets[e] .. offsets[e + 1] -
+ * 1 of out [max_rows][n] are act(x W_e^T + b_e), x = a[index[row]] (index NULL: a[row]),
+ * with a bf16 [a_rows][k], W bf16 [experts][n or 2 n][k], bias fp32 [experts][n or 2 n] or
+ * NULL, out bf16 or fp32. offsets [experts + 1] (rising from 0 to at most max_rows) and
+ * index [max_rows] are read on the device; groups may be empty, and rows from
+ * offsets[experts] on are neither read nor written. Sums are fp32, rounded once as they are
+ * stored. n and k are multiples of 8 (gated: n of 16), lda and ldo too; a, w and out are
+ * 16-byte aligned. FB_EINVAL for other sizes, experts outside [1, FB_ROUTE_MAX_EXPERTS],
+ * max_rows outside [0, FB_ROUTE_MAX_PAIRS], or, found on the device, offsets that are not
+ * as above or an index outside [0, a_rows) (the outputs are then not usable). */
+typedef struct fb_experts {
+  int experts, n, k, max_rows, a_rows;
+  const void* a;
+  int64_t lda;
+  const int32_t *index, *offsets;
+  const void* w;
+  const float* bias;
+  int act;
+  void* out;
+  int out_type;
+  int64_t ldo;
+} fb_experts;
+fb_status fb_op_expert_gemm(fb_model* m, const fb_experts* g);
+
+/* fb_moe_forward: the feed-forward of a block as a mixture of experts, in one call:
+ *   logits = a router_w^T                  [rows][router_rows], the first `experts` used
+ *   fb_op_route, w1 with `act` (n = hidden, k = dim), w2 (n = dim, k = hidden)
+ *   fb_op_sandwich_norm(s) with y = the experts' rows, combined by the router's weights
+ * a: bf16 [s->rows][dim], contiguous, the normed input (the a of the fb_op_sandwich_norm
+ * before it); s->a, the next block's input, may be the same buffer. s->y, slot and weight
+ * must be NULL (the call fills them in). router_w: bf16 [router_rows][dim], router_rows a
+ * multiple of 8 and at least `experts`; rows behind `experts` are ignored (padded to a
+ * multiple of 128 the product runs on the tensor cores where dim % 64 == 0). hidden and dim
+ * are multiples of 16. valid: as in fb_op_route, or NULL. The
+ * scratch buffers are the model's and grow on demand (FB_ENOMEM). */
+typedef struct fb_moe {
+  int dim, hidden, experts, top_k, renorm, act, router_rows;
+  const void *router_w, *w1, *w2;
+  const float *b1, *b2;
+} fb_moe;
+fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const uint8_t* valid,
+                         const fb_sandwich* s);
 
 /* ---- allocation-free stream-K GEMM (an engineering entry point: the paper has no
  * counterpart; it computes what fb_op_gemm with impl 4 computes) ---------------------

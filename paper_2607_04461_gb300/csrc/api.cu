@@ -205,6 +205,9 @@ struct fb_model {
   // launches; reset after a device error)
   float* attn_ws = nullptr;
   int* attn_flags = nullptr;
+  // scratch of fb_moe_forward, grown on demand
+  uint8_t* moe_ws = nullptr;
+  size_t moe_bytes = 0;
   // statistics
   unsigned timing_mask = 0;
   int op_repeat = 1;
@@ -331,6 +334,8 @@ fb_status end_call(fb_model* m) {
   CKS(reset_errors(m));
   if (code == FB_DEVERR_WAIT_TIMEOUT)
     return fail(FB_ECUDA, "device wait timed out (a kernel gave up after its time limit)");
+  if (code == FB_DEVERR_BAD_INDEX)
+    return fail(FB_EINVAL, "an index or offset array holds values out of range");
   return fail(FB_ECUDA, "device error %d", code);
 }
 
@@ -406,6 +411,107 @@ fb_status run_qkn(fb_model* m, bf16* x, int rows, int ld, int nseg, int dcol, co
   KTimer t(m, FB_K_QKNORM, 6.0 * rows * nseg * m->c.dim, 4.0 * rows * nseg * m->c.dim);
   CK(qk_norm_rope(x, rows, ld, m->c.dim, nseg, dcol, w0, dw, m->c.eps_rms, rope, m->P,
                   m->c.head_dim, norm_few_rows(m->num_sms, m->num_sms == m->dev_sms), m->st));
+  return FB_OK;
+}
+
+// ---- mixture of experts between two norms ---------------------------------------------
+double type_bytes(int type) { return type == FB_F32 ? 4 : 2; }
+
+fb_status run_sandwich(fb_model* m, const fb_sandwich& s) {
+  const double n = (double)s.rows * s.dim;
+  double bytes = n * type_bytes(s.h_type) * (s.h_out ? 2 : 1) + (s.a ? n * type_bytes(s.a_type) : 0);
+  if (s.y) bytes += n * type_bytes(s.y_type) * (s.parts ? s.parts : 1);
+  SandwichArgs a;
+  static_cast<fb_sandwich&>(a) = s;
+  KTimer t(m, FB_K_SANDWICH, n * (20 + 2 * s.parts), bytes);
+  CK(sandwich_norm(a, m->derr, m->num_sms, m->st));
+  return FB_OK;
+}
+
+fb_status run_route(fb_model* m, const fb_route& r) {
+  const double n = (double)r.tokens * r.experts;
+  RouteArgs a;
+  static_cast<fb_route&>(a) = r;
+  KTimer t(m, FB_K_ROUTE, n * (4 + r.top_k),
+           n * type_bytes(r.logits_type) + 16.0 * r.tokens * r.top_k);
+  CK(route(a, m->st));
+  return FB_OK;
+}
+
+// (the work of max_rows rows that reach every expert)
+fb_status run_experts(fb_model* m, const ExpertArgs& g) {
+  const double nw = g.act >= FB_ACT_SWIGLU ? 2.0 * g.n : g.n;
+  KTimer t(m, FB_K_EXPERT, 2.0 * g.max_rows * nw * g.k,
+           2.0 * g.experts * nw * g.k + 2.0 * (g.index ? g.a_rows : g.max_rows) * g.k +
+               type_bytes(g.out_type) * g.max_rows * g.n);
+  CK(expert_gemm(g, m->derr, m->num_sms, m->st));
+  return FB_OK;
+}
+
+bool known_type(int t) { return t == FB_BF16 || t == FB_F32; }
+
+fb_status check_sandwich(const fb_sandwich& s) {
+  if (s.rows < 0 || s.dim < 1 || s.dim > FB_SANDWICH_MAX_DIM)
+    return fail(FB_EINVAL, "rows=%d dim=%d: dim must be in [1, %d]", s.rows, s.dim,
+                FB_SANDWICH_MAX_DIM);
+  if (s.rows > 0 && (!s.h || (!s.h_out && !s.a)))
+    return fail(FB_EINVAL, "null h, or nothing to write");
+  if (!known_type(s.h_type) || (s.y && !known_type(s.y_type)) || (s.a && !known_type(s.a_type)))
+    return fail(FB_EINVAL, "types must be FB_BF16 or FB_F32");
+  for (int k : {s.post, s.pre})
+    if (k < FB_NORM_NONE || k > FB_NORM_LAYER) return fail(FB_EINVAL, "unknown norm %d", k);
+  if (s.ldh < s.dim || (s.h_out && s.ldho < s.dim) || (s.a && s.lda < s.dim) ||
+      (s.y && s.ldy < s.dim))
+    return fail(FB_EINVAL, "a row stride is below dim=%d", s.dim);
+  if (s.group_rows < 0 || (s.group_rows > 0 && s.ldm < s.dim && (s.gate || s.mul || s.add)))
+    return fail(FB_EINVAL, "group_rows=%d needs a modulation row stride of at least dim",
+                s.group_rows);
+  if (s.y) {
+    if (s.parts < 0 || s.parts > FB_SANDWICH_MAX_PARTS)
+      return fail(FB_EINVAL, "parts=%d outside [0, %d]", s.parts, FB_SANDWICH_MAX_PARTS);
+    if (s.parts > 0 && (!s.slot || !s.weight)) return fail(FB_EINVAL, "slot and weight required");
+    if (s.parts == 0 && s.y_rows < s.rows)
+      return fail(FB_EINVAL, "y has %d rows for %d", s.y_rows, s.rows);
+    if (s.y_rows < 0) return fail(FB_EINVAL, "y_rows=%d", s.y_rows);
+  }
+  return FB_OK;
+}
+
+fb_status check_route(const fb_route& r) {
+  if (r.experts < 1 || r.experts > FB_ROUTE_MAX_EXPERTS)
+    return fail(FB_EINVAL, "experts=%d outside [1, %d]", r.experts, FB_ROUTE_MAX_EXPERTS);
+  if (r.top_k < 1 || r.top_k > r.experts || r.top_k > FB_ROUTE_MAX_TOP_K)
+    return fail(FB_EINVAL, "top_k=%d outside [1, min(experts, %d)]", r.top_k, FB_ROUTE_MAX_TOP_K);
+  if (r.tokens < 0 || r.tokens > FB_ROUTE_MAX_PAIRS / r.top_k)
+    return fail(FB_EINVAL, "tokens=%d", r.tokens);
+  if (!r.offsets || (r.tokens > 0 && (!r.logits || !r.expert || !r.weight || !r.slot || !r.token)))
+    return fail(FB_EINVAL, "null argument");
+  if (!known_type(r.logits_type)) return fail(FB_EINVAL, "logits must be FB_BF16 or FB_F32");
+  if (r.ldl < r.experts) return fail(FB_EINVAL, "the logits' row stride is below experts");
+  return FB_OK;
+}
+
+fb_status expert_args(const fb_experts& g, ExpertArgs* out) {
+  if (g.experts < 1 || g.experts > FB_ROUTE_MAX_EXPERTS)
+    return fail(FB_EINVAL, "experts=%d outside [1, %d]", g.experts, FB_ROUTE_MAX_EXPERTS);
+  if (g.max_rows < 0 || g.max_rows > FB_ROUTE_MAX_PAIRS || g.a_rows < 0)
+    return fail(FB_EINVAL, "max_rows=%d a_rows=%d", g.max_rows, g.a_rows);
+  if (g.act < FB_ACT_NONE || g.act > FB_ACT_GEGLU) return fail(FB_EINVAL, "unknown act %d", g.act);
+  const int nm = g.act >= FB_ACT_SWIGLU ? 16 : 8;
+  if (g.n < 1 || g.k < 1 || g.n % nm || g.k % 8)
+    return fail(FB_EINVAL, "n=%d must be a multiple of %d, k=%d of 8", g.n, nm, g.k);
+  if (!g.offsets || (g.max_rows > 0 && (!g.a || !g.w || !g.out)))
+    return fail(FB_EINVAL, "null argument");
+  if (!known_type(g.out_type)) return fail(FB_EINVAL, "out must be FB_BF16 or FB_F32");
+  if (g.lda < g.k || g.ldo < g.n || g.lda % 8 || g.ldo % 8)
+    return fail(FB_EINVAL, "row strides must be multiples of 8, at least k and n");
+  for (const void* p : {g.a, g.w, (const void*)g.out})
+    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(FB_EINVAL, "16-byte alignment required");
+  if (!g.index && g.a_rows < g.max_rows)
+    return fail(FB_EINVAL, "a has %d rows for %d", g.a_rows, g.max_rows);
+  if (g.max_rows > 0 && g.a_rows < 1) return fail(FB_EINVAL, "a is empty");
+  *out = {g.experts, g.n, g.k, g.max_rows, g.a_rows, (const bf16*)g.a, g.lda, g.index, g.offsets,
+          (const bf16*)g.w, g.bias, g.act, g.out, g.out_type, g.ldo};
   return FB_OK;
 }
 
@@ -901,6 +1007,22 @@ fb_status ensure_anchors(fb_model* m, size_t need) {
   }
   CKS(dalloc_t(m, &m->anchors, need));
   m->anchor_elems = need;
+  return FB_OK;
+}
+
+// The scratch of fb_moe_forward holds at least `need` bytes (growing it waits for its users).
+fb_status ensure_moe(fb_model* m, size_t need) {
+  if (need <= m->moe_bytes) return FB_OK;
+  fb_stream_op_not_kernel();
+  CK(cudaStreamSynchronize(m->st));
+  if (m->moe_ws) {
+    cudaFree(m->moe_ws);
+    m->allocs.erase(std::find(m->allocs.begin(), m->allocs.end(), (void*)m->moe_ws));
+    m->moe_ws = nullptr;
+    m->moe_bytes = 0;
+  }
+  CKS(dalloc_t(m, &m->moe_ws, need));
+  m->moe_bytes = need;
   return FB_OK;
 }
 
@@ -1557,7 +1679,7 @@ fb_status fb_reset_stats(fb_model* m) {
 const char* fb_kernel_name(int kind) {
   static const char* names[FB_K_COUNT] = {"gemm_tc", "gemm_simt", "attn_self", "attn_cross",
                                           "ln_mod", "qk_norm_rope", "proxy_add", "patch_embed",
-                                          "head_euler", "small"};
+                                          "head_euler", "small", "sandwich_norm", "route", "expert_gemm"};
   return (kind >= 0 && kind < FB_K_COUNT) ? names[kind] : "?";
 }
 
@@ -1594,6 +1716,112 @@ fb_status fb_op_attention(fb_model* m, const void* Q, int ldq, const void* K, in
   a.heads = heads; a.head_dim = head_dim;
   CKS(begin_call(m));
   for (int r = 0; r < m->op_repeat; ++r) CKS(run_attn(m, a, FB_K_ATTN_SELF, impl));
+  return end_call(m);
+}
+
+fb_status fb_op_sandwich_norm(fb_model* m, const fb_sandwich* s) {
+  if (!m || !s) return fail(FB_EINVAL, "null argument");
+  CKS(check_sandwich(*s));
+  CKS(begin_call(m));
+  for (int r = 0; r < m->op_repeat; ++r) CKS(run_sandwich(m, *s));
+  return end_call(m);
+}
+
+fb_status fb_op_route(fb_model* m, const fb_route* r) {
+  if (!m || !r) return fail(FB_EINVAL, "null argument");
+  CKS(check_route(*r));
+  CKS(begin_call(m));
+  for (int i = 0; i < m->op_repeat; ++i) CKS(run_route(m, *r));
+  return end_call(m);
+}
+
+fb_status fb_op_expert_gemm(fb_model* m, const fb_experts* g) {
+  if (!m || !g) return fail(FB_EINVAL, "null argument");
+  ExpertArgs a;
+  CKS(expert_args(*g, &a));
+  CKS(begin_call(m));
+  for (int r = 0; r < m->op_repeat; ++r) CKS(run_experts(m, a));
+  return end_call(m);
+}
+
+fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const uint8_t* valid,
+                         const fb_sandwich* s0) {
+  if (!m || !moe || !s0 || !a || !moe->router_w) return fail(FB_EINVAL, "null argument");
+  if (s0->y || s0->slot || s0->weight)
+    return fail(FB_EINVAL, "y, slot and weight are the call's own: they must be NULL");
+  if (moe->dim != s0->dim) return fail(FB_EINVAL, "dim=%d, s->dim=%d", moe->dim, s0->dim);
+  if (moe->hidden < 1 || moe->dim % 16 || moe->hidden % 16)
+    return fail(FB_EINVAL, "dim=%d and hidden=%d must be multiples of 16", moe->dim, moe->hidden);
+  if (moe->router_rows < moe->experts || moe->router_rows % 8)
+    return fail(FB_EINVAL, "router_rows=%d must be a multiple of 8, at least experts",
+                moe->router_rows);
+  CKS(check_sandwich(*s0));
+  fb_route r{};
+  r.tokens = s0->rows;
+  r.experts = moe->experts;
+  r.top_k = moe->top_k;
+  r.logits = a;  // (any address: the scratch buffers are not laid out yet)
+  r.logits_type = FB_F32;
+  r.ldl = moe->router_rows;
+  r.valid = valid;
+  r.renorm = moe->renorm;
+  if (r.top_k < 1 || r.tokens > FB_ROUTE_MAX_PAIRS / r.top_k)
+    return fail(FB_EINVAL, "rows=%d top_k=%d", r.tokens, r.top_k);
+  const size_t T = r.tokens, S = T * r.top_k;
+  // scratch: hidden rows, expert rows, logits, the router's lists
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += (bytes + 255) / 256 * 256;
+    return o;
+  };
+  const size_t o_hid = take(S * moe->hidden * sizeof(bf16)), o_y = take(S * moe->dim * sizeof(bf16)),
+               o_log = take(T * moe->router_rows * sizeof(float)), o_exp = take(S * 4),
+               o_w = take(S * 4), o_slot = take(S * 4), o_tok = take(S * 4),
+               o_off = take((FB_ROUTE_MAX_EXPERTS + 1) * 4);
+  uint8_t* ws = nullptr;
+  fb_experts up{}, down{};
+  fb_sandwich s = *s0;
+  auto lay_out = [&] {
+    r.logits = ws + o_log;
+    r.expert = (int32_t*)(ws + o_exp);
+    r.weight = (float*)(ws + o_w);
+    r.slot = (int32_t*)(ws + o_slot);
+    r.token = (int32_t*)(ws + o_tok);
+    r.offsets = (int32_t*)(ws + o_off);
+    up = {moe->experts, moe->hidden, moe->dim, (int)S, (int)T, a, moe->dim, r.token, r.offsets,
+          moe->w1, moe->b1, moe->act, ws + o_hid, FB_BF16, moe->hidden};
+    down = {moe->experts, moe->dim, moe->hidden, (int)S, (int)S, ws + o_hid, moe->hidden, nullptr,
+            r.offsets, moe->w2, moe->b2, FB_ACT_NONE, ws + o_y, FB_BF16, moe->dim};
+    s.y = ws + o_y;
+    s.y_type = FB_BF16;
+    s.y_rows = (int)S;
+    s.parts = r.top_k;
+    s.ldy = moe->dim;
+    s.slot = r.slot;
+    s.weight = r.weight;
+  };
+  // every argument is checked before the scratch is sized and anything runs
+  ws = reinterpret_cast<uint8_t*>(uintptr_t(256));
+  lay_out();
+  ExpertArgs gu, gd;
+  CKS(check_route(r));
+  CKS(expert_args(up, &gu));
+  CKS(expert_args(down, &gd));
+  CKS(check_sandwich(s));
+  if (T == 0) return FB_OK;
+  CKS(begin_call(m));
+  CKS(ensure_moe(m, at));
+  ws = m->moe_ws;
+  lay_out();
+  CKS(expert_args(up, &gu));
+  CKS(expert_args(down, &gd));
+  CKS(run_gemm(m, gemm_args((int)T, moe->router_rows, moe->dim, (const bf16*)a,
+                            (const bf16*)moe->router_w, nullptr, EPI_RESID, ws + o_log)));
+  CKS(run_route(m, r));
+  CKS(run_experts(m, gu));
+  CKS(run_experts(m, gd));
+  CKS(run_sandwich(m, s));
   return end_call(m);
 }
 

@@ -8,7 +8,8 @@
 typedef __nv_bfloat16 bf16;
 
 // Error codes a kernel writes to the model's device error word.
-enum { FB_DEVERR_NONE = 0, FB_DEVERR_WAIT_TIMEOUT = 1, FB_DEVERR_BAD_ARG = 2 };
+enum { FB_DEVERR_NONE = 0, FB_DEVERR_WAIT_TIMEOUT = 1, FB_DEVERR_BAD_ARG = 2,
+       FB_DEVERR_BAD_INDEX = 3 };
 
 // A kernel's error record (16 bytes, 8-byte aligned): the error word at err[0], zero while all
 // is well, and at err + 2 the address of a second copy in mapped host memory, or null. The

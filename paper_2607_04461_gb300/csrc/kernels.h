@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "common.cuh"
+#include "flashbon.h"
 
 // ---- GEMM: out[M][N] = epilogue(A[M][K] * W[N][K]^T) --------------------------------
 struct GemmArgs {
@@ -138,6 +139,25 @@ cudaError_t gemv(const bf16* W, const float* b, const float* x, const GemvOut& o
 // emb[s] = [cos(1000 t_s f_k), sin(1000 t_s f_k)], f_k = 10000^(-k/half).
 cudaError_t timestep_sincos(const CondSteps& ts, int ns, int dim, float* emb, cudaStream_t st);
 cudaError_t f32_to_bf16(const float* x, bf16* y, size_t n, cudaStream_t st);
+
+// ---- mixture of experts between two norms (flashbon.h has the definitions) -------------
+struct SandwichArgs : fb_sandwich {};
+cudaError_t sandwich_norm(const SandwichArgs& s, int* err, int num_sms, cudaStream_t st);
+struct RouteArgs : fb_route {};
+cudaError_t route(const RouteArgs& r, cudaStream_t st);
+struct ExpertArgs {
+  int experts, n, k, max_rows, a_rows;
+  const bf16* A;
+  int64_t lda;
+  const int32_t *index, *offsets;
+  const bf16* W;
+  const float* bias;
+  int act;
+  void* out;
+  int out_type;
+  int64_t ldo;
+};
+cudaError_t expert_gemm(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st);
 
 // ---- measurement probe ----------------------------------------------------------------
 // One CTA per entry of `grid`, each timing (SM clock cycles, cycles[cta]) `reps` tcgen05.mma

@@ -4,6 +4,8 @@ fallback: if the library is missing, loading raises.
 
 Buffers may be numpy arrays (host memory) or torch tensors (host or CUDA); they are
 passed to the library as raw pointers and must be contiguous float32 / uint8 / int32.
+The make_sandwich, make_route and make_experts arguments are CUDA tensors, whose rows may be
+further apart than they are long.
 """
 from __future__ import annotations
 
@@ -19,7 +21,8 @@ LIB_PATH = os.path.join(_HERE, "libflashbon.so")
 
 FB_OK, FB_EINVAL, FB_ENOMEM, FB_ECUDA, FB_EPLAN, FB_ESTATE = range(6)
 KERNEL_KINDS = ["gemm_tc", "gemm_simt", "attn_self", "attn_cross", "ln_mod", "qk_norm_rope",
-                "proxy_add", "patch_embed", "head_euler", "small"]
+                "proxy_add", "patch_embed", "head_euler", "small", "sandwich_norm", "route",
+                "expert_gemm"]
 K = {name: i for i, name in enumerate(KERNEL_KINDS)}
 
 
@@ -48,6 +51,48 @@ class fb_kstat(ctypes.Structure):
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
 
 
+class fb_sandwich(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("dim", ctypes.c_int),
+                ("h", ctypes.c_void_p), ("h_type", ctypes.c_int), ("ldh", ctypes.c_int64),
+                ("y", ctypes.c_void_p), ("y_type", ctypes.c_int), ("y_rows", ctypes.c_int),
+                ("parts", ctypes.c_int), ("ldy", ctypes.c_int64), ("slot", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("post", ctypes.c_int), ("post_eps", ctypes.c_float),
+                ("post_w", ctypes.c_void_p), ("post_b", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("resid_scale", ctypes.c_float),
+                ("h_out", ctypes.c_void_p), ("ldho", ctypes.c_int64), ("pre", ctypes.c_int),
+                ("pre_eps", ctypes.c_float), ("mul_base", ctypes.c_float),
+                ("mul", ctypes.c_void_p), ("add", ctypes.c_void_p), ("a", ctypes.c_void_p),
+                ("a_type", ctypes.c_int), ("lda", ctypes.c_int64), ("group_rows", ctypes.c_int),
+                ("ldm", ctypes.c_int64)]
+
+
+class fb_route(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int), ("experts", ctypes.c_int), ("top_k", ctypes.c_int),
+                ("logits", ctypes.c_void_p), ("logits_type", ctypes.c_int),
+                ("ldl", ctypes.c_int64), ("valid", ctypes.c_void_p), ("renorm", ctypes.c_int),
+                ("expert", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("slot", ctypes.c_void_p), ("token", ctypes.c_void_p),
+                ("offsets", ctypes.c_void_p)]
+
+
+class fb_experts(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int), ("n", ctypes.c_int), ("k", ctypes.c_int),
+                ("max_rows", ctypes.c_int), ("a_rows", ctypes.c_int), ("a", ctypes.c_void_p),
+                ("lda", ctypes.c_int64), ("index", ctypes.c_void_p), ("offsets", ctypes.c_void_p),
+                ("w", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("act", ctypes.c_int),
+                ("out", ctypes.c_void_p), ("out_type", ctypes.c_int), ("ldo", ctypes.c_int64)]
+
+
+class fb_moe(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("dim", "hidden", "experts", "top_k", "renorm", "act",
+                                            "router_rows")] + [
+        (n, ctypes.c_void_p) for n in ("router_w", "w1", "w2", "b1", "b2")]
+
+
+FB_BF16, FB_F32 = 0, 1
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+ACTS = {"none": 0, "gelu": 1, "swiglu": 2, "geglu": 3}
+
 EXPORTS = ["fb_weights_count", "fb_weights_entry", "fb_init_model", "fb_free", "fb_set_stream",
            "fb_encode_text", "fb_draft", "fb_refine", "fb_plan_from_phi", "fb_block_forward",
            "fb_last_error", "fb_set_timing", "fb_get_stats", "fb_reset_stats", "fb_kernel_name",
@@ -58,7 +103,8 @@ EXPORTS = ["fb_weights_count", "fb_weights_entry", "fb_init_model", "fb_free", "
            "fb_test_fail_alloc", "fb_test_alloc_calls", "fb_test_poison_counters",
            "fb_test_request_handover", "fb_test_attention_split", "fb_test_plan_traffic",
            "fb_probe_mma_rate", "fb_probe_mma_gap", "fb_probe_mufu", "fb_probe_tmem_load",
-           "fb_probe_mma_mix"]
+           "fb_probe_mma_mix", "fb_op_sandwich_norm", "fb_op_route", "fb_op_expert_gemm",
+           "fb_moe_forward"]
 
 PAIR_VERIFIER = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
                                  ctypes.POINTER(ctypes.c_int))
@@ -117,6 +163,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "fb_test_plan_traffic": (I, [ctypes.POINTER(fb_cfg), P, I, P, P, S, ctypes.POINTER(I),
                                      ctypes.POINTER(I), ctypes.POINTER(D)]),
         "fb_test_attention_split": (I, [P, I, I, I, I, I, ctypes.POINTER(I)]),
+        "fb_op_sandwich_norm": (I, [P, ctypes.POINTER(fb_sandwich)]),
+        "fb_op_route": (I, [P, ctypes.POINTER(fb_route)]),
+        "fb_op_expert_gemm": (I, [P, ctypes.POINTER(fb_experts)]),
+        "fb_moe_forward": (I, [P, ctypes.POINTER(fb_moe), P, P, ctypes.POINTER(fb_sandwich)]),
         "fb_probe_mma_rate": (I, [I, I, I, ctypes.POINTER(ctypes.c_double)]),
         "fb_probe_mma_gap": (I, [I, ctypes.POINTER(ctypes.c_double)]),
         "fb_probe_mufu": (I, [I, ctypes.POINTER(ctypes.c_double)]),
@@ -502,6 +552,165 @@ def fb_op_attention(model, Q, ldq, Kt, ldk, V, ldv, O, ldo, batch, Lq, Lkv, kv_b
                                           head_dim, impl))
 
 
+# ---- mixture-of-experts feed-forward between two norms ----------------------------------
+# make_* build the argument structures from CUDA tensors; they keep references to the tensors
+# and can be used for any number of calls.
+
+def _tensor(name, x, dtypes, shape, rows=False):
+    """The pointer of CUDA tensor x (None: null) after a check of its type and shape (None in
+    shape: any size); contiguous, or with `rows` only along each row."""
+    if x is None:
+        return None
+    if not getattr(x, "is_cuda", False):
+        raise TypeError(f"{name}: expected a CUDA tensor")
+    if str(x.dtype).removeprefix("torch.") not in dtypes:
+        raise TypeError(f"{name}: expected {' or '.join(dtypes)}, got {x.dtype}")
+    if x.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, x.shape)):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
+    if rows:
+        if x.shape[1] > 1 and x.stride(1) != 1:
+            raise ValueError(f"{name}: rows must be contiguous")
+    elif not x.is_contiguous():
+        raise ValueError(f"{name}: tensor must be contiguous")
+    return x.data_ptr()
+
+
+_FLOATS = ("bfloat16", "float32")
+
+
+def _row_stride(x):
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1])
+
+
+def _type(x):
+    return FB_F32 if x.dtype.itemsize == 4 else FB_BF16
+
+
+def make_sandwich(h, y=None, slot=None, weight=None, post="none", post_eps=1e-6, post_w=None,
+                  post_b=None, gate=None, resid_scale=1.0, h_out=None, pre="none", pre_eps=1e-6,
+                  mul_base=1.0, mul=None, add=None, a=None, group_rows=0):
+    """fb_sandwich for fb_op_sandwich_norm. h [rows][dim] bf16 or fp32; y [rows][dim], or with
+    slot and weight ([rows][parts] int32 and fp32) the rows that slot points to; norms "none",
+    "rms" or "layer"; gate, mul and add [groups][dim] fp32, row r // group_rows of them for row
+    r (one row and group_rows 0: the same for all); h_out (may be h) and a [rows][dim]."""
+    rows, dim = h.shape
+    s = fb_sandwich(rows=rows, dim=dim, resid_scale=resid_scale, post=NORMS[post],
+                    post_eps=post_eps, pre=NORMS[pre], pre_eps=pre_eps, mul_base=mul_base,
+                    group_rows=group_rows)
+    s.h, s.h_type, s.ldh = _tensor("h", h, _FLOATS, (rows, dim), True), _type(h), _row_stride(h)
+    if y is not None:
+        s.y, s.y_type = _tensor("y", y, _FLOATS, (None, dim), True), _type(y)
+        s.y_rows, s.ldy = y.shape[0], _row_stride(y)
+    if slot is not None:
+        if y is None or weight is None:
+            raise ValueError("slot needs y and weight")
+        s.parts = slot.shape[1]
+        if s.parts < 1:
+            raise ValueError("slot: at least one part")
+        s.slot = _tensor("slot", slot, ("int32",), (rows, s.parts))
+        s.weight = _tensor("weight", weight, ("float32",), (rows, s.parts))
+    s.post_w = _tensor("post_w", post_w, ("float32",), (dim,))
+    s.post_b = _tensor("post_b", post_b, ("float32",), (dim,))
+    groups = -(-rows // group_rows) if group_rows > 0 else 1
+    strides = set()
+    for name, x in (("gate", gate), ("mul", mul), ("add", add)):
+        if x is None:
+            continue
+        setattr(s, name, _tensor(name, x, ("float32",), (None, dim), True))
+        if x.shape[0] < groups:
+            raise ValueError(f"{name}: {x.shape[0]} rows for {groups} groups")
+        strides.add(_row_stride(x))
+    if len(strides) > 1 and groups > 1:
+        raise ValueError("gate, mul and add must have the same row stride")
+    s.ldm = max(strides, default=dim)
+    if h_out is not None:
+        s.h_out = _tensor("h_out", h_out, (str(h.dtype).removeprefix("torch."),), (rows, dim), True)
+        s.ldho = _row_stride(h_out)
+    if a is not None:
+        s.a, s.a_type = _tensor("a", a, _FLOATS, (rows, dim), True), _type(a)
+        s.lda = _row_stride(a)
+    s._keep = (h, y, slot, weight, post_w, post_b, gate, mul, add, h_out, a)
+    return s
+
+
+def make_route(logits, expert, weight, slot, token, offsets, valid=None, renorm=False):
+    """fb_route for fb_op_route. logits [tokens][experts] bf16 or fp32; expert, slot int32 and
+    weight fp32 [tokens][top_k], token int32 [tokens * top_k], offsets int32 [experts + 1];
+    valid [tokens] uint8 or None."""
+    tokens, experts = logits.shape
+    k = expert.shape[1]
+    r = fb_route(tokens=tokens, experts=experts, top_k=k, renorm=int(bool(renorm)))
+    r.logits = _tensor("logits", logits, _FLOATS, (tokens, experts), True)
+    r.logits_type, r.ldl = _type(logits), _row_stride(logits)
+    r.valid = _tensor("valid", valid, ("uint8",), (tokens,))
+    r.expert = _tensor("expert", expert, ("int32",), (tokens, k))
+    r.weight = _tensor("weight", weight, ("float32",), (tokens, k))
+    r.slot = _tensor("slot", slot, ("int32",), (tokens, k))
+    r.token = _tensor("token", token, ("int32",), (tokens * k,))
+    r.offsets = _tensor("offsets", offsets, ("int32",), (experts + 1,))
+    r._keep = (logits, valid, expert, weight, slot, token, offsets)
+    return r
+
+
+def make_experts(a, w, offsets, out, index=None, bias=None, act="none"):
+    """fb_experts for fb_op_expert_gemm. a [a_rows][k] bf16; w [experts][n or 2 n][k] bf16;
+    offsets [experts + 1] and index [max_rows] int32; bias [experts][n or 2 n] fp32; out
+    [max_rows][n] bf16 or fp32; act "none", "gelu", "swiglu" or "geglu" (the last two: the n
+    gate rows of w and bias before the n up rows)."""
+    experts, nw, k = w.shape
+    gated = ACTS[act] >= ACTS["swiglu"]
+    if gated and nw % 2:
+        raise ValueError("w: gate rows and up rows differ in number")
+    n = nw // 2 if gated else nw
+    g = fb_experts(experts=experts, n=n, k=k, max_rows=out.shape[0], a_rows=a.shape[0],
+                   act=ACTS[act])
+    g.a, g.lda = _tensor("a", a, ("bfloat16",), (None, k), True), _row_stride(a)
+    g.w = _tensor("w", w, ("bfloat16",), (experts, nw, k))
+    g.offsets = _tensor("offsets", offsets, ("int32",), (experts + 1,))
+    g.index = _tensor("index", index, ("int32",), (out.shape[0],))
+    g.bias = _tensor("bias", bias, ("float32",), (experts, nw))
+    g.out, g.out_type = _tensor("out", out, _FLOATS, (None, n), True), _type(out)
+    g.ldo = _row_stride(out)
+    g._keep = (a, w, offsets, out, index, bias)
+    return g
+
+
+def make_moe(router_w, w1, w2, top_k, b1=None, b2=None, act="gelu", renorm=False):
+    """fb_moe for fb_moe_forward. router_w [router_rows][dim] bf16 (padded rows behind the
+    experts are ignored); w1 [experts][hidden or 2 hidden][dim], w2 [experts][dim][hidden] bf16;
+    biases fp32."""
+    experts, dim, hidden = w2.shape
+    nw = 2 * hidden if ACTS[act] >= ACTS["swiglu"] else hidden
+    p = fb_moe(dim=dim, hidden=hidden, experts=experts, top_k=top_k, renorm=int(bool(renorm)),
+               act=ACTS[act], router_rows=router_w.shape[0])
+    p.router_w = _tensor("router_w", router_w, ("bfloat16",), (None, dim))
+    p.w1 = _tensor("w1", w1, ("bfloat16",), (experts, nw, dim))
+    p.w2 = _tensor("w2", w2, ("bfloat16",), (experts, dim, hidden))
+    p.b1 = _tensor("b1", b1, ("float32",), (experts, nw))
+    p.b2 = _tensor("b2", b2, ("float32",), (experts, dim))
+    p._keep = (router_w, w1, w2, b1, b2)
+    return p
+
+
+def fb_op_sandwich_norm(model: int, args: fb_sandwich) -> None:
+    _check(load_library().fb_op_sandwich_norm(model, ctypes.byref(args)))
+
+
+def fb_op_route(model: int, args: fb_route) -> None:
+    _check(load_library().fb_op_route(model, ctypes.byref(args)))
+
+
+def fb_op_expert_gemm(model: int, args: fb_experts) -> None:
+    _check(load_library().fb_op_expert_gemm(model, ctypes.byref(args)))
+
+
+def fb_moe_forward(model: int, moe: fb_moe, a, sandwich: fb_sandwich, valid=None) -> None:
+    """a: the normed input, bf16 [rows][dim]; valid: uint8 [rows] or None."""
+    _check(load_library().fb_moe_forward(
+        model, ctypes.byref(moe), _tensor("a", a, ("bfloat16",), (sandwich.rows, moe.dim)),
+        _tensor("valid", valid, ("uint8",), (sandwich.rows,)), ctypes.byref(sandwich)))
+
+
 class Model:
     """Owns an fb_model handle; methods forward to the fb_* functions."""
 
@@ -560,6 +769,18 @@ class Model:
 
     def block_forward(self, layer, h, n, t):
         fb_block_forward(self.handle, layer, h, n, t)
+
+    def op_sandwich_norm(self, args):
+        fb_op_sandwich_norm(self.handle, args)
+
+    def op_route(self, args):
+        fb_op_route(self.handle, args)
+
+    def op_expert_gemm(self, args):
+        fb_op_expert_gemm(self.handle, args)
+
+    def moe_forward(self, moe, a, sandwich, valid=None):
+        fb_moe_forward(self.handle, moe, a, sandwich, valid)
 
     def set_timing(self, mask):
         fb_set_timing(self.handle, mask)

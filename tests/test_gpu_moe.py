@@ -1,0 +1,552 @@
+"""The operators of a mixture-of-experts feed-forward between two norms, through the public
+calls, against their definitions in float64.
+
+Tolerances, from the arithmetic:
+  * fp32 elementwise chains and row sums: a row of D values is summed in at most D / 32 + 16
+    additions that follow one another, so a statistic is off by at most (D / 32 + 16) 6e-8
+    (the row sums' errors are random: half of it covers them); every further operation adds 6e-8 of
+    its operands' size. Each element is compared with the sum of its terms' sizes.
+  * rounding to bf16: 2^-8 of the value (8 significant bits, half a unit of the last one).
+  * products: a 64-wide K block is four MMAs, each of which may cut the running sum by one
+    fp32 unit, 1.2e-7 of it. The largest result stands for the running sum.
+  * bf16 results of GELU and SiLU take the hardware tanh, 2^-10.9 of tanh, which x / 2 multiplies.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_04461_gb300 import flashbon as fb
+from paper_2607_04461_gb300 import synth
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def model():
+    m = fb.Model(synth.TINY, synth.make_weights(synth.TINY))
+    yield m
+    m.close()
+
+
+def gen(seed):
+    return torch.Generator("cuda").manual_seed(seed)
+
+
+def padded(x, pad, fill=7.0):
+    wide = torch.full((x.shape[0], x.shape[1] + pad), fill, dtype=x.dtype, device="cuda")
+    wide[:, :x.shape[1]] = x
+    return wide[:, :x.shape[1]]
+
+
+# ---- norms around a block -------------------------------------------------------------
+
+def norm64(x, size, kind, eps):
+    """The norm in float64, and the size of its terms."""
+    if kind == "none":
+        return x, size
+    mean = x.mean(1, keepdim=True) if kind == "layer" else torch.zeros_like(x[:, :1])
+    rstd = 1 / (((x - mean) ** 2).mean(1, keepdim=True) + eps).sqrt()
+    return (x - mean) * rstd, (size + mean.abs()) * rstd
+
+
+def sandwich_case(model, rows, D, parts=0, y_t=BF, h_t=F32, a_t=BF, post="rms", pre="layer",
+                  group=0, pad=0, seed=0, gate=True, mods=True, affine=True, in_place=False,
+                  with_y=True, drop=0.2, y_off=0.0, scale=0.75, mul_base=1.0, eps=1e-6):
+    g = gen(1000 + seed)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    h = padded((3 * randn(rows, D) + 0.5).to(h_t), pad)
+    h0 = h.clone()
+    y = slot = weight = None
+    if with_y:
+        y = padded((randn(rows * max(1, parts) + 3, D) + y_off).to(y_t), pad)
+    if parts:
+        slot = torch.randperm(rows * parts, generator=g, device="cuda").view(rows, parts)
+        gone = torch.rand(rows, parts, generator=g, device="cuda") < drop
+        if rows > 2:
+            gone[1] = True  # a token without any expert
+        weight = torch.rand(rows, parts, generator=g, device="cuda")
+        y[slot[gone]] = float("nan")
+        slot, weight = slot.masked_fill(gone, -1).int(), weight.masked_fill(gone, math.inf)
+    groups = -(-rows // group) if group else 1
+    wide = randn(groups, 3 * D + 4) if mods else None  # gate, mul, add side by side
+    gt = wide[:, :D] if gate and mods else None
+    mul, add = (wide[:, D:2 * D], wide[:, 2 * D:3 * D]) if mods else (None, None)
+    pw, pb = (1 + 0.2 * randn(D), 0.1 * randn(D)) if affine else (None, None)
+    h_out = h if in_place else padded(torch.full((rows, D), 5.0, device="cuda").to(h_t), pad)
+    a = padded(torch.full((rows, D), 5.0, device="cuda").to(a_t), pad) if pre is not None else None
+    s = fb.make_sandwich(h, y=y, slot=slot, weight=weight, post=post, post_eps=eps, post_w=pw,
+                         post_b=pb, gate=gt, resid_scale=scale, h_out=h_out, pre=pre or "none",
+                         pre_eps=eps, mul_base=mul_base, mul=mul, add=add, a=a, group_rows=group)
+    model.op_sandwich_norm(s)
+    torch.cuda.synchronize()
+
+    of = torch.arange(rows, device="cuda") // group if group else torch.zeros(rows, device="cuda").long()
+    per = lambda x, none: torch.full((1, 1), none, device="cuda").double() if x is None else x.double()[of]  # noqa: E731
+    hd = h0.double()
+    want, size = scale * hd, (scale * hd).abs()
+    if with_y:
+        if parts:
+            yd, ysize = torch.zeros_like(hd), torch.zeros_like(hd)
+            for j in range(parts):
+                ok = (slot[:, j] >= 0).nonzero()[:, 0]
+                t = weight[ok, j, None].double() * y[slot[ok, j].long()].double()
+                yd[ok] += t
+                ysize[ok] += t.abs()
+        else:
+            yd = y[:rows].double()
+            ysize = yd.abs()
+        u, usize = norm64(yd, ysize, post, eps)
+        if affine:
+            u, usize = u * pw.double() + pb.double(), usize * pw.double().abs() + pb.double().abs()
+        want = want + per(gt, 1.0) * u
+        size = size + per(gt, 1.0).abs() * usize
+    unit = 0.5 * (D / 32 + 16) * 6e-8 + 10 * 6e-8
+    check(h_out, want, unit * size, h_t)
+    if a is not None:
+        n, nsize = norm64(want, size, pre, eps)
+        f = mul_base + (mul.double()[of] if mods else 0.0)
+        want_a = n * f + per(add, 0.0)
+        check(a, want_a, 2 * unit * (nsize * (abs(f) if not mods else f.abs()) + per(add, 0.0).abs()), a_t)
+    if pad:  # what lies between the rows
+        for x in (h_out, a):
+            if x is not None:
+                base = x.as_strided((rows, D + pad), (D + pad, 1))
+                assert torch.all(base[:, D:] == 7.0)
+
+
+def check(got, want, tol, dtype):
+    assert torch.isfinite(got.float()).all()
+    if dtype == BF:
+        tol = tol + 2.0 ** -8 * (want.abs() + tol)
+    bad = (got.double() - want).abs() - tol
+    assert bad.max().item() <= 0, f"{bad.max().item():.3e} over, {(bad > 0).sum().item()} elements"
+
+
+@pytest.mark.parametrize("rows,D", [
+    (1, 1), (3, 7), (5, 8), (2, 33), (9, 128), (1, 1536), (7, 1536), (300, 1536), (1561, 1536),
+    (33, 1000), (12, 1235), (65, 2048), (17, 2056), (31, 5120), (6, 6001), (5, 8192), (3, 9000), (2, 16384),
+    (4, 16383),
+])
+@pytest.mark.parametrize("post,pre", [("rms", "layer"), ("layer", "rms"), ("none", "none")])
+def test_sandwich_widths(model, rows, D, post, pre):
+    sandwich_case(model, rows, D, post=post, pre=pre, seed=D)
+
+
+@pytest.mark.parametrize("y_t", [BF, F32])
+@pytest.mark.parametrize("h_t", [BF, F32])
+@pytest.mark.parametrize("a_t", [BF, F32])
+@pytest.mark.parametrize("D,pad", [(256, 0), (256, 8), (256, 3), (1536, 4), (777, 1)])
+def test_sandwich_types_and_strides(model, y_t, h_t, a_t, D, pad):
+    sandwich_case(model, 37, D, y_t=y_t, h_t=h_t, a_t=a_t, pad=pad, parts=0, seed=pad)
+    sandwich_case(model, 37, D, y_t=y_t, h_t=h_t, a_t=a_t, pad=pad, parts=2, seed=pad, in_place=True)
+
+
+@pytest.mark.parametrize("parts", [1, 2, 3, 8, 16])
+@pytest.mark.parametrize("rows,D", [(1, 256), (40, 1536), (130, 515)])
+def test_sandwich_combines_expert_rows(model, parts, rows, D):
+    """Rows without some of their experts, or any; rows that nothing points to hold NaN and
+    the weights of missing ones infinity."""
+    sandwich_case(model, rows, D, parts=parts, seed=parts)
+    sandwich_case(model, rows, D, parts=parts, seed=parts, drop=1.1, y_t=F32)
+
+
+@pytest.mark.parametrize("group", [1, 7, 100, 4000])
+def test_sandwich_modulation_groups(model, group):
+    sandwich_case(model, 100, 1536, group=group, seed=group)
+    sandwich_case(model, 100, 100, group=group, seed=group, h_t=BF)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(with_y=False), dict(with_y=False, scale=1.0, pre="rms"), dict(pre=None), dict(gate=False),
+    dict(mods=False), dict(affine=False), dict(affine=False, mods=False, post="layer"),
+    dict(mul_base=0.0), dict(scale=0.0), dict(scale=-1.5, in_place=True),
+    dict(y_off=100.0, post="layer"), dict(y_off=-30.0, post="rms", eps=1e-3),
+])
+@pytest.mark.parametrize("D", [640, 1536, 1001])
+def test_sandwich_parts_left_out(model, D, kw):
+    sandwich_case(model, 50, D, seed=5, **kw)
+
+
+def test_sandwich_many_rows(model):
+    """More rows than one wave holds, for each row's own place in the outputs."""
+    sandwich_case(model, 49920, 1536, group=1560, seed=3)
+    sandwich_case(model, 20001, 1536, parts=2, seed=4)
+    sandwich_case(model, 9001, 5120, seed=6)
+
+
+def test_sandwich_special_values(model):
+    """A row with a NaN or an infinity stays its own; a constant row has no variance."""
+    D = 1536
+    y = torch.randn(6, D, device="cuda").to(BF)
+    y[1, 5], y[2, 700] = float("nan"), float("inf")
+    y[3] = 3.0
+    h = torch.randn(6, D, device="cuda")
+    a, h_out = torch.zeros(6, D, device="cuda"), torch.zeros(6, D, device="cuda")
+    model.op_sandwich_norm(fb.make_sandwich(h, y=y, post="layer", pre="rms", a=a, h_out=h_out))
+    assert torch.isnan(a[1]).all() and torch.isnan(a[2]).all()
+    assert torch.equal(h_out[3], h[3])  # (3 - 3) rstd = 0
+    for r in (0, 3, 4, 5):
+        assert torch.isfinite(a[r]).all() and torch.isfinite(h_out[r]).all()
+
+
+def test_sandwich_slot_out_of_range(model):
+    y, h = torch.randn(4, 256, device="cuda").to(BF), torch.randn(3, 256, device="cuda")
+    slot = torch.tensor([[0], [4], [1]], dtype=torch.int32, device="cuda")
+    w = torch.ones(3, 1, device="cuda")
+    h_out = torch.zeros_like(h)
+    with pytest.raises(fb.FlashBonError) as e:
+        model.op_sandwich_norm(fb.make_sandwich(h, y=y, slot=slot, weight=w, h_out=h_out))
+    assert e.value.status == fb.FB_EINVAL
+    slot[1] = 3  # the next call finds nothing left of it
+    model.op_sandwich_norm(fb.make_sandwich(h, y=y, slot=slot, weight=w, h_out=h_out))
+    assert torch.allclose(h_out, h + y[slot[:, 0].long()].float())
+
+
+# ---- router ---------------------------------------------------------------------------
+
+def route64(logits, valid, k, renorm):
+    """One token and one expert at a time, in numpy."""
+    x = logits.float().cpu().numpy().astype(np.float64)
+    T, E = x.shape
+    x = np.where(np.isnan(x), -np.inf, np.minimum(x, np.finfo(np.float32).max))
+    if valid is not None:
+        x[valid.cpu().numpy() == 0] = -np.inf
+    expert, weight = np.full((T, k), -1), np.zeros((T, k))
+    slot, lists = np.full((T, k), -1), [[] for _ in range(E)]
+    for t in range(T):
+        order = [e for e in np.argsort(-x[t], kind="stable") if x[t, e] > -np.inf]
+        got = order[:k]
+        if got:
+            p = np.exp(x[t, got if renorm else order] - x[t, got[0]])
+            weight[t, :len(got)] = np.exp(x[t, got] - x[t, got[0]]) / p.sum()
+        expert[t, :len(got)] = got
+        for j, e in enumerate(got):
+            lists[e].append((t, j))
+    offsets, token = np.cumsum([0] + [len(v) for v in lists]), np.full(T * k, -1)
+    for e, v in enumerate(lists):
+        for i, (t, j) in enumerate(v):
+            slot[t, j], token[offsets[e] + i] = offsets[e] + i, t
+    return expert, weight, slot, token, offsets
+
+
+def route_buffers(T, E, k):
+    i32 = dict(dtype=torch.int32, device="cuda")
+    return (torch.full((T, k), 99, **i32), torch.full((T, k), 9.0, device="cuda"),
+            torch.full((T, k), 99, **i32), torch.full((T * k,), 99, **i32), torch.full((E + 1,), 99, **i32))
+
+
+def route_case(model, logits, k, valid=None, renorm=False):
+    T, E = logits.shape
+    out = route_buffers(T, E, k)
+    r = fb.make_route(logits, *out, valid=valid, renorm=renorm)
+    want = route64(logits, valid, k, renorm)
+    for _ in range(2):  # (the second call finds the workspace as the first left it)
+        model.op_route(r)
+        for name, g, w in zip(("expert", "weight", "slot", "token", "offsets"), out, want):
+            if name != "weight":
+                assert np.array_equal(g.cpu().numpy(), w), name
+        # exp of a difference: 2 units and 6e-8 of its size; a sum of E / 32 + 5 terms
+        tol = 6e-8 * (4 + E / 32 + 5 + 40)
+        assert (np.abs(out[1].cpu().numpy() - want[1]) <= tol * want[1] + 1e-37).all()
+
+
+@pytest.mark.parametrize("T,E,k", [
+    (1, 1, 1), (1, 8, 2), (1, 512, 16), (2, 3, 3), (5, 33, 4), (31, 8, 8), (100, 64, 8),
+    (257, 256, 8), (513, 2, 1), (1000, 5, 2), (1560, 8, 2), (3000, 160, 6), (4097, 64, 1),
+    (700, 512, 16), (9001, 16, 4), (33000, 8, 2),
+])
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_route(model, T, E, k, dtype):
+    g = gen(T * 7 + E)
+    x = torch.randn(T, E, generator=g, device="cuda")
+    route_case(model, x.to(dtype), k, renorm=bool(T % 2))
+
+
+@pytest.mark.parametrize("k", [1, 2, 6])
+@pytest.mark.parametrize("E", [6, 40, 300])
+def test_route_ties_masks_and_padding(model, E, k):
+    g = gen(E + k)
+    T = 400
+    x = torch.randint(-3, 4, (T, E), generator=g, device="cuda").float() * 0.25  # many ties
+    x[::5] = x[::5] * -0.0                                 # -0 and +0 are equal
+    x[torch.rand(T, E, generator=g, device="cuda") < 0.6] = -math.inf
+    x[3] = -math.inf                                       # no expert left
+    x[7] = float("nan")
+    x[8, 1], x[9, 2], x[9, 4] = float("nan"), math.inf, math.inf
+    x[10] = torch.finfo(F32).min                           # the lowest value is a value
+    x[11] = -math.inf
+    x[11, E - 1] = -1e30
+    route_case(model, x, k)
+    route_case(model, x, k, renorm=True)
+    valid = (torch.rand(T, generator=g, device="cuda") < 0.5).to(torch.uint8)
+    x[valid == 0] = float("nan")
+    route_case(model, x, k, valid=valid)
+    route_case(model, x, k, valid=torch.zeros_like(valid))
+    route_case(model, padded(x, 5, float("nan")), k, valid=valid * 3)
+
+
+def test_route_all_to_one_expert(model):
+    x = torch.full((5000, 64), -1.0, device="cuda")
+    x[:, 63], x[:, 0] = 5.0, 4.0
+    route_case(model, x, 2)
+
+
+def test_route_without_tokens(model):
+    out = route_buffers(0, 9, 2)
+    model.op_route(fb.make_route(torch.zeros(0, 9, device="cuda"), *out))
+    assert torch.equal(out[4].cpu(), torch.zeros(10, dtype=torch.int32))
+
+
+# ---- products grouped by expert -------------------------------------------------------
+
+def act64(v, act, n):
+    if act in ("gelu", "geglu"):
+        f = lambda x: 0.5 * x * (1 + torch.tanh(math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3)))  # noqa: E731
+    else:
+        f = lambda x: x * torch.sigmoid(x)  # noqa: E731
+    if act == "none":
+        return v
+    return f(v) if act == "gelu" else f(v[:, :n]) * v[:, n:]
+
+
+def experts_case(model, sizes, n, k, act="none", gather=True, out_t=BF, bias=True, pad=0, seed=0,
+                 spare=0, tail=0):
+    """sizes: rows of each expert; spare: rows of out that no expert has; tail: elements
+    between the rows."""
+    g = gen(seed + 17 * n + k)
+    E, S = len(sizes), sum(sizes)
+    nw = 2 * n if act in ("swiglu", "geglu") else n
+    T = max(1, S // 2 + 1) if gather else S + spare
+    a = padded(torch.randn(max(T, 1), k, generator=g, device="cuda").to(BF), pad)
+    w = torch.empty(E, nw, k, dtype=BF, device="cuda").normal_(0, k ** -0.5, generator=g)
+    b = 0.3 * torch.randn(E, nw, generator=g, device="cuda") if bias else None
+    off = torch.tensor([0] + list(np.cumsum(sizes)), dtype=torch.int32, device="cuda")
+    idx = None
+    if gather:
+        idx = torch.full((S + spare,), -9, dtype=torch.int32, device="cuda")
+        idx[:S] = torch.randint(0, T, (S,), generator=g, device="cuda").int()
+    out = padded(torch.full((S + spare, n), 3.0, device="cuda").to(out_t), tail)
+    args = fb.make_experts(a, w, off, out, index=idx, bias=b, act=act)
+    model.op_expert_gemm(args)
+    torch.cuda.synchronize()
+    first = out.clone()
+    r0 = 0
+    for e, r in enumerate(sizes):
+        if r:
+            x = (a[idx[r0:r0 + r].long()] if gather else a[r0:r0 + r]).double()
+            v = x @ w[e].double().T
+            if bias:
+                v = v + b[e].double()
+            want = act64(v, act, n)
+            tol = 4 * -(-k // 64) * 1.2e-7 * v.abs().max() * torch.ones_like(want)
+            if act != "none":
+                tol = tol * 1.2
+                if out_t == BF:
+                    tol = tol + 2.0 ** -10.9 * 0.5 * v[:, :n].abs()
+                tol = tol + 6e-7 * v[:, :n].abs()
+            if nw > n:
+                tol = tol * v[:, n:].abs() + 1.2 * v[:, :n].abs() * 4 * -(-k // 64) * 1.2e-7 * v.abs().max()
+            tol = tol + 3e-7 * want.abs()
+            check(out[r0:r0 + r], want, tol, out_t)
+        r0 += r
+    assert torch.all(out[S:] == 3.0)
+    if tail:
+        base = out.as_strided((S + spare, n + tail), (n + tail, 1))
+        assert torch.all(base[:, n:] == 7.0)
+    model.op_expert_gemm(args)  # the same bits every time
+    torch.cuda.synchronize()
+    assert torch.equal(out, first)
+
+
+ACTS = ["none", "gelu", "swiglu", "geglu"]
+
+
+@pytest.mark.parametrize("sizes", [
+    [1], [0, 1], [2, 0, 0, 3], [8, 8], [1, 1, 1, 1, 0, 1], [15, 17], [16, 33, 1], [40] * 3,
+    [130, 0, 257, 5], [600], [300, 17, 0, 0, 255, 256],
+])
+@pytest.mark.parametrize("act", ACTS)
+def test_experts_sizes(model, sizes, act):
+    experts_case(model, sizes, 256, 128, act=act, seed=len(sizes))
+
+
+@pytest.mark.parametrize("n,k", [(16, 8), (48, 40), (64, 64), (112, 72), (144, 1000), (256, 1536),
+                                 (272, 136), (1000 // 16 * 16, 1032), (1536, 4096)])
+@pytest.mark.parametrize("sizes", [[3, 0, 2], [70, 5, 141]])
+@pytest.mark.parametrize("act", ["none", "geglu"])
+@pytest.mark.parametrize("out_t", [BF, F32])
+def test_experts_widths(model, n, k, sizes, act, out_t):
+    experts_case(model, sizes, n, k, act=act, out_t=out_t, seed=1)
+
+
+@pytest.mark.parametrize("n", [8, 24, 200, 1000])
+def test_experts_n_multiple_of_8(model, n):
+    experts_case(model, [20, 0, 3], n, 96, seed=2)
+    experts_case(model, [20, 0, 3], n, 96, act="gelu", gather=False, out_t=F32, seed=2)
+
+
+@pytest.mark.parametrize("out_t", [BF, F32])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("gather", [True, False])
+def test_experts_types_strides_and_spare_rows(model, act, gather, out_t):
+    experts_case(model, [5, 0, 90, 260], 160, 200, act=act, gather=gather, out_t=out_t, pad=8,
+                 spare=40, tail=16, seed=3)
+    experts_case(model, [1, 2], 160, 200, act=act, gather=gather, out_t=out_t, pad=8, spare=4,
+                 tail=16, bias=False, seed=4)
+    experts_case(model, [0, 0], 160, 200, act=act, gather=gather, out_t=out_t, spare=4, seed=4)
+
+
+@pytest.mark.parametrize("sizes,n,k,act", [
+    ([390] * 8, 8960, 1536, "gelu"),
+    ([390] * 8, 1536, 8960, "none"),
+    ([0, 4000, 3, 700], 2048, 1536, "swiglu"),
+    (list(range(64)), 1024, 1536, "swiglu"),
+    ([(i * 37) % 11 for i in range(512)], 256, 512, "none"),
+    ([2] * 4, 4096, 1536, "swiglu"),
+    ([1, 1], 1536, 8960, "none"),
+    ([13], 1536, 8960, "none"),
+])
+def test_experts_at_size(model, sizes, n, k, act):
+    experts_case(model, sizes, n, k, act=act, gather=act != "none", seed=9)
+
+
+@pytest.mark.parametrize("k", [4096, 8960])
+@pytest.mark.parametrize("sizes", [[4, 1], [200, 31]])
+def test_experts_long_sums_fp32(model, k, sizes):
+    """A long K in fp32: the error is that of sums no longer than 80 K blocks."""
+    a = torch.randn(sum(sizes), k, generator=gen(k), device="cuda").to(BF)
+    w = torch.empty(2, 512, k, dtype=BF, device="cuda").normal_(0, k ** -0.5, generator=gen(k + 1))
+    off = torch.tensor([0, sizes[0], sum(sizes)], dtype=torch.int32, device="cuda")
+    out = torch.zeros(sum(sizes), 512, device="cuda")
+    model.op_expert_gemm(fb.make_experts(a, w, off, out))
+    want = torch.cat([a[:sizes[0]].double() @ w[0].double().T, a[sizes[0]:].double() @ w[1].double().T])
+    assert ((out.double() - want).norm() / want.norm()).item() <= 80 * 1.2e-7
+
+
+def test_experts_infinities_and_nan_stay_in_their_rows(model):
+    a = torch.randn(40, 128, device="cuda").to(BF)
+    a[3, 5], a[17, 0] = float("nan"), float("inf")
+    w = torch.randn(2, 256, 128, device="cuda").to(BF)
+    off = torch.tensor([0, 18, 40], dtype=torch.int32, device="cuda")
+    out = torch.zeros(40, 256, dtype=BF, device="cuda")
+    model.op_expert_gemm(fb.make_experts(a, w, off, out))
+    fine = torch.isfinite(out.float()).all(1)
+    assert not fine[3] and not fine[17] and fine.sum() == 38
+
+
+@pytest.mark.parametrize("offsets", [[1, 5, 9], [0, 9, 5], [0, 5, 12], [0, -3, 9], [0, 1 << 30, 9]])
+@pytest.mark.parametrize("rows", [10, 200])
+def test_experts_bad_offsets(model, offsets, rows):
+    scale = rows // 10
+    a, w = torch.randn(rows, 64, device="cuda").to(BF), torch.randn(2, 64, 64, device="cuda").to(BF)
+    out = torch.zeros(rows, 64, dtype=BF, device="cuda")
+    off = torch.tensor([min(o * scale, 1 << 30) for o in offsets], dtype=torch.int32, device="cuda")
+    with pytest.raises(fb.FlashBonError) as e:
+        model.op_expert_gemm(fb.make_experts(a, w, off, out))
+    assert e.value.status == fb.FB_EINVAL
+    off.copy_(torch.tensor([0, 5, 9]) * scale)
+    model.op_expert_gemm(fb.make_experts(a, w, off, out))
+
+
+@pytest.mark.parametrize("rows", [4, 100])
+@pytest.mark.parametrize("bad", [-1, 50, 1 << 30])
+def test_experts_bad_index(model, rows, bad):
+    a, w = torch.randn(50, 64, device="cuda").to(BF), torch.randn(2, 64, 64, device="cuda").to(BF)
+    out = torch.zeros(rows, 64, dtype=BF, device="cuda")
+    off = torch.tensor([0, 2, rows], dtype=torch.int32, device="cuda")
+    idx = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    idx[rows - 1] = bad
+    with pytest.raises(fb.FlashBonError) as e:
+        model.op_expert_gemm(fb.make_experts(a, w, off, out, index=idx))
+    assert e.value.status == fb.FB_EINVAL
+    idx[rows - 1] = 49
+    model.op_expert_gemm(fb.make_experts(a, w, off, out, index=idx))
+
+
+def test_stream_budget_repeat_and_counters(model):
+    """On a caller's stream and a few SMs, launched several times back to back."""
+    st = torch.cuda.Stream()
+    before = model.stats()
+    try:
+        model.set_stream(st)
+        model.set_sm_budget(10)
+        fb.fb_set_op_repeat(model.handle, 3)
+        with torch.cuda.stream(st):
+            experts_case(model, [70, 3, 400], 512, 256, act="swiglu", seed=30)
+            sandwich_case(model, 500, 1536, parts=2, seed=30)
+            route_case(model, torch.randn(700, 32, device="cuda"), 4)
+    finally:
+        fb.fb_set_op_repeat(model.handle, 1)
+        model.set_sm_budget(0)
+        model.set_stream(None)
+    after = model.stats()
+    n = {k: after[k]["launches"] - before[k]["launches"] for k in ("sandwich_norm", "route", "expert_gemm")}
+    assert n == {"sandwich_norm": 3, "route": 6, "expert_gemm": 6}
+
+
+# ---- all of it ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("T,D,H,E,k,act,pad_to", [
+    (1, 256, 512, 8, 2, "gelu", 8), (77, 256, 128, 4, 1, "swiglu", 128),
+    (500, 1536, 1024, 16, 4, "swiglu", 128), (301, 144, 80, 5, 3, "geglu", 8),
+])
+def test_moe_forward(model, T, D, H, E, k, act, pad_to):
+    """The feed-forward in one call against float64 on the router's own choice."""
+    g = gen(T)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    nw = H if act == "gelu" else 2 * H
+    rows = -(-E // pad_to) * pad_to
+    router = (randn(rows, D) * D ** -0.5).to(BF)
+    router[E:] = float("nan")  # ignored
+    w1, w2 = (randn(E, nw, D) * D ** -0.5).to(BF), (randn(E, D, H) * H ** -0.5).to(BF)
+    b1, b2 = 0.1 * randn(E, nw), 0.1 * randn(E, D)
+    a, h = randn(T, D).to(BF), randn(T, D)
+    gate, mul, add = randn(1, D), 0.3 * randn(1, D), 0.3 * randn(1, D)
+    valid = torch.ones(T, dtype=torch.uint8, device="cuda")
+    valid[T // 2 + 1:: 7] = 0
+    moe = fb.make_moe(router, w1, w2, k, b1=b1, b2=b2, act=act, renorm=True)
+    h_out, a_out = torch.zeros_like(h), torch.zeros_like(a)
+    s = fb.make_sandwich(h, post="rms", gate=gate, resid_scale=0.875, h_out=h_out, pre="layer",
+                         mul=mul, add=add, a=a_out)
+    model.moe_forward(moe, a, s, valid=valid)
+
+    logits = torch.zeros(T, rows, device="cuda")
+    fb.fb_op_gemm(model.handle, T, rows, D, a, router, None, 2, logits)
+    out = route_buffers(T, E, k)
+    model.op_route(fb.make_route(logits[:, :E], *out, valid=valid, renorm=True))
+    expert, weight = out[0].long(), out[1].double()
+    y = torch.zeros(T, D, dtype=torch.float64, device="cuda")
+    for e in range(E):
+        t, j = (expert == e).nonzero(as_tuple=True)
+        x = act64(a[t].double() @ w1[e].double().T + b1[e].double(), act, H)
+        y[t] += weight[t, j, None] * (x @ w2[e].double().T + b2[e].double())
+    u = norm64(y, y, "rms", 1e-6)[0]
+    want = 0.875 * h.double() + gate.double() * u
+    want_a = norm64(want, want, "layer", 1e-6)[0] * (1 + mul.double()) + add.double()
+    # two bf16 roundings on the way (hidden rows, expert rows), each 2^-9 at most of what
+    # the norm scales to one, random over a sum: 2^-9 sqrt(2) of the rms, five times that
+    # at the largest of all elements
+    assert ((h_out.double() - want) / gate.abs().clamp(min=1e-3)).abs().max().item() <= 5 * 2 ** -8.5 * max(1.0, u.abs().max().item())
+    err = (h_out.double() - want).norm() / (gate.double() * u).norm()
+    assert err.item() <= 2 ** -8.5
+    assert ((a_out.double() - want_a).norm() / want_a.norm()).item() <= 2 ** -7.5
+
+
+def test_moe_forward_rejects(model):
+    w1, w2 = torch.zeros(4, 64, 32, dtype=BF, device="cuda"), torch.zeros(4, 32, 64, dtype=BF, device="cuda")
+    moe = fb.make_moe(torch.zeros(8, 32, dtype=BF, device="cuda"), w1, w2, 2)
+    h, a = torch.zeros(3, 32, device="cuda"), torch.zeros(3, 32, dtype=BF, device="cuda")
+    with pytest.raises(fb.FlashBonError):  # y belongs to the call
+        model.moe_forward(moe, a, fb.make_sandwich(h, y=a, h_out=h))
+    with pytest.raises(fb.FlashBonError):  # more experts a token than there are
+        model.moe_forward(fb.make_moe(torch.zeros(8, 32, dtype=BF, device="cuda"), w1, w2, 5), a,
+                          fb.make_sandwich(h, h_out=h))
+    with pytest.raises(fb.FlashBonError):  # fewer router rows than experts
+        model.moe_forward(fb.make_moe(torch.zeros(0, 32, dtype=BF, device="cuda"), w1, w2, 2), a,
+                          fb.make_sandwich(h, h_out=h))
+    with pytest.raises(ValueError):
+        model.moe_forward(moe, a[:2].contiguous(), fb.make_sandwich(h, h_out=h))
