@@ -1923,6 +1923,7 @@ fb_status fb_set_device_wait_limit(unsigned long long ns) {
   if (ns == 0) ns = FB_WAIT_LIMIT_NS;
   CK(gemm_tc_set_wait_limit(ns));
   CK(attention_tc_set_wait_limit(ns));
+  CK(expert_gemm_set_wait_limit(ns));
   return FB_OK;
 }
 

@@ -3,112 +3,579 @@
 // with act GELU (tanh form) or, over W_e's 2 n rows (gate rows, then up rows), SiLU or GELU of
 // the first n results times the other n. The sizes of the groups are read on the device.
 //
-// 64 x 64 tiles on the CUDA cores; a row tile belongs to one expert.
+// tcgen05 kernel, a cluster of two CTAs per tile of 256 weight rows x w tokens of one expert
+// (cta_group::2): the weight rows are the MMA's M side (128 per CTA, one per TMEM lane), the
+// tokens its N side, any multiple of 16 up to 256, so that ragged groups cost at most 15 rows
+// of padding each. Every CTA reads the offsets, picks the widest tile T that the launch uses
+// (choose_width) and cuts each group into equal tiles no wider than that; clusters take the
+// tiles in turn, an expert's weight rows fastest, which keeps its weights in L2 while its
+// tokens pass.
+//  * warp 0 loads weights, one TMA box of 128 rows x 64 k. Gated weights come as 16 gate rows
+//    and 16 up rows by turns (a 5-dimensional map over the two halves), so that the two values
+//    an output needs lie 16 lanes apart in one warp, and the weights stay as they are.
+//  * warps 10 and 11 load token rows, a K block each by turns: boxes of 64 and 8 consecutive
+//    rows, or with an index four rows of anywhere at a time (tile::gather4).
+//  * warp 1 issues the MMAs, warps 2-9 of both CTAs run the epilogue: bias and activation on
+//    TMEM columns, results through a shared-memory tile and TMA boxes of 16 tokens; the last,
+//    partly filled box of a group leaves by plain stores, since the rows behind it are the next
+//    expert's.
+// Sums are fp32 in TMEM. For fp32 results a K past 80 blocks of 64 is summed in parts with
+// accumulators of their own (the tensor core's sums lose about 7e-8 per block).
+// Every wait is bounded (mbar_wait): a role that gives up records it and the kernel ends.
+#include <cudaTypedefs.h>
+
+#include <atomic>
+
 #include "kernels.h"
 
 namespace {
 
-constexpr int TR = 64, TC = 64, TK = 16, THREADS = 256;
+constexpr int BK = 64;                  // 64 bf16 = 128 bytes: one swizzle row
+constexpr int W_ROWS = 128;             // weight rows of a CTA
+constexpr int W_BYTES = W_ROWS * BK * 2;
+constexpr int TMEM_COLS = 512;
+constexpr int MAX_STAGES = 8, MAX_ACCS = 8;
+constexpr int THREADS = 384;            // W loader, MMA, 8 epilogue warps, 2 token loaders
+constexpr int MAX_T = 256, T_STEP = 16, WIDTHS = MAX_T / T_STEP;
+constexpr int MAX_E = FB_ROUTE_MAX_EXPERTS;
+constexpr int SMEM_BYTES = 229888;      // (room for a normalisation block beside it, as the GEMM's)
+constexpr int EPI_TILE = 2048;          // an epilogue warp's tile: CHUNK tokens x 32 rows
+constexpr int EPI_BYTES = 8 * 2 * EPI_TILE;
+constexpr int TABLE_BYTES = (2 * (MAX_E + 8) * 4 + 127) / 128 * 128;
+constexpr int BAR_BYTES = 512;
+constexpr int RING_BYTES = SMEM_BYTES - BAR_BYTES - EPI_BYTES - TABLE_BYTES;
+static_assert(RING_BYTES % 128 == 0, "TMA tiles lie on 128-byte boundaries");
+constexpr int PART_BLOCKS = 80;         // K blocks of one accumulator, for fp32 results
 
-__device__ __forceinline__ float act_value(int act, float x, float up) {
-  switch (act) {
-    case FB_ACT_GELU:
-    case FB_ACT_GEGLU: {
-      const float g = 0.5f * x * (1.f + tanhf(0.7978845608028654f * (x + 0.044715f * x * x * x)));
-      return act == FB_ACT_GELU ? g : g * up;
-    }
-    case FB_ACT_SWIGLU: return x / (1.f + expf(-x)) * up;
-  }
-  return x;
+__host__ __device__ __forceinline__ int acc_cols_of(int T) { return (T + 31) / 32 * 32; }
+
+// ---- activations ------------------------------------------------------------------------
+// EXACT: for fp32 results; else the hardware tanh (2^-10.9 of it), within bf16's rounding.
+template <bool EXACT>
+__device__ __forceinline__ float gelu_f(float x) {
+  if (!EXACT) return gelu_tanh_f(x);
+  return 0.5f * x * (1.f + tanhf(0.7978845608028654f * (x + 0.044715f * x * x * x)));
+}
+template <bool EXACT>
+__device__ __forceinline__ float silu_of(float x) {
+  if (EXACT) return x / (1.f + expf(-x));
+  const float h = 0.5f * x;  // x / (1 + e^-x) = x / 2 (1 + tanh(x / 2))
+  return fmaf(h, tanh_approx(h), h);
 }
 
-__global__ void __launch_bounds__(THREADS) expert_gemm_kernel(const ExpertArgs g, int* err) {
-  griddep_wait();
-  griddep_launch();
-  __shared__ float xs[TK][TR + 1], ws[TK][TC + 1], us[TK][TC + 1];
-  __shared__ int s_e, s_r0, s_r1;
-  __shared__ int src[TR];
-  const bool gated = g.act >= FB_ACT_SWIGLU;
-  if (threadIdx.x == 0) {
-    s_e = -1;
-    int tile = 0, prev = 0;
-    for (int e = 0; e < g.experts; ++e) {
-      const int r0 = g.offsets[e], r1 = g.offsets[e + 1];
-      if (r0 != prev || r1 < r0 || r1 > g.max_rows) {
-        fb_report(err, FB_DEVERR_BAD_INDEX);
-        s_e = -1;
+// ---- TMA --------------------------------------------------------------------------------
+__device__ __forceinline__ void tma_load_3d_cg2(uint32_t dst, const CUtensorMap* map, uint32_t bar,
+                                                int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_5d_cg2(uint32_t dst, const CUtensorMap* map, uint32_t bar,
+                                                int x, int d1, int d2, int d3, int d4) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(d1), "r"(d2), "r"(d3), "r"(d4), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_rows_cg2(uint32_t dst, const CUtensorMap* map,
+                                                  uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+// four rows of anywhere (the map's box is one row)
+__device__ __forceinline__ void tma_gather4_cg2(uint32_t dst, const CUtensorMap* map, uint32_t bar,
+                                                int x, int r0, int r1, int r2, int r3) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4.mbarrier::"
+      "complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar)
+      : "memory");
+}
+
+// ---- tiles ------------------------------------------------------------------------------
+struct Tile {
+  int e, f, r0, w, nv;  // expert, weight-row tile, first row, width, rows of it that exist
+};
+// The tiles of this cluster, one after the other. off: the group offsets; first: the token
+// tiles before each group's.
+struct TileIter {
+  const int *off, *first;
+  int t, step, n_ft, n_tiles, E, e;
+  __device__ TileIter(const int* off_, const int* first_, int c, int G, int n_ft_, int E_)
+      : off(off_), first(first_), t(c), step(G), n_ft(n_ft_), n_tiles(first_[E_] * n_ft_), E(E_),
+        e(0) {}
+  // (the whole warp, converged)
+  __device__ bool next(Tile& k) {
+    if (t >= n_tiles) return false;
+    const int tt = t / n_ft, lane = threadIdx.x % 32;
+    k.f = t - tt * n_ft;
+    t += step;
+    while (true) {  // the group that holds token tile tt: the first whose end lies behind it
+      const unsigned m = __ballot_sync(0xffffffffu, e + lane < E && first[e + lane + 1] > tt);
+      if (m) {
+        e += __ffs(m) - 1;
         break;
       }
-      prev = r1;
-      const int n = (r1 - r0 + TR - 1) / TR;
-      if ((int)blockIdx.y >= tile && (int)blockIdx.y < tile + n) {
-        s_e = e;
-        s_r0 = r0 + ((int)blockIdx.y - tile) * TR;
-        s_r1 = min(s_r0 + TR, r1);
-      }
-      tile += n;
+      e += 32;
     }
+    const int r = off[e + 1] - off[e], nt = first[e + 1] - first[e];
+    k.e = e;
+    k.w = ((r + nt - 1) / nt + T_STEP - 1) / T_STEP * T_STEP;
+    k.r0 = off[e] + (tt - first[e]) * k.w;
+    const int left = off[e + 1] - k.r0;
+    k.nv = left < k.w ? left : k.w;
+    return true;
+  }
+};
+
+template <bool GATED, bool F32>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+    expert_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
+                     const __grid_constant__ CUtensorMap tmA8, const __grid_constant__ CUtensorMap tmO,
+                     const ExpertArgs g, int* err) {
+  extern __shared__ __align__(1024) uint8_t smem[];  // (operand tiles need the alignment)
+  if ((smem_u32(smem) & 1023u) != 0) {
+    if (threadIdx.x == 0) fb_report(err, FB_DEVERR_BAD_ARG);
+    return;
+  }
+  uint8_t* epi_smem = smem + RING_BYTES;
+  int* off = reinterpret_cast<int*>(epi_smem + EPI_BYTES);
+  int* first = off + MAX_E + 8;
+  uint64_t* full = reinterpret_cast<uint64_t*>(epi_smem + EPI_BYTES + TABLE_BYTES);
+  uint64_t* empty = full + MAX_STAGES;
+  uint64_t* tmem_full = empty + MAX_STAGES;
+  uint64_t* tmem_empty = tmem_full + MAX_ACCS;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(tmem_empty + MAX_ACCS);
+  uint32_t* gave_up = tmem_holder + 1;  // a role of this CTA gave up a wait
+  int* bad = reinterpret_cast<int*>(tmem_holder + 2);
+  int* width = bad + 1;
+  unsigned* cost = reinterpret_cast<unsigned*>(width + 1);  // of each width, and its token tiles
+  unsigned* count = cost + WIDTHS;
+
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t rank = cluster_ctarank();
+  const int cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+  const int nw = GATED ? 2 * g.n : g.n, n_ft = (nw + 2 * W_ROWS - 1) / (2 * W_ROWS);
+  const int nk = (g.k + BK - 1) / BK, E = g.experts;
+  const int parts = F32 ? (nk + PART_BLOCKS - 1) / PART_BLOCKS < MAX_ACCS
+                              ? (nk + PART_BLOCKS - 1) / PART_BLOCKS : MAX_ACCS
+                        : 1;
+  bool failed = false;
+
+  if (threadIdx.x == 0) {
+    *gave_up = 0;
+    *bad = 0;
+    for (int s = 0; s < MAX_STAGES; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int a = 0; a < MAX_ACCS; ++a) {
+      mbar_init(&tmem_full[a], 1);
+      mbar_init(&tmem_empty[a], 16);  // 8 epilogue warps x 2 CTAs
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tma_prefetch_desc(&tmW);
+    tma_prefetch_desc(&tmA);
+    if (!g.index) tma_prefetch_desc(&tmA8);
+    tma_prefetch_desc(&tmO);
+  }
+  if (threadIdx.x >= 64 && threadIdx.x < 64 + 2 * WIDTHS) cost[threadIdx.x - 64] = 0;
+  if (warp == 1) tmem_alloc_cg2(tmem_holder, TMEM_COLS);
+  griddep_wait();
+  griddep_launch();
+  // ---- the groups and the tile width ----
+  __syncthreads();
+  for (int i = threadIdx.x; i <= E; i += THREADS) {
+    const int o = g.offsets[i], p = i ? g.offsets[i - 1] : 0;
+    off[i] = o;
+    if (o < p || o > g.max_rows || (i == 0 && o != 0)) *bad = 1;
   }
   __syncthreads();
-  if (s_e < 0) return;
-  const int e = s_e, r0 = s_r0, nr = s_r1 - s_r0, c0 = blockIdx.x * TC;
-  if (threadIdx.x < TR) {
-    int s = r0 + min((int)threadIdx.x, nr - 1);
-    if (g.index) s = g.index[s];
-    if (s < 0 || s >= g.a_rows) {
-      fb_report(err, FB_DEVERR_BAD_INDEX);
-      s = 0;
-    }
-    src[threadIdx.x] = s;
-  }
-  __syncthreads();
-  const size_t nw = gated ? 2 * (size_t)g.n : g.n;
-  const bf16* W = g.W + (size_t)e * nw * g.k;
-  const int tr = threadIdx.x / 16 * 4, tc = threadIdx.x % 16 * 4;
-  float acc[4][4] = {}, acu[4][4] = {};
-  for (int k0 = 0; k0 < g.k; k0 += TK) {
-    for (int i = threadIdx.x; i < TR * TK; i += THREADS) {
-      const int row = i / TK, k = i % TK;
-      const bool in = k0 + k < g.k;
-      xs[k][row] = in ? __bfloat162float(g.A[(size_t)src[row] * g.lda + k0 + k]) : 0.f;
-      const bool win = in && c0 + row < g.n;
-      ws[k][row] = win ? __bfloat162float(W[(size_t)(c0 + row) * g.k + k0 + k]) : 0.f;
-      if (gated)
-        us[k][row] = win ? __bfloat162float(W[((size_t)g.n + c0 + row) * g.k + k0 + k]) : 0.f;
-    }
+  if (*bad) {  // (every CTA sees the same)
+    if (threadIdx.x == 0) fb_report(err, FB_DEVERR_BAD_INDEX);
+    for (int i = threadIdx.x; i <= E; i += THREADS) off[i] = 0;
     __syncthreads();
-    for (int k = 0; k < TK; ++k)
+  }
+  for (int i = threadIdx.x; i < E * WIDTHS; i += THREADS) {
+    const int e = i / WIDTHS, c = i % WIDTHS, T = T_STEP * (c + 1);
+    const int r = off[e + 1] - off[e];
+    if (r == 0) continue;
+    const int nt = (r + T - 1) / T, w = ((r + nt - 1) / nt + T_STEP - 1) / T_STEP * T_STEP;
+    atomicAdd(&count[c], (unsigned)nt);
+    atomicAdd(&cost[c], (unsigned)(nt * (256 + w > 313 ? 256 + w : 313)));
+  }
+  __syncthreads();
+  if (warp == 0) {
+    // choose_width: the width of the least estimated time in SM clocks (the rule and figures
+    // of the dense GEMM's tiles: 256 + w clocks of operands, or 313 of issue, per K block; in
+    // the fullest cluster each tile but the first takes its mainloop or its epilogue)
+    const int T = T_STEP * (lane + 1);
+    float est = 3e38f;
+    // (the ring holds a tile's K parts, and at least four where there are several)
+    if (lane < WIDTHS && (parts == 1 || acc_cols_of(T) * (parts < 4 ? 4 : parts) <= TMEM_COLS)) {
+      const float n = (float)count[lane] * n_ft, rounds = ceilf(n / n_clusters);
+      const float main = count[lane] ? (float)cost[lane] / count[lane] * nk : 0.f;
+      const float epi = F32 ? 3300.f + 30.f * T : 2900.f + 12.f * T;
+      est = main + (rounds - 1.f) * fmaxf(main, epi) + (F32 ? 28.f : 16.f) * T;
+    }
+    float best = est;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int o = 16; o > 0; o >>= 1) best = fminf(best, __shfl_xor_sync(0xffffffffu, best, o));
+    const int Tb = T_STEP * __ffs(__ballot_sync(0xffffffffu, est == best));
+    int sum = 0;
+    for (int e0 = 0; e0 <= E; e0 += 32) {
+      const int e = e0 + lane;
+      int n = e < E ? (off[e + 1] - off[e] + Tb - 1) / Tb : 0, s = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += v;
+      }
+      if (e <= E) first[e] = sum + s - n;
+      sum += __shfl_sync(0xffffffffu, s, 31);
+    }
+    if (lane == 0) *width = Tb;
+  }
+  tc_fence_before();
+  cluster_sync();  // barriers initialised, TMEM allocated, tables written
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_holder;
+  const int T = *width;
+  const int stage_bytes = W_BYTES + T / 2 * BK * 2;
+  const int stages = RING_BYTES / stage_bytes < MAX_STAGES ? RING_BYTES / stage_bytes : MAX_STAGES;
+  const int acc_cols = acc_cols_of(T);
+  const int n_accs = TMEM_COLS / acc_cols < MAX_ACCS ? TMEM_COLS / acc_cols : MAX_ACCS;
+  TileIter ti(off, first, cluster, n_clusters, n_ft, E);
+  Tile k;
+
+  if (warp == 0) {
+    // ---------------- weights (both CTAs) ----------------
+    int stage = 0;
+    uint32_t phase = 0;
+    while (!failed && ti.next(k)) {
+      const uint32_t bytes = 2 * (W_BYTES + k.w / 2 * BK * 2);
+      for (int kb = 0; kb < nk; ++kb) {
+        if (!mbar_wait_warp(&empty[stage], phase ^ 1u, err)) { failed = true; break; }
+        if (elect_one()) {
+          const uint32_t dst = smem_u32(smem) + stage * stage_bytes;
+          const uint32_t fb = mapa_shared(smem_u32(&full[stage]), 0);
+          if (rank == 0) mbar_expect_tx(&full[stage], bytes);
+          if (GATED)
+            tma_load_5d_cg2(dst, &tmW, fb, kb * BK, 0, 0, (2 * k.f + (int)rank) * 4, k.e);
+          else
+            tma_load_3d_cg2(dst, &tmW, fb, kb * BK, (2 * k.f + (int)rank) * W_ROWS, k.e);
+        }
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp >= 10) {
+    // ---------------- token rows (both CTAs) ----------------
+    int stage = 0;
+    uint32_t phase = 0;
+    bool mine = warp == 10;  // K blocks alternate between the two warps
+    while (!failed && ti.next(k)) {
+      const int half = k.w / 2, a0 = k.r0 + half * (int)rank, end = k.r0 + k.nv;
+      int src[4] = {0, 0, 0, 0};
+      const int n4 = half / 4;
+      if (g.index && lane < n4) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          acc[i][j] += xs[k][tr + i] * ws[k][tc + j];
-          if (gated) acu[i][j] += xs[k][tr + i] * us[k][tc + j];
+          const int row = a0 + 4 * lane + j;
+          src[j] = g.index[row < end ? row : end - 1];
+          if (src[j] < 0 || src[j] >= g.a_rows) {
+            fb_report(err, FB_DEVERR_BAD_INDEX);
+            src[j] = 0;
+          }
         }
-    __syncthreads();
-  }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int c = c0 + tc + j;
-      if (tr + i >= nr || c >= g.n) continue;
-      float v = acc[i][j], u = acu[i][j];
-      if (g.bias) {
-        v += g.bias[e * nw + c];
-        if (gated) u += g.bias[e * nw + g.n + c];
       }
-      v = act_value(g.act, v, u);
-      const size_t o = (size_t)(r0 + tr + i) * g.ldo + c;
-      if (g.out_type == FB_F32)
-        reinterpret_cast<float*>(g.out)[o] = v;
-      else
-        reinterpret_cast<bf16*>(g.out)[o] = __float2bfloat16(v);
+      for (int kb = 0; kb < nk; ++kb, mine = !mine) {
+        if (mine) {
+          if (!mbar_wait_warp(&empty[stage], phase ^ 1u, err)) { failed = true; break; }
+          const uint32_t dst = smem_u32(smem) + stage * stage_bytes + W_BYTES;
+          const uint32_t fb = mapa_shared(smem_u32(&full[stage]), 0);
+          if (g.index) {
+#pragma unroll 4
+            for (int i = 0; i < n4; ++i) {
+              const int r0 = __shfl_sync(0xffffffffu, src[0], i), r1 = __shfl_sync(0xffffffffu, src[1], i);
+              const int r2 = __shfl_sync(0xffffffffu, src[2], i), r3 = __shfl_sync(0xffffffffu, src[3], i);
+              if (elect_one()) tma_gather4_cg2(dst + i * (4 * BK * 2), &tmA, fb, kb * BK, r0, r1, r2, r3);
+            }
+          } else if (elect_one()) {
+            int i = 0;
+            for (; i + 64 <= half; i += 64)
+              tma_load_rows_cg2(dst + i * (BK * 2), &tmA, fb, kb * BK, a0 + i);
+            for (; i < half; i += 8)
+              tma_load_rows_cg2(dst + i * (BK * 2), &tmA8, fb, kb * BK, a0 + i);
+          }
+        }
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+      }
     }
+  } else if (warp == 1) {
+    if (rank == 0) {
+      // ---------------- MMA issuer (even CTA) ----------------
+      const uint32_t ring_lo = desc_lo_k(smem_u32(smem));
+      const int part_len = (nk + parts - 1) / parts;
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      while (!failed && ti.next(k)) {
+        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(k.w >> 3) << 17) |
+                               ((uint32_t)(2 * W_ROWS >> 4) << 24);
+        // the tile's K parts, each in the ring's next accumulator
+        for (int p = 0, kb = 0; !failed && p < parts; ++p) {
+          if (!mbar_wait_warp(&tmem_empty[acc], acc_phase ^ 1u, err)) { failed = true; break; }
+          tc_fence_after();
+          const uint32_t d_tmem = tmem_base + acc * acc_cols;
+          const int start = kb, end = nk - kb < part_len ? nk : kb + part_len;
+          for (; kb < end; ++kb) {
+            if (!mbar_wait_warp(&full[stage], phase, err)) { failed = true; break; }
+            tc_fence_after();
+            const uint32_t wlo = ring_lo + (uint32_t)(stage * (stage_bytes >> 4));
+            const uint32_t alo = wlo + (W_BYTES >> 4);
+            if (elect_one()) {
+#pragma unroll
+              for (int j = 0; j < BK / 16; ++j)
+                tc_mma_cg2_lo(d_tmem, wlo + 2 * j, alo + 2 * j, DESC_HI, idesc,
+                              (kb > start || j > 0) ? 1u : 0u);
+              tc_commit_mc(&empty[stage], 0x3);
+              if (kb + 1 == end) tc_commit_mc(&tmem_full[acc], 0x3);
+            }
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
+          }
+          if (++acc == n_accs) { acc = 0; acc_phase ^= 1u; }
+        }
+      }
+    }
+  } else {
+    // ---------------- epilogue (warps 2..9 of both CTAs) ----------------
+    // warp: weight rows quarter * 32 .. + 31 of this CTA's 128 (its TMEM lanes), every other
+    // CH-token chunk of the tile; FW output features, a lane's own or (gated) a lane pair's
+    constexpr int CH = F32 ? 16 : 32, FW = GATED ? 16 : 32, ES = F32 ? 4 : 2;
+    const int quarter = warp & 3, half = (warp - 2) >> 2, we = warp - 2;
+    const uint32_t te_remote = mapa_shared(smem_u32(&tmem_empty[0]), 0);
+    uint8_t* tiles = epi_smem + we * 2 * EPI_TILE;
+    int acc = 0, buf = 0;
+    uint32_t acc_phase = 0;
+    while (!failed && ti.next(k)) {
+      // the last part's accumulator is complete after all others of the tile
+      int last = acc + parts - 1;
+      uint32_t last_phase = acc_phase;
+      if (last >= n_accs) { last -= n_accs; last_phase ^= 1u; }
+      const int wrow = (2 * k.f + (int)rank) * W_ROWS + quarter * 32;  // of the interleaved rows
+      const int f0 = GATED ? wrow / 2 : wrow;
+      const int feature = f0 + (GATED ? lane & 15 : lane);
+      float bias = 0.f;
+      if (g.bias && feature < g.n)
+        bias = __ldg(g.bias + (size_t)k.e * nw + feature + (GATED && lane >= 16 ? g.n : 0));
+      const bool ok = mbar_wait(&tmem_full[last], last_phase, err);
+      if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+      tc_fence_after();
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll 1
+      for (int t0 = half * CH; t0 < k.nv && f0 < g.n; t0 += 2 * CH) {
+        float v[CH];
+        for (int p = 0; p < parts; ++p) {
+          uint32_t r[CH];
+          const uint32_t a = taddr + (acc + p < n_accs ? acc + p : acc + p - n_accs) * acc_cols + t0;
+          if (CH == 32) {
+            tmem_ld32(a, r);
+            tmem_ld_wait();
+            reg_fence32(r);
+          } else {
+            tmem_ld16(a, r);
+            tmem_ld_wait();
+            reg_fence16(r);
+          }
+#pragma unroll
+          for (int j = 0; j < CH; ++j)
+            v[j] = p == 0 ? __uint_as_float(r[j]) : v[j] + __uint_as_float(r[j]);
+        }
+        uint8_t* tile = tiles + buf * EPI_TILE;
+        buf ^= 1;
+        if (elect_one()) bulk_wait_read<1>();  // the store from this tile two chunks ago
+        __syncwarp();
+        if (GATED) {
+          // tokens j and j + 1: lanes 0-15 form j's outputs, lanes 16-31 j + 1's
+#pragma unroll
+          for (int j = 0; j < CH; j += 2) {
+            const float x0 = v[j] + bias, x1 = v[j + 1] + bias;
+            const float got = __shfl_xor_sync(0xffffffffu, lane < 16 ? x1 : x0, 16);
+            const float gate = lane < 16 ? x0 : got, up = lane < 16 ? got : x1;
+            const float y = (g.act == FB_ACT_SWIGLU ? silu_of<F32>(gate) : gelu_f<F32>(gate)) * up;
+            if (F32)
+              reinterpret_cast<float*>(tile)[j * 16 + lane] = y;
+            else
+              reinterpret_cast<bf16*>(tile)[j * 16 + lane] = __float2bfloat16(y);
+          }
+        } else if (F32) {
+#pragma unroll
+          for (int j = 0; j < CH; ++j) {
+            const float x = v[j] + bias;
+            reinterpret_cast<float*>(tile)[j * 32 + lane] = g.act == FB_ACT_GELU ? gelu_f<true>(x) : x;
+          }
+        } else {
+          // two tokens' values of each lane's feature as one 4-byte store per lane: lanes
+          // exchange with their neighbour, even lanes then hold two features of token j, odd
+          // lanes of token j + 1
+          uint32_t* tw = reinterpret_cast<uint32_t*>(tile) + (lane & 1) * 16 + (lane >> 1);
+#pragma unroll
+          for (int j = 0; j < CH; j += 2) {
+            float y0 = v[j] + bias, y1 = v[j + 1] + bias;
+            if (g.act == FB_ACT_GELU) gelu_tanh_f2(y0, y1);
+            const float got = __shfl_xor_sync(0xffffffffu, (lane & 1) ? y0 : y1, 1);
+            tw[j * 16] = (lane & 1) ? pack_bf16x2(got, y1) : pack_bf16x2(y0, got);
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        const int n = k.nv - t0 < CH ? k.nv - t0 : CH;  // tokens of the chunk that exist
+        if (elect_one()) {
+#pragma unroll
+          for (int b = 0; b < CH; b += 16)
+            if (b + 16 <= n) tma_store_2d(&tmO, smem_u32(tile) + b * FW * ES, f0, k.r0 + t0 + b);
+          bulk_commit();
+        }
+        if (n % 16) {  // 16 bytes at a time: n is a multiple of 8 features
+          constexpr int PIECES = FW * ES / 16, PE = 16 / ES;
+          const int b = n / 16 * 16;
+          for (int i = lane; i < (n - b) * PIECES; i += 32) {
+            const int tok = b + i / PIECES, c = i % PIECES;
+            if (f0 + c * PE < g.n)
+              *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(g.out) +
+                                        ((size_t)(k.r0 + t0 + tok) * g.ldo + f0 + c * PE) * ES) =
+                  *reinterpret_cast<const uint4*>(tile + tok * FW * ES + c * 16);
+          }
+          __syncwarp();
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      for (int p = 0; p < parts; ++p) {
+        if (lane == 0) mbar_arrive_cluster(te_remote + acc * (uint32_t)sizeof(uint64_t));
+        if (++acc == n_accs) { acc = 0; acc_phase ^= 1u; }
+      }
+    }
+    // own TMA stores complete (one lane issued them all)
+    if (elect_one()) bulk_wait<0>();
+  }
+
+  if (failed) *gave_up = 1;
+  tc_fence_before();
+  cluster_sync();
+  if (*gave_up != 0) {
+    // After a timeout, give TMA loads that may still be in flight time to land before the
+    // shared memory they target is released (they complete within microseconds).
+    const uint64_t t0 = fb_globaltimer();
+    while (fb_globaltimer() - t0 < 100000ull) __nanosleep(1000);
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_cg2(tmem_base, TMEM_COLS);
+  }
+}
+
+// ---- host -------------------------------------------------------------------------------
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
+  static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+    cudaDriverEntryPointQueryResult q;
+    void* p = nullptr;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                         &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    cudaGetLastError();
+    return static_cast<PFN_cuTensorMapEncodeTiled_v12000>(nullptr);
+  }();
+  return fn;
+}
+
+template <int R>
+bool make_map(CUtensorMap* map, const void* ptr, bool f32, const cuuint64_t (&dims)[R],
+              const cuuint64_t (&stride_elems)[R - 1], const cuuint32_t (&box)[R], bool swizzle) {
+  auto enc = encoder();
+  if (!enc) return false;
+  cuuint64_t strides[R - 1];
+  cuuint32_t estr[R];
+  for (int i = 0; i < R; ++i) {
+    estr[i] = 1;
+    if (i) strides[i - 1] = stride_elems[i - 1] * (f32 ? 4 : 2);
+  }
+  return enc(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, R,
+             const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+             swizzle ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Clusters that the current device can hold at once, asked once per device.
+template <bool GATED, bool F32>
+int resident_clusters(int num_sms) {
+  constexpr int DEVICES = 64;
+  static std::atomic<int> known[DEVICES];  // zero until a launch has asked (any thread)
+  int dev = 0, sms = 0, n = 0;
+  if (cudaGetDevice(&dev) == cudaSuccess && dev < DEVICES) {
+    n = known[dev].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+  }
+  cudaLaunchConfig_t cfg = {};
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) {
+    cfg.gridDim = dim3(sms / 2 * 2, 1, 1);
+    cfg.blockDim = dim3(THREADS, 1, 1);
+    cfg.dynamicSmemBytes = SMEM_BYTES;
+    if (cudaOccupancyMaxActiveClusters(&n, expert_tc_kernel<GATED, F32>, &cfg) == cudaSuccess &&
+        n > 0) {
+      if (dev < DEVICES) known[dev].store(n, std::memory_order_relaxed);
+      return n;
+    }
+  }
+  cudaGetLastError();
+  return num_sms / 2;
+}
+
+template <bool GATED, bool F32>
+cudaError_t launch(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st) {
+  auto kern = expert_tc_kernel<GATED, F32>;
+  cudaError_t e =
+      cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+  if (e != cudaSuccess) return e;
+  typedef cuuint64_t u64;
+  const u64 K = g.k, N = g.n, E = g.experts;
+  CUtensorMap mw, ma, ma8{}, mo;  // ma8: unused with an index
+  const bool w_ok =
+      GATED ? make_map<5>(&mw, g.W, false, {K, 16, 2, N / 16, E}, {K, N * K, 16 * K, 2 * N * K},
+                          {BK, 16, 2, W_ROWS / 32, 1}, true)
+            : make_map<3>(&mw, g.W, false, {K, N, E}, {K, N * K}, {BK, W_ROWS, 1}, true);
+  const u64 rows = g.a_rows, lda = g.lda, orows = g.max_rows, ldo = g.ldo;
+  if (!w_ok ||
+      !make_map<2>(&ma, g.A, false, {K, rows}, {lda}, {BK, g.index ? 1u : 64u}, true) ||
+      (!g.index && !make_map<2>(&ma8, g.A, false, {K, rows}, {lda}, {BK, 8}, true)) ||
+      !make_map<2>(&mo, g.out, F32, {N, orows}, {ldo}, {GATED ? 16u : 32u, 16}, false))
+    return cudaErrorInvalidValue;
+  const int occ = resident_clusters<GATED, F32>(num_sms);
+  const int mc = occ < num_sms / 2 ? occ : num_sms / 2;
+  // no more clusters than there can be tiles: 16 rows at least each but a group's last
+  const int n_ft = ((GATED ? 2 * g.n : g.n) + 2 * W_ROWS - 1) / (2 * W_ROWS);
+  const long long groups = g.experts < g.max_rows ? g.experts : g.max_rows;
+  const long long tiles = (g.max_rows / T_STEP + groups) * n_ft;
+  const int clusters = tiles < mc ? (int)tiles : mc;
+  return launch_k(kern, dim3(2 * clusters), dim3(THREADS), SMEM_BYTES, st, mw, ma, ma8, mo, g, err);
 }
 
 }  // namespace
 
+cudaError_t expert_gemm_set_wait_limit(unsigned long long ns) { return fb_set_wait_limit_tu(ns); }
+
 cudaError_t expert_gemm(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st) {
   if (g.max_rows == 0) return cudaSuccess;
-  const dim3 grid((g.n + TC - 1) / TC, (g.max_rows + TR - 1) / TR + g.experts);
-  return launch_k(expert_gemm_kernel, grid, dim3(THREADS), 0, st, g, err);
+  if (num_sms < 2) return cudaErrorInvalidValue;
+  const bool f32 = g.out_type == FB_F32;
+  if (g.act >= FB_ACT_SWIGLU)
+    return f32 ? launch<true, true>(g, err, num_sms, st) : launch<true, false>(g, err, num_sms, st);
+  return f32 ? launch<false, true>(g, err, num_sms, st) : launch<false, false>(g, err, num_sms, st);
 }

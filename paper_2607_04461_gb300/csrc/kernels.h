@@ -158,6 +158,8 @@ struct ExpertArgs {
   int64_t ldo;
 };
 cudaError_t expert_gemm(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st);
+// Sets the expert_gemm unit's device wait limit on the current device (ns).
+cudaError_t expert_gemm_set_wait_limit(unsigned long long ns);
 
 // ---- measurement probe ----------------------------------------------------------------
 // One CTA per entry of `grid`, each timing (SM clock cycles, cycles[cta]) `reps` tcgen05.mma
