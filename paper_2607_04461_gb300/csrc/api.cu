@@ -205,7 +205,7 @@ struct fb_model {
   // launches; reset after a device error)
   float* attn_ws = nullptr;
   int* attn_flags = nullptr;
-  // scratch of fb_moe_forward, grown on demand
+  // scratch of fb_op_expert_gemm and fb_moe_forward, grown on demand
   uint8_t* moe_ws = nullptr;
   size_t moe_bytes = 0;
   // statistics
@@ -428,18 +428,28 @@ fb_status run_sandwich(fb_model* m, const fb_sandwich& s) {
   return FB_OK;
 }
 
-fb_status run_route(fb_model* m, const fb_route& r) {
-  const double n = (double)r.tokens * r.experts;
+RouteArgs route_args(const fb_route& r) {
   RouteArgs a;
   static_cast<fb_route&>(a) = r;
+  return a;
+}
+// ws: route_ws_bytes
+fb_status run_route(fb_model* m, const fb_route& r, uint8_t* ws) {
+  const double n = (double)r.tokens * r.experts;
+  const RouteArgs a = route_args(r);
   KTimer t(m, FB_K_ROUTE, n * (4 + r.top_k),
-           n * type_bytes(r.logits_type) + 16.0 * r.tokens * r.top_k);
-  CK(route(a, m->st));
+           n * type_bytes(r.logits_type) + 16.0 * r.tokens * r.top_k, route_launches(a));
+  CK(route(a, ws, m->st));
   return FB_OK;
 }
 
-// (the work of max_rows rows that reach every expert)
-fb_status run_experts(fb_model* m, const ExpertArgs& g) {
+// (the work of max_rows rows that reach every expert) ws: expert_gemm_ws_bytes
+fb_status run_experts(fb_model* m, const ExpertArgs& g0, uint8_t* ws) {
+  ExpertArgs g = g0;
+  if (expert_gemm_ws_bytes(g) > 0) {
+    KTimer t(m, FB_K_SMALL, 0, 4.0 * g.max_rows * g.k);
+    CK(expert_copy_rows(&g, reinterpret_cast<bf16*>(ws), m->derr, m->num_sms, m->st));
+  }
   const double nw = g.act >= FB_ACT_SWIGLU ? 2.0 * g.n : g.n;
   KTimer t(m, FB_K_EXPERT, 2.0 * g.max_rows * nw * g.k,
            2.0 * g.experts * nw * g.k + 2.0 * (g.index ? g.a_rows : g.max_rows) * g.k +
@@ -1010,7 +1020,7 @@ fb_status ensure_anchors(fb_model* m, size_t need) {
   return FB_OK;
 }
 
-// The scratch of fb_moe_forward holds at least `need` bytes (growing it waits for its users).
+// The scratch of the mixture-of-experts calls holds at least `need` bytes (growing it waits for its users).
 fb_status ensure_moe(fb_model* m, size_t need) {
   if (need <= m->moe_bytes) return FB_OK;
   fb_stream_op_not_kernel();
@@ -1731,7 +1741,8 @@ fb_status fb_op_route(fb_model* m, const fb_route* r) {
   if (!m || !r) return fail(FB_EINVAL, "null argument");
   CKS(check_route(*r));
   CKS(begin_call(m));
-  for (int i = 0; i < m->op_repeat; ++i) CKS(run_route(m, *r));
+  CKS(ensure_moe(m, route_ws_bytes(route_args(*r))));
+  for (int i = 0; i < m->op_repeat; ++i) CKS(run_route(m, *r, m->moe_ws));
   return end_call(m);
 }
 
@@ -1740,7 +1751,8 @@ fb_status fb_op_expert_gemm(fb_model* m, const fb_experts* g) {
   ExpertArgs a;
   CKS(expert_args(*g, &a));
   CKS(begin_call(m));
-  for (int r = 0; r < m->op_repeat; ++r) CKS(run_experts(m, a));
+  CKS(ensure_moe(m, expert_gemm_ws_bytes(a)));
+  for (int r = 0; r < m->op_repeat; ++r) CKS(run_experts(m, a, m->moe_ws));
   return end_call(m);
 }
 
@@ -1810,6 +1822,7 @@ fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const ui
   CKS(expert_args(down, &gd));
   CKS(check_sandwich(s));
   if (T == 0) return FB_OK;
+  const size_t o_rows = take(expert_gemm_ws_bytes(gu)), o_cnt = take(route_ws_bytes(route_args(r)));
   CKS(begin_call(m));
   CKS(ensure_moe(m, at));
   ws = m->moe_ws;
@@ -1818,9 +1831,9 @@ fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const ui
   CKS(expert_args(down, &gd));
   CKS(run_gemm(m, gemm_args((int)T, moe->router_rows, moe->dim, (const bf16*)a,
                             (const bf16*)moe->router_w, nullptr, EPI_RESID, ws + o_log)));
-  CKS(run_route(m, r));
-  CKS(run_experts(m, gu));
-  CKS(run_experts(m, gd));
+  CKS(run_route(m, r, ws + o_cnt));
+  CKS(run_experts(m, gu, ws + o_rows));
+  CKS(run_experts(m, gd, nullptr));  // (no index, no copy)
   CKS(run_sandwich(m, s));
   return end_call(m);
 }

@@ -143,8 +143,13 @@ cudaError_t f32_to_bf16(const float* x, bf16* y, size_t n, cudaStream_t st);
 // ---- mixture of experts between two norms (flashbon.h has the definitions) -------------
 struct SandwichArgs : fb_sandwich {};
 cudaError_t sandwich_norm(const SandwichArgs& s, int* err, int num_sms, cudaStream_t st);
-struct RouteArgs : fb_route {};
-cudaError_t route(const RouteArgs& r, cudaStream_t st);
+struct RouteArgs : fb_route {
+  bool vec = false;  // rows of logits begin on 16 bytes and hold a multiple of 4 (set by route)
+};
+// ws: route_ws_bytes of scratch
+size_t route_ws_bytes(const RouteArgs& r);
+int route_launches(const RouteArgs& r);
+cudaError_t route(const RouteArgs& r, void* ws, cudaStream_t st);
 struct ExpertArgs {
   int experts, n, k, max_rows, a_rows;
   const bf16* A;
@@ -157,6 +162,10 @@ struct ExpertArgs {
   int out_type;
   int64_t ldo;
 };
+// Bytes of scratch for the rows of A in expert order, where the product is faster on a copy of
+// them (else 0); expert_copy_rows makes that copy and points *g at it.
+size_t expert_gemm_ws_bytes(const ExpertArgs& g);
+cudaError_t expert_copy_rows(ExpertArgs* g, bf16* ws, int* err, int num_sms, cudaStream_t st);
 cudaError_t expert_gemm(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st);
 // Sets the expert_gemm unit's device wait limit on the current device (ns).
 cudaError_t expert_gemm_set_wait_limit(unsigned long long ns);
