@@ -482,6 +482,145 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   }
 }
 
+// ---- few rows ---------------------------------------------------------------------------
+// A handful of rows read every weight of their experts once: what counts is to have all SMs
+// reading at full depth, also where 256-row tiles would be too few (one token's FFN down: 12
+// tiles, 28.9 us; 11.3 here). A block takes 16 weight rows of one expert (gated: 8 gate rows and
+// their up rows), its warps split k, and the weights go straight from memory into the operand
+// registers of mma.sync (m16n8k16: the weights are the M side, eight token rows the N side): the
+// tensor instruction is only there to keep the arithmetic out of the way of the loads. Its k
+// index is a permuted one, the same for both operands: lane (g, t) of a step of 32 holds k
+// 8 t .. 8 t + 7 of weight rows g and g + 8 and of token row g, 16 bytes each.
+constexpr int FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32, FEW_UNROLL = 4;
+
+__device__ __forceinline__ void mma_16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2,
+                                          uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+      "{%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// NT: eight token rows each; a group of more is taken in several passes.
+template <bool GATED, bool F32, int NT>
+__global__ void __launch_bounds__(FEW_THREADS) expert_few_kernel(const ExpertArgs g, int* err) {
+  griddep_wait();
+  griddep_launch();
+  __shared__ float part[FEW_WARPS][16][8 * NT + 1];
+  __shared__ int found[3];  // the block's expert, its rows
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, gr = lane / 4, t = lane % 4;
+  const int blocks_n = GATED ? (g.n + 7) / 8 : (g.n + 15) / 16;
+  // the blockIdx.x / blocks_n-th group that has rows
+  const int want = blockIdx.x / blocks_n;
+  if (warp == 0) {
+    int seen = 0;
+    bool bad = false;
+    if (lane == 0) found[0] = -1;
+    __syncwarp();
+    for (int e0 = 0; e0 < g.experts; e0 += 32) {
+      const int e = e0 + lane;
+      const int a = e < g.experts ? g.offsets[e] : 0, b = e < g.experts ? g.offsets[e + 1] : 0;
+      const unsigned some = __ballot_sync(0xffffffffu, b > a);
+      const int at = seen + __popc(some & ((1u << lane) - 1));
+      if (b > a && at == want) {
+        found[0] = e;
+        found[1] = a;
+        found[2] = b;
+      }
+      seen += __popc(some);
+      bad = bad || b < a || a < 0 || b > g.max_rows || (e == 0 && a != 0);
+    }
+    if (__any_sync(0xffffffffu, bad) && lane == 0) {
+      fb_report(err, FB_DEVERR_BAD_INDEX);
+      found[0] = -1;
+    }
+  }
+  __syncthreads();
+  const int e = found[0], r0 = found[1], r1 = found[2];
+  if (e < 0) return;
+  const int f0 = (blockIdx.x % blocks_n) * (GATED ? 8 : 16);
+  const size_t nw = GATED ? 2 * (size_t)g.n : g.n;
+  // this lane's two weight rows (past the last one: the last one again, not stored)
+  const int fa = min(f0 + gr, g.n - 1), fb = GATED ? g.n + fa : min(f0 + 8 + gr, g.n - 1);
+  const bf16* wa = g.W + ((size_t)e * nw + fa) * g.k + 8 * t;
+  const bf16* wb = g.W + ((size_t)e * nw + fb) * g.k + 8 * t;
+  const int steps = (g.k + 31) / 32;
+  const int s0 = steps * warp / FEW_WARPS, s1 = steps * (warp + 1) / FEW_WARPS;
+  for (int p0 = r0; p0 < r1; p0 += 8 * NT) {
+    const bf16* x[NT];
+    bool have[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int row = p0 + 8 * i + gr;
+      have[i] = row < r1;
+      int src = have[i] ? row : r0;
+      if (g.index) src = g.index[src];
+      if (src < 0 || src >= g.a_rows) {
+        fb_report(err, FB_DEVERR_BAD_INDEX);
+        src = 0;
+      }
+      x[i] = g.A + (size_t)src * g.lda + 8 * t;
+    }
+    float c[NT][4] = {};
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    for (int s = s0; s < s1; s += FEW_UNROLL) {
+      uint4 a[FEW_UNROLL], b[FEW_UNROLL], v[FEW_UNROLL][NT];
+#pragma unroll
+      for (int u = 0; u < FEW_UNROLL; ++u) {
+        const int kk = 32 * (s + u);
+        const bool in = s + u < s1 && kk + 8 * t < g.k;
+        a[u] = in ? __ldg(reinterpret_cast<const uint4*>(wa + kk)) : zero;
+        b[u] = in ? __ldg(reinterpret_cast<const uint4*>(wb + kk)) : zero;
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+          v[u][i] = in && have[i] ? *reinterpret_cast<const uint4*>(x[i] + kk) : zero;
+      }
+#pragma unroll
+      for (int u = 0; u < FEW_UNROLL; ++u)
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          mma_16816(c[i], a[u].x, b[u].x, a[u].y, b[u].y, v[u][i].x, v[u][i].y);
+          mma_16816(c[i], a[u].z, b[u].z, a[u].w, b[u].w, v[u][i].z, v[u][i].w);
+        }
+    }
+    // c[i][0..1]: weight row gr, token rows 2 t and 2 t + 1 of part i; c[i][2..3]: row gr + 8
+    __syncthreads();  // (the last pass's sums are read)
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        part[warp][gr][8 * i + 2 * t + j] = c[i][j];
+        part[warp][gr + 8][8 * i + 2 * t + j] = c[i][2 + j];
+      }
+    __syncthreads();
+    constexpr int F = GATED ? 8 : 16;
+    for (int o = threadIdx.x; o < F * 8 * NT; o += FEW_THREADS) {
+      const int f = o % F, row = o / F;
+      if (f0 + f >= g.n || p0 + row >= r1) continue;
+      float v = 0.f, up = 0.f;
+#pragma unroll
+      for (int w = 0; w < FEW_WARPS; ++w) {
+        v += part[w][f][row];
+        if (GATED) up += part[w][f + 8][row];
+      }
+      if (g.bias) {
+        v += g.bias[e * nw + f0 + f];
+        if (GATED) up += g.bias[e * nw + g.n + f0 + f];
+      }
+      if (GATED)
+        v = (g.act == FB_ACT_SWIGLU ? silu_of<F32>(v) : gelu_f<F32>(v)) * up;
+      else if (g.act == FB_ACT_GELU)
+        v = gelu_f<F32>(v);
+      const size_t at = (size_t)(p0 + row) * g.ldo + f0 + f;
+      if (F32)
+        reinterpret_cast<float*>(g.out)[at] = v;
+      else
+        reinterpret_cast<bf16*>(g.out)[at] = __float2bfloat16(v);
+    }
+  }
+}
+
 // Rows in expert order: dst[r] = A[index[r]], one warp per row.
 __global__ void __launch_bounds__(256) gather_rows_kernel(const ExpertArgs g, bf16* dst, int* err) {
   griddep_wait();
@@ -561,7 +700,27 @@ int resident_clusters(int num_sms) {
 }
 
 template <bool GATED, bool F32>
+cudaError_t launch_few(const ExpertArgs& g, int* err, cudaStream_t st) {
+  const int blocks_n = GATED ? (g.n + 7) / 8 : (g.n + 15) / 16;
+  const long long groups = g.experts < g.max_rows ? g.experts : g.max_rows;  // with rows, at most
+  return g.max_rows <= 8
+             ? launch_k(expert_few_kernel<GATED, F32, 1>, dim3(groups * blocks_n), dim3(FEW_THREADS), 0,
+                        st, g, err)
+             : launch_k(expert_few_kernel<GATED, F32, 2>, dim3(groups * blocks_n), dim3(FEW_THREADS), 0,
+                        st, g, err);
+}
+
+template <bool GATED, bool F32>
 cudaError_t launch(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st) {
+  const int n_ft = ((GATED ? 2 * g.n : g.n) + 2 * W_ROWS - 1) / (2 * W_ROWS);
+  const long long groups = g.experts < g.max_rows ? g.experts : g.max_rows;  // with rows, at most
+  // Few rows whose tiles would leave SM pairs idle go to the streaming kernel; with tiles for all
+  // pairs the TMA ring keeps memory busier than it does (us, streamed / tiles; 8 experts, rows x n
+  // x k, gated): 2 x 4096 x 1536 gated 8.2 / 11.1, 2 x 1536 x 8960 11.3 / 28.9, 4 x 8960 x 1536
+  // 13.5 / 15.4, 8 x 8960 x 1536 35.1 / 30.9, 8 x 1536 x 4096 11.4 / 16.4, 16 x 1536 x 4096
+  // 19.3 / 21.2, 16 x 8960 x 1536 60.6 / 38.6; 2 experts, 32 x 2048 x 2048 5.6 / 11.2, 64 11.9 / 11.5.
+  if (g.max_rows <= 32 && groups * n_ft <= num_sms / 2 * (g.max_rows <= 8 ? 2 : 1))
+    return launch_few<GATED, F32>(g, err, st);
   auto kern = expert_tc_kernel<GATED, F32>;
   cudaError_t e =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
@@ -582,8 +741,6 @@ cudaError_t launch(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st) 
   const int occ = resident_clusters<GATED, F32>(num_sms);
   const int mc = occ < num_sms / 2 ? occ : num_sms / 2;
   // no more clusters than there can be tiles: 16 rows at least each but a group's last
-  const int n_ft = ((GATED ? 2 * g.n : g.n) + 2 * W_ROWS - 1) / (2 * W_ROWS);
-  const long long groups = g.experts < g.max_rows ? g.experts : g.max_rows;
   const long long tiles = (g.max_rows / T_STEP + groups) * n_ft;
   const int clusters = tiles < mc ? (int)tiles : mc;
   return launch_k(kern, dim3(2 * clusters), dim3(THREADS), SMEM_BYTES, st, mw, ma, ma8, mo, g, err);
