@@ -13,14 +13,16 @@
 //  * warp 0 loads weights, one TMA box of 128 rows x 64 k. Gated weights come as 16 gate rows
 //    and 16 up rows by turns (a 5-dimensional map over the two halves), so that the two values
 //    an output needs lie 16 lanes apart in one warp, and the weights stay as they are.
-//  * warps 10 and 11 load token rows, a K block each by turns: boxes of 64 and 8 consecutive
+//  * warps 10 and up load token rows, a K block each by turns: boxes of 64 and 8 consecutive
 //    rows, or with an index four rows of anywhere at a time (tile::gather4).
 //  * warp 1 issues the MMAs, warps 2-9 of both CTAs run the epilogue: bias and activation on
 //    TMEM columns, results through a shared-memory tile and TMA boxes of 16 tokens; the last,
 //    partly filled box of a group leaves by plain stores, since the rows behind it are the next
 //    expert's.
-// Sums are fp32 in TMEM. For fp32 results a K past 80 blocks of 64 is summed in parts with
-// accumulators of their own (the tensor core's sums lose about 7e-8 per block).
+// Sums are fp32 in TMEM. The tensor core's sums lose about 6e-8 of the result per K block of 64,
+// which fp32 results would show: they take K in parts of 14 blocks, each into an accumulator of
+// the ring, and the epilogue warps add the parts up (33 tokens over 64 experts, K = 1032: 1.0e-6
+// off in one part, 5e-7 in two; plain fp32 sums 2.5e-7). Their tiles are no wider than 128.
 // Every wait is bounded (mbar_wait): a role that gives up records it and the kernel ends.
 #include <cudaTypedefs.h>
 
@@ -35,7 +37,12 @@ constexpr int W_ROWS = 128;             // weight rows of a CTA
 constexpr int W_BYTES = W_ROWS * BK * 2;
 constexpr int TMEM_COLS = 512;
 constexpr int MAX_STAGES = 8, MAX_ACCS = 8;
-constexpr int THREADS = 384;            // W loader, MMA, 8 epilogue warps, 2 token loaders
+// Warps: weight loader, MMA, 8 epilogue warps, token loaders: two, or four that gather rows (in
+// fp32, whose epilogue holds its sums in registers, two).
+template <bool F32, bool GATHER>
+struct Warps {
+  static constexpr int LOADERS = GATHER && !F32 ? 4 : 2, THREADS = 32 * (10 + LOADERS);
+};
 constexpr int MAX_T = 256, T_STEP = 16, WIDTHS = MAX_T / T_STEP;
 constexpr int MAX_E = FB_ROUTE_MAX_EXPERTS;
 constexpr int SMEM_BYTES = 229888;      // (room for a normalisation block beside it, as the GEMM's)
@@ -45,7 +52,8 @@ constexpr int TABLE_BYTES = (2 * (MAX_E + 8) * 4 + 127) / 128 * 128;
 constexpr int BAR_BYTES = 512;
 constexpr int RING_BYTES = SMEM_BYTES - BAR_BYTES - EPI_BYTES - TABLE_BYTES;
 static_assert(RING_BYTES % 128 == 0, "TMA tiles lie on 128-byte boundaries");
-constexpr int PART_BLOCKS = 80;         // K blocks of one accumulator, for fp32 results
+constexpr int PART_BLOCKS = 14;         // K blocks of one accumulator, for fp32 results
+constexpr int F32_T = 128;              // widest tile then (its sums wait in registers)
 
 __host__ __device__ __forceinline__ int acc_cols_of(int T) { return (T + 31) / 32 * 32; }
 
@@ -136,11 +144,12 @@ struct TileIter {
   }
 };
 
-template <bool GATED, bool F32>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+template <bool GATED, bool F32, bool GATHER>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::THREADS, 1)
     expert_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                      const __grid_constant__ CUtensorMap tmA8, const __grid_constant__ CUtensorMap tmO,
                      const ExpertArgs g, int* err) {
+  constexpr int THREADS = Warps<F32, GATHER>::THREADS, LOADERS = Warps<F32, GATHER>::LOADERS;
   extern __shared__ __align__(1024) uint8_t smem[];  // (operand tiles need the alignment)
   if ((smem_u32(smem) & 1023u) != 0) {
     if (threadIdx.x == 0) fb_report(err, FB_DEVERR_BAD_ARG);
@@ -165,9 +174,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   const int cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
   const int nw = GATED ? 2 * g.n : g.n, n_ft = (nw + 2 * W_ROWS - 1) / (2 * W_ROWS);
   const int nk = (g.k + BK - 1) / BK, E = g.experts;
-  const int parts = F32 ? (nk + PART_BLOCKS - 1) / PART_BLOCKS < MAX_ACCS
-                              ? (nk + PART_BLOCKS - 1) / PART_BLOCKS : MAX_ACCS
-                        : 1;
+  const int parts = F32 ? (nk + PART_BLOCKS - 1) / PART_BLOCKS : 1;
   bool failed = false;
 
   if (threadIdx.x == 0) {
@@ -184,7 +191,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma_prefetch_desc(&tmW);
     tma_prefetch_desc(&tmA);
-    if (!g.index) tma_prefetch_desc(&tmA8);
+    if (!GATHER) tma_prefetch_desc(&tmA8);
     tma_prefetch_desc(&tmO);
   }
   if (threadIdx.x >= 64 && threadIdx.x < 64 + 2 * WIDTHS) cost[threadIdx.x - 64] = 0;
@@ -219,8 +226,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     // the fullest cluster each tile but the first takes its mainloop or its epilogue)
     const int T = T_STEP * (lane + 1);
     float est = 3e38f;
-    // (the ring holds a tile's K parts, and at least four where there are several)
-    if (lane < WIDTHS && (parts == 1 || acc_cols_of(T) * (parts < 4 ? 4 : parts) <= TMEM_COLS)) {
+    if (lane < WIDTHS && (!F32 || T <= F32_T)) {
       const float n = (float)count[lane] * n_ft, rounds = ceilf(n / n_clusters);
       const float main = count[lane] ? (float)cost[lane] / count[lane] * nk : 0.f;
       const float epi = F32 ? 3300.f + 30.f * T : 2900.f + 12.f * T;
@@ -280,12 +286,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     // ---------------- token rows (both CTAs) ----------------
     int stage = 0;
     uint32_t phase = 0;
-    bool mine = warp == 10;  // K blocks alternate between the two warps
+    int turn = warp - 10;  // K blocks until this warp's next: they go round the loaders
     while (!failed && ti.next(k)) {
       const int half = k.w / 2, a0 = k.r0 + half * (int)rank, end = k.r0 + k.nv;
       int src[4] = {0, 0, 0, 0};
       const int n4 = half / 4;
-      if (g.index && lane < n4) {
+      if (GATHER && lane < n4) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int row = a0 + 4 * lane + j;
@@ -296,12 +302,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
           }
         }
       }
-      for (int kb = 0; kb < nk; ++kb, mine = !mine) {
-        if (mine) {
+      for (int kb = 0; kb < nk; ++kb) {
+        if (turn-- == 0) {
+          turn = LOADERS - 1;
           if (!mbar_wait_warp(&empty[stage], phase ^ 1u, err)) { failed = true; break; }
           const uint32_t dst = smem_u32(smem) + stage * stage_bytes + W_BYTES;
           const uint32_t fb = mapa_shared(smem_u32(&full[stage]), 0);
-          if (g.index) {
+          if (GATHER) {
 #pragma unroll 4
             for (int i = 0; i < n4; ++i) {
               const int r0 = __shfl_sync(0xffffffffu, src[0], i), r1 = __shfl_sync(0xffffffffu, src[1], i);
@@ -365,38 +372,57 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     int acc = 0, buf = 0;
     uint32_t acc_phase = 0;
     while (!failed && ti.next(k)) {
-      // the last part's accumulator is complete after all others of the tile
-      int last = acc + parts - 1;
-      uint32_t last_phase = acc_phase;
-      if (last >= n_accs) { last -= n_accs; last_phase ^= 1u; }
       const int wrow = (2 * k.f + (int)rank) * W_ROWS + quarter * 32;  // of the interleaved rows
       const int f0 = GATED ? wrow / 2 : wrow;
       const int feature = f0 + (GATED ? lane & 15 : lane);
       float bias = 0.f;
       if (g.bias && feature < g.n)
         bias = __ldg(g.bias + (size_t)k.e * nw + feature + (GATED && lane >= 16 ? g.n : 0));
-      const bool ok = mbar_wait(&tmem_full[last], last_phase, err);
-      if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-      tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
-#pragma unroll 1
-      for (int t0 = half * CH; t0 < k.nv && f0 < g.n; t0 += 2 * CH) {
-        float v[CH];
-        for (int p = 0; p < parts; ++p) {
-          uint32_t r[CH];
-          const uint32_t a = taddr + (acc + p < n_accs ? acc + p : acc + p - n_accs) * acc_cols + t0;
-          if (CH == 32) {
-            tmem_ld32(a, r);
-            tmem_ld_wait();
-            reg_fence32(r);
-          } else {
-            tmem_ld16(a, r);
+      // fp32 results: the parts' sums are added up here as they are done, a part's accumulator
+      // going back to the ring at once
+      float sum[F32 ? F32_T / 2 : 1];
+      bool ok = true;
+      for (int p = 0; p < parts; ++p) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&tmem_full[acc], acc_phase, err));
+        if (!ok) break;
+        tc_fence_after();
+        if constexpr (F32) {
+#pragma unroll
+          for (int c = 0; c < F32_T / (2 * CH); ++c) {
+            const int t0 = (half + 2 * c) * CH;
+            if (t0 >= k.nv || f0 >= g.n) break;
+            uint32_t r[16];
+            tmem_ld16(taddr + acc * acc_cols + t0, r);
             tmem_ld_wait();
             reg_fence16(r);
-          }
 #pragma unroll
-          for (int j = 0; j < CH; ++j)
-            v[j] = p == 0 ? __uint_as_float(r[j]) : v[j] + __uint_as_float(r[j]);
+            for (int j = 0; j < 16; ++j)
+              sum[c * CH + j] = __uint_as_float(r[j]) + (p == 0 ? 0.f : sum[c * CH + j]);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(te_remote + acc * (uint32_t)sizeof(uint64_t));
+          if (++acc == n_accs) { acc = 0; acc_phase ^= 1u; }
+        }
+      }
+      if (!ok) { failed = true; break; }
+      constexpr int UNROLL = F32 ? F32_T / (2 * CH) : 1;  // (sum's indices are constants)
+#pragma unroll UNROLL
+      for (int c = 0; c < (F32 ? F32_T : MAX_T) / (2 * CH); ++c) {
+        const int t0 = (half + 2 * c) * CH;
+        if (t0 >= k.nv || f0 >= g.n) break;
+        float v[CH];
+        if constexpr (F32) {
+#pragma unroll
+          for (int j = 0; j < CH; ++j) v[j] = sum[c * CH + j];
+        } else {
+          uint32_t r[32];
+          tmem_ld32(taddr + acc * acc_cols + t0, r);
+          tmem_ld_wait();
+          reg_fence32(r);
+#pragma unroll
+          for (int j = 0; j < CH; ++j) v[j] = __uint_as_float(r[j]);
         }
         uint8_t* tile = tiles + buf * EPI_TILE;
         buf ^= 1;
@@ -456,9 +482,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
           __syncwarp();
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      for (int p = 0; p < parts; ++p) {
+      if constexpr (!F32) {
+        tc_fence_before();
+        __syncwarp();
         if (lane == 0) mbar_arrive_cluster(te_remote + acc * (uint32_t)sizeof(uint64_t));
         if (++acc == n_accs) { acc = 0; acc_phase ^= 1u; }
       }
@@ -491,7 +517,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 // tensor instruction is only there to keep the arithmetic out of the way of the loads. Its k
 // index is a permuted one, the same for both operands: lane (g, t) of a step of 32 holds k
 // 8 t .. 8 t + 7 of weight rows g and g + 8 and of token row g, 16 bytes each.
-constexpr int FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32, FEW_UNROLL = 4;
+constexpr int FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32, FEW_LONG_K = 2048;
 
 __device__ __forceinline__ void mma_16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2,
                                           uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -502,9 +528,12 @@ __device__ __forceinline__ void mma_16816(float* c, uint32_t a0, uint32_t a1, ui
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// NT: eight token rows each; a group of more is taken in several passes.
-template <bool GATED, bool F32, int NT>
-__global__ void __launch_bounds__(FEW_THREADS) expert_few_kernel(const ExpertArgs g, int* err) {
+// NT: eight token rows each; a group of more is taken in several passes. UN: steps of 32 k that a
+// warp has on their way, BLOCKS per SM that leave it the registers for that. Inputs from memory,
+// one token, us with 4 steps and 5 blocks an SM / 4 and 4 / 6 and 2: 4096 x 1536 gated 12.3 / 12.0
+// / 14.0 (six steps a warp in all), 1536 x 4096 14.7 / 10.0 / 7.0, 1536 x 8960 29.4 / 21.1 / 12.1.
+template <bool GATED, bool F32, int NT, int UN, int BLOCKS>
+__global__ void __launch_bounds__(FEW_THREADS, BLOCKS) expert_few_kernel(const ExpertArgs g, int* err) {
   griddep_wait();
   griddep_launch();
   __shared__ float part[FEW_WARPS][16][8 * NT + 1];
@@ -564,10 +593,10 @@ __global__ void __launch_bounds__(FEW_THREADS) expert_few_kernel(const ExpertArg
     }
     float c[NT][4] = {};
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    for (int s = s0; s < s1; s += FEW_UNROLL) {
-      uint4 a[FEW_UNROLL], b[FEW_UNROLL], v[FEW_UNROLL][NT];
+    for (int s = s0; s < s1; s += UN) {
+      uint4 a[UN], b[UN], v[UN][NT];
 #pragma unroll
-      for (int u = 0; u < FEW_UNROLL; ++u) {
+      for (int u = 0; u < UN; ++u) {
         const int kk = 32 * (s + u);
         const bool in = s + u < s1 && kk + 8 * t < g.k;
         a[u] = in ? __ldg(reinterpret_cast<const uint4*>(wa + kk)) : zero;
@@ -577,7 +606,7 @@ __global__ void __launch_bounds__(FEW_THREADS) expert_few_kernel(const ExpertArg
           v[u][i] = in && have[i] ? *reinterpret_cast<const uint4*>(x[i] + kk) : zero;
       }
 #pragma unroll
-      for (int u = 0; u < FEW_UNROLL; ++u)
+      for (int u = 0; u < UN; ++u)
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
           mma_16816(c[i], a[u].x, b[u].x, a[u].y, b[u].y, v[u][i].x, v[u][i].y);
@@ -675,7 +704,7 @@ bool make_map(CUtensorMap* map, const void* ptr, bool f32, const cuuint64_t (&di
 }
 
 // Clusters that the current device can hold at once, asked once per device.
-template <bool GATED, bool F32>
+template <bool GATED, bool F32, bool GATHER>
 int resident_clusters(int num_sms) {
   constexpr int DEVICES = 64;
   static std::atomic<int> known[DEVICES];  // zero until a launch has asked (any thread)
@@ -687,9 +716,9 @@ int resident_clusters(int num_sms) {
   cudaLaunchConfig_t cfg = {};
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) {
     cfg.gridDim = dim3(sms / 2 * 2, 1, 1);
-    cfg.blockDim = dim3(THREADS, 1, 1);
+    cfg.blockDim = dim3(Warps<F32, GATHER>::THREADS, 1, 1);
     cfg.dynamicSmemBytes = SMEM_BYTES;
-    if (cudaOccupancyMaxActiveClusters(&n, expert_tc_kernel<GATED, F32>, &cfg) == cudaSuccess &&
+    if (cudaOccupancyMaxActiveClusters(&n, expert_tc_kernel<GATED, F32, GATHER>, &cfg) == cudaSuccess &&
         n > 0) {
       if (dev < DEVICES) known[dev].store(n, std::memory_order_relaxed);
       return n;
@@ -703,25 +732,15 @@ template <bool GATED, bool F32>
 cudaError_t launch_few(const ExpertArgs& g, int* err, cudaStream_t st) {
   const int blocks_n = GATED ? (g.n + 7) / 8 : (g.n + 15) / 16;
   const long long groups = g.experts < g.max_rows ? g.experts : g.max_rows;  // with rows, at most
-  return g.max_rows <= 8
-             ? launch_k(expert_few_kernel<GATED, F32, 1>, dim3(groups * blocks_n), dim3(FEW_THREADS), 0,
-                        st, g, err)
-             : launch_k(expert_few_kernel<GATED, F32, 2>, dim3(groups * blocks_n), dim3(FEW_THREADS), 0,
-                        st, g, err);
+  auto kern = g.max_rows > 8        ? expert_few_kernel<GATED, F32, 2, 4, 2>
+              : g.k > FEW_LONG_K ? expert_few_kernel<GATED, F32, 1, 6, 2>
+                                    : expert_few_kernel<GATED, F32, 1, 4, GATED ? 4 : 3>;
+  return launch_k(kern, dim3(groups * blocks_n), dim3(FEW_THREADS), 0, st, g, err);
 }
 
-template <bool GATED, bool F32>
+template <bool GATED, bool F32, bool GATHER>
 cudaError_t launch(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st) {
-  const int n_ft = ((GATED ? 2 * g.n : g.n) + 2 * W_ROWS - 1) / (2 * W_ROWS);
-  const long long groups = g.experts < g.max_rows ? g.experts : g.max_rows;  // with rows, at most
-  // Few rows whose tiles would leave SM pairs idle go to the streaming kernel; with tiles for all
-  // pairs the TMA ring keeps memory busier than it does (us, streamed / tiles; 8 experts, rows x n
-  // x k, gated): 2 x 4096 x 1536 gated 8.2 / 11.1, 2 x 1536 x 8960 11.3 / 28.9, 4 x 8960 x 1536
-  // 13.5 / 15.4, 8 x 8960 x 1536 35.1 / 30.9, 8 x 1536 x 4096 11.4 / 16.4, 16 x 1536 x 4096
-  // 19.3 / 21.2, 16 x 8960 x 1536 60.6 / 38.6; 2 experts, 32 x 2048 x 2048 5.6 / 11.2, 64 11.9 / 11.5.
-  if (g.max_rows <= 32 && groups * n_ft <= num_sms / 2 * (g.max_rows <= 8 ? 2 : 1))
-    return launch_few<GATED, F32>(g, err, st);
-  auto kern = expert_tc_kernel<GATED, F32>;
+  auto kern = expert_tc_kernel<GATED, F32, GATHER>;
   cudaError_t e =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
   if (e != cudaSuccess) return e;
@@ -734,31 +753,51 @@ cudaError_t launch(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st) 
             : make_map<3>(&mw, g.W, false, {K, N, E}, {K, N * K}, {BK, W_ROWS, 1}, true);
   const u64 rows = g.a_rows, lda = g.lda, orows = g.max_rows, ldo = g.ldo;
   if (!w_ok ||
-      !make_map<2>(&ma, g.A, false, {K, rows}, {lda}, {BK, g.index ? 1u : 64u}, true) ||
-      (!g.index && !make_map<2>(&ma8, g.A, false, {K, rows}, {lda}, {BK, 8}, true)) ||
+      !make_map<2>(&ma, g.A, false, {K, rows}, {lda}, {BK, GATHER ? 1u : 64u}, true) ||
+      (!GATHER && !make_map<2>(&ma8, g.A, false, {K, rows}, {lda}, {BK, 8}, true)) ||
       !make_map<2>(&mo, g.out, F32, {N, orows}, {ldo}, {GATED ? 16u : 32u, 16}, false))
     return cudaErrorInvalidValue;
-  const int occ = resident_clusters<GATED, F32>(num_sms);
+  const int occ = resident_clusters<GATED, F32, GATHER>(num_sms);
   const int mc = occ < num_sms / 2 ? occ : num_sms / 2;
   // no more clusters than there can be tiles: 16 rows at least each but a group's last
+  const int n_ft = ((GATED ? 2 * g.n : g.n) + 2 * W_ROWS - 1) / (2 * W_ROWS);
+  const long long groups = g.experts < g.max_rows ? g.experts : g.max_rows;
   const long long tiles = (g.max_rows / T_STEP + groups) * n_ft;
   const int clusters = tiles < mc ? (int)tiles : mc;
-  return launch_k(kern, dim3(2 * clusters), dim3(THREADS), SMEM_BYTES, st, mw, ma, ma8, mo, g, err);
+  return launch_k(kern, dim3(2 * clusters), dim3(Warps<F32, GATHER>::THREADS), SMEM_BYTES, st, mw, ma, ma8, mo, g, err);
+}
+
+template <bool GATED, bool F32>
+cudaError_t choose(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st) {
+  const int n_ft = ((GATED ? 2 * g.n : g.n) + 2 * W_ROWS - 1) / (2 * W_ROWS);
+  const long long groups = g.experts < g.max_rows ? g.experts : g.max_rows;  // with rows, at most
+  // Few rows whose tiles would leave SM pairs idle go to the streaming kernel; with tiles for all
+  // pairs the TMA ring keeps memory busier than it does (us, streamed / tiles; 8 experts, rows x n
+  // x k, gated): 2 x 4096 x 1536 gated 8.2 / 11.1, 2 x 1536 x 8960 11.3 / 28.9, 4 x 8960 x 1536
+  // 13.5 / 15.4, 8 x 8960 x 1536 35.1 / 30.9, 8 x 1536 x 4096 11.4 / 16.4, 16 x 1536 x 4096
+  // 19.3 / 21.2, 16 x 8960 x 1536 60.6 / 38.6; 2 experts, 32 x 2048 x 2048 5.6 / 11.2, 64 11.9 / 11.5.
+  if (g.max_rows <= 32 && groups * n_ft <= num_sms / 2 * (g.max_rows <= 8 ? 2 : 1))
+    return launch_few<GATED, F32>(g, err, st);
+  return g.index ? launch<GATED, F32, true>(g, err, num_sms, st)
+                 : launch<GATED, F32, false>(g, err, num_sms, st);
 }
 
 }  // namespace
 
 cudaError_t expert_gemm_set_wait_limit(unsigned long long ns) { return fb_set_wait_limit_tu(ns); }
 
-// Groups of more than 96 rows on average have their rows copied to expert order first; smaller
-// ones are gathered by the product itself. A TMA gather costs its issuing warp 68 clocks per
-// four rows, which the loaders hide up to about that width; the copy is one more launch, about
-// 5 us, and 6 bytes per element. Measured (us, gathered / copied), E = 8, 8960 x 1536: 64 rows
-// a group 42.9 / 46.0, 96 48.4 / 47.3, 128 54.9 / 48.4, 390 130 / 73, 6240 1648 / 864.
-constexpr int GATHER_ROWS = 96;
+// Large groups have their rows copied to expert order first; small ones are gathered by the
+// product itself. A TMA gather costs its issuing warp 68 clocks per four rows whatever the form
+// of the loop, which four loaders hide up to tiles of about 192 rows (two, with fp32 results, 96);
+// the copy is one more launch, about 5 us, and 6 bytes per element. Measured (us, gathered /
+// copied): 8 experts, 8960 x 1536, 64 rows a group 41.5 / 46.0, 128 45.2 / 48.7, 195 52.0 / 52.2,
+// 256 68 / 63, 390 86 / 77, 6240 1061 / 864; 64 experts, 1024 x 1536 gated, 130 rows 78.5 / 86.8,
+// 300 126 / 125; fp32, 64 rows 25.4 / 29.9, 130 38.9 / 34.5. (Six or eight loaders: 965 at 6240
+// rows, but every further warp slows all others; copies by cp.async into the ring 2278: the issuer
+// then needs a proxy fence per K block, which waits for the SM's copies in flight.)
 size_t expert_gemm_ws_bytes(const ExpertArgs& g) {
-  return g.index && g.max_rows > (long long)GATHER_ROWS * g.experts
-             ? (size_t)g.max_rows * g.k * sizeof(bf16) : 0;
+  const long long most = g.out_type == FB_F32 ? 96 : 192;  // rows a group, on average
+  return g.index && g.max_rows > most * g.experts ? (size_t)g.max_rows * g.k * sizeof(bf16) : 0;
 }
 
 cudaError_t expert_copy_rows(ExpertArgs* g, bf16* ws, int* err, int num_sms, cudaStream_t st) {
@@ -778,6 +817,6 @@ cudaError_t expert_gemm(const ExpertArgs& g, int* err, int num_sms, cudaStream_t
   if (num_sms < 2) return cudaErrorInvalidValue;
   const bool f32 = g.out_type == FB_F32;
   if (g.act >= FB_ACT_SWIGLU)
-    return f32 ? launch<true, true>(g, err, num_sms, st) : launch<true, false>(g, err, num_sms, st);
-  return f32 ? launch<false, true>(g, err, num_sms, st) : launch<false, false>(g, err, num_sms, st);
+    return f32 ? choose<true, true>(g, err, num_sms, st) : choose<true, false>(g, err, num_sms, st);
+  return f32 ? choose<false, true>(g, err, num_sms, st) : choose<false, false>(g, err, num_sms, st);
 }
