@@ -438,9 +438,10 @@ fb_status fb_op_route(fb_model* m, const fb_route* r);
  * with a bf16 [a_rows][k], W bf16 [experts][n or 2 n][k], bias fp32 [experts][n or 2 n] or
  * NULL, out bf16 or fp32. offsets [experts + 1] (rising from 0 to at most max_rows) and
  * index [max_rows] are read on the device; groups may be empty, and rows from
- * offsets[experts] on are not written (nor their index entries read). Sums are fp32,
- * rounded once as they are stored. n and k are multiples of 8 (gated: n of 16), lda and ldo too; a, w and out are
- * 16-byte aligned. FB_EINVAL for other sizes, experts outside [1, FB_ROUTE_MAX_EXPERTS],
+ * offsets[experts] on are not written (nor their index entries read). Sums are fp32, rounded
+ * once as they are stored. n and k are multiples of 8 (gated: n of 16), lda and ldo too; a, w
+ * and out are 16-byte aligned. Large groups of indexed rows are copied to a scratch buffer of
+ * the model first (it grows on demand: FB_ENOMEM). FB_EINVAL for other sizes, experts outside [1, FB_ROUTE_MAX_EXPERTS],
  * max_rows outside [0, FB_ROUTE_MAX_PAIRS], or, found on the device, offsets that are not
  * as above or an index outside [0, a_rows) (the outputs are then not usable). */
 typedef struct fb_experts {

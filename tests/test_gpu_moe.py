@@ -550,3 +550,18 @@ def test_moe_forward_rejects(model):
                           fb.make_sandwich(h, h_out=h))
     with pytest.raises(ValueError):
         model.moe_forward(moe, a[:2].contiguous(), fb.make_sandwich(h, h_out=h))
+
+
+def test_example_runs_the_operators_together(capsys):
+    """The example's chain of layers. Its error: three bf16 roundings (normed input, hidden
+    rows, expert rows), each 2^-8 / sqrt(3) rms of its values, and a token whose second and
+    third logits nearly tie may go elsewhere (few enough to fit in twice that)."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "moe_feed_forward.py")
+    spec = importlib.util.spec_from_file_location("moe_feed_forward", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    assert mod.main(["--tokens", "200", "--layers", "2", "--experts", "6"]) <= 2 * 3 ** 0.5 * 2 ** -8 / 3 ** 0.5
+    assert "off by" in capsys.readouterr().out
