@@ -13,6 +13,9 @@
 //    other's counts through distributed shared memory (one block up to 32 tokens);
 //  * more tokens take three launches: choice and counts by blocks of up to 128 tokens, the
 //    blocks' counts added up expert by expert, and the pairs put in their places.
+// One token over 8 experts 2.5 us, 1560 5.9, 49920 over 64 (top 8) 28: bound by the latency of the
+// chains and launches up to a few thousand tokens, then by the choice's instructions (46 % of the
+// issue slots in 22 of the 28 us); the 19 MB that the last one moves would take 2.8.
 #include <float.h>
 
 #include "kernels.h"

@@ -13,8 +13,10 @@
 // parameter rows and the data go through: 199 us at 49920 rows of 1536, 141 with pieces of 4).
 // VEC: rows begin on a boundary of 4 values; else one value at a time, neighbours on
 // neighbouring lanes. Few rows, which are bound by the latency of one row's chain, get more
-// threads and load the row's parameters (EARLY) together with the row. 4.5 TB/s of 6.8 at 1560
-// rows of 1536 (y in bf16, h in fp32), 6.5 at 49920, one row 2.7 us.
+// threads and load the row's parameters (EARLY) together with the row. 3.9 TB/s of 6.8 at 1560
+// rows of 1536 (y in bf16, h in fp32), 6.5 at 49920, one row 2.7 us. Rows of no alignment are
+// bound by their instructions, 4 accesses for every one: 49920 rows of 1235 184 us, 4.0 TB/s
+// (244 with a comparison per value and threads for 1536).
 #include "kernels.h"
 
 namespace {
@@ -52,14 +54,25 @@ struct Row {
         const uint2 a = *reinterpret_cast<const uint2*>(reinterpret_cast<const bf16*>(base) + o);
         w[0] = a.x; w[1] = a.y;
       }
+    } else if (type == FB_F32) {
+      load_each(reinterpret_cast<const uint32_t*>(base) + at, i, D, tid, w);
+    } else {
+      load_each(reinterpret_cast<const uint16_t*>(base) + at, i, D, tid, w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] <<= 16;
+    }
+  }
+  // (a piece that lies wholly within the row needs one comparison)
+  template <typename T>
+  static __device__ __forceinline__ void load_each(const T* p, int i, int D, int tid, uint32_t* w) {
+    p += col(i, 0, tid);
+    if (col(i, 3, tid) < D) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = p[j * THREADS];
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (col(i, j, tid) >= D) continue;
-        const size_t o = at + col(i, j, tid);
-        w[j] = type == FB_F32 ? reinterpret_cast<const uint32_t*>(base)[o]
-                              : (uint32_t) reinterpret_cast<const uint16_t*>(base)[o] << 16;
-      }
+      for (int j = 0; j < 3; ++j)
+        if (col(i, j, tid) < D) w[j] = p[j * THREADS];
     }
   }
   static __device__ __forceinline__ void values(const uint32_t* w, int type, f2* v) {
@@ -87,15 +100,16 @@ struct Row {
         u.y = pack_bf16x2(v[2], v[3]);
         *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(base) + o) = u;
       }
-    } else {
+    } else if (type == FB_F32) {
+      float* p = reinterpret_cast<float*>(base) + at + col(i, 0, tid);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (col(i, j, tid) >= D) continue;
-        if (type == FB_F32)
-          reinterpret_cast<float*>(base)[at + col(i, j, tid)] = v[j];
-        else
-          reinterpret_cast<bf16*>(base)[at + col(i, j, tid)] = __float2bfloat16(v[j]);
-      }
+      for (int j = 0; j < 4; ++j)
+        if (col(i, 3, tid) < D || col(i, j, tid) < D) p[j * THREADS] = v[j];
+    } else {
+      bf16* p = reinterpret_cast<bf16*>(base) + at + col(i, 0, tid);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (col(i, 3, tid) < D || col(i, j, tid) < D) p[j * THREADS] = __float2bfloat16(v[j]);
     }
   }
   // A parameter row's piece, or `none` where there is no such row. Read-only loads: they need
@@ -109,10 +123,17 @@ struct Row {
         asm volatile("ld.global.nc.v4.f32 {%0, %1, %2, %3}, [%4];"
                      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "l"(p + col(i, 0, tid)));
       } else {
+        p += col(i, 0, tid);
+        if (col(i, 3, tid) < D) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (col(i, j, tid) < D)
-            asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v[j]) : "l"(p + col(i, j, tid)));
+          for (int j = 0; j < 4; ++j)
+            asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v[j]) : "l"(p + j * THREADS));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 3; ++j)
+            if (col(i, j, tid) < D)
+              asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v[j]) : "l"(p + j * THREADS));
+        }
       }
     }
     x[0] = f2_join(v[0], v[1]);
@@ -121,6 +142,7 @@ struct Row {
   // zeros in the place of values past D (in a piece that holds some; VEC: there are none)
   static __device__ __forceinline__ void clear_tail(f2* v, int i, int D, int tid) {
     if constexpr (!VEC) {
+      if (col(i, 3, tid) < D) return;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         float a, b;
@@ -355,10 +377,14 @@ cudaError_t middle(const SandwichArgs& s, bool many, int* err, cudaStream_t st) 
   const int D = s.dim;
   if (D <= 256) return run<32, 2, VEC, false, 4>(s, many, err, st);
   if (D <= 512) return run<64, 2, VEC>(s, many, err, st);
+  if (D <= 768) return run<96, 2, VEC>(s, many, err, st);
   if (D <= 1024) return run<128, 2, VEC>(s, many, err, st);
+  if (D <= 1280) return run<160, 2, VEC>(s, many, err, st);
   if (D <= 1536) return run<192, 2, VEC>(s, many, err, st);
   if (D <= 2048) return run<256, 2, VEC>(s, many, err, st);
+  if (D <= 2816) return run<352, 2, VEC>(s, many, err, st);
   if (D <= 4096) return run<512, 2, VEC>(s, many, err, st);
+  if (D <= 5120) return run<320, 4, VEC>(s, many, err, st);
   if (D <= 8192) return run<512, 4, VEC>(s, many, err, st);
   return run<512, 8, VEC>(s, many, err, st);
 }
