@@ -211,13 +211,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
     for (int i = threadIdx.x; i <= E; i += THREADS) off[i] = 0;
     __syncthreads();
   }
-  for (int i = threadIdx.x; i < E * WIDTHS; i += THREADS) {
-    const int e = i / WIDTHS, c = i % WIDTHS, T = T_STEP * (c + 1);
-    const int r = off[e + 1] - off[e];
-    if (r == 0) continue;
-    const int nt = (r + T - 1) / T, w = (r + nt - 1) / nt;
-    atomicAdd(&count[c], (unsigned)nt);
-    atomicAdd(&cost[c], (unsigned)(nt * (256 + w > 313 ? 256 + w : 313)));
+  {
+    // (nt tiles of widths that add up to r: 256 nt + r, see below)
+    const int c = threadIdx.x % WIDTHS, T = T_STEP * (c + 1);
+    unsigned tiles = 0, clocks = 0;
+    for (int e = threadIdx.x / WIDTHS; e < E; e += THREADS / WIDTHS) {
+      const int r = off[e + 1] - off[e], nt = (r + T - 1) / T;
+      tiles += nt;
+      clocks += 256 * nt + r > 313 * nt ? 256 * nt + r : 313 * nt;
+    }
+    if (tiles) {
+      atomicAdd(&count[c], tiles);
+      atomicAdd(&cost[c], clocks);
+    }
   }
   __syncthreads();
   if (warp == 0) {
