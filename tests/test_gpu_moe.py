@@ -565,3 +565,71 @@ def test_example_runs_the_operators_together(capsys):
     spec.loader.exec_module(mod)
     assert mod.main(["--tokens", "200", "--layers", "2", "--experts", "6"]) <= 2 * 3 ** 0.5 * 2 ** -8 / 3 ** 0.5
     assert "off by" in capsys.readouterr().out
+
+
+def test_experts_bad_index_in_copied_rows(model):
+    """Groups so large that their rows are copied first."""
+    a, w = torch.randn(50, 64, device="cuda").to(BF), torch.randn(2, 64, 64, device="cuda").to(BF)
+    out = torch.zeros(1000, 64, dtype=BF, device="cuda")
+    off = torch.tensor([0, 400, 1000], dtype=torch.int32, device="cuda")
+    idx = torch.zeros(1000, dtype=torch.int32, device="cuda")
+    idx[999] = 50
+    with pytest.raises(fb.FlashBonError) as e:
+        model.op_expert_gemm(fb.make_experts(a, w, off, out, index=idx))
+    assert e.value.status == fb.FB_EINVAL
+    idx[999] = 49
+    model.op_expert_gemm(fb.make_experts(a, w, off, out, index=idx))
+    want = a[idx.long()].double()
+    want = torch.cat([want[:400] @ w[0].double().T, want[400:] @ w[1].double().T])
+    check(out, want, 4 * 1.2e-7 * want.abs().max() * torch.ones_like(want), BF)
+
+
+@pytest.mark.parametrize("sizes", [[200, 300, 0], [0, 1000], [193, 193]])
+@pytest.mark.parametrize("act", ACTS)
+def test_experts_copied_rows(model, sizes, act):
+    experts_case(model, sizes, 144, 136, act=act, spare=7, pad=8, seed=40)
+
+
+def test_scratch_failure_leaves_the_model_usable():
+    """A scratch buffer that cannot be had: FB_ENOMEM, and the next call grows it."""
+    with fb.Model(synth.TINY, synth.make_weights(synth.TINY)) as m:
+        x = torch.randn(3000, 40, device="cuda")
+        out = route_buffers(3000, 40, 3)
+        r = fb.make_route(x, *out)
+        try:
+            fb.fb_test_fail_alloc(0)
+            with pytest.raises(fb.FlashBonError) as e:
+                m.op_route(r)
+            assert e.value.status == fb.FB_ENOMEM
+        finally:
+            fb.fb_test_fail_alloc(-1)
+        route_case(m, x, 3)
+        n = fb.fb_test_alloc_calls()
+        m.op_route(r)
+        assert fb.fb_test_alloc_calls() == n  # (nothing more to allocate)
+
+
+def test_two_models_at_once():
+    """Operators of two models from two threads, each with scratch and errors of its own."""
+    import threading
+    failed = []
+
+    def work(seed):
+        try:
+            with fb.Model(synth.TINY, synth.make_weights(synth.TINY)) as m:
+                st = torch.cuda.Stream()
+                m.set_stream(st)
+                with torch.cuda.stream(st):
+                    for i in range(4):
+                        experts_case(m, [250, 3, 400 + seed], 256, 192, act="swiglu", seed=seed + i)
+                        route_case(m, torch.randn(2000 + seed, 12, device="cuda"), 3)
+                        sandwich_case(m, 700, 520, parts=2, seed=seed + i)
+                m.set_stream(None)
+        except BaseException as e:  # noqa: BLE001
+            failed.append(e)
+    ts = [threading.Thread(target=work, args=(k,)) for k in (50, 60)]
+    for t in ts:
+        t.start()
+    for t in ts:
+        t.join()
+    assert not failed, failed
