@@ -13,9 +13,9 @@
 //    other's counts through distributed shared memory (one block up to 32 tokens);
 //  * more tokens take three launches: choice and counts by blocks of up to 128 tokens, the
 //    blocks' counts added up expert by expert, and the pairs put in their places.
-// One token over 8 experts 2.5 us, 1560 5.9, 49920 over 64 (top 8) 28: bound by the latency of the
+// One token over 8 experts 2.5 us, 1560 5.9, 49920 over 64 (top 8) 26: bound by the latency of the
 // chains and launches up to a few thousand tokens, then by the choice's instructions (46 % of the
-// issue slots in 22 of the 28 us); the 19 MB that the last one moves would take 2.8.
+// issue slots in its kernel); the 19 MB that the last one moves would take 2.8.
 #include <float.h>
 
 #include "kernels.h"
@@ -326,15 +326,17 @@ __global__ void __launch_bounds__(128) route_sum_kernel(const RouteArgs r, int* 
   griddep_launch();
   const int lane = threadIdx.x % 32, e = blockIdx.x * 4 + threadIdx.x / 32;
   if (e >= r.experts) return;
+  constexpr int PER = 16;  // blocks a lane: one pass up to 512
   int sum = 0;
-  for (int b0 = 0; b0 < blocks; b0 += 128) {
-    int n[4], s = 0;  // four blocks a lane
+  for (int b0 = 0; b0 < blocks; b0 += 32 * PER) {
+    int n[PER], s = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int b = b0 + 4 * lane + j;
+    for (int j = 0; j < PER; ++j) {
+      const int b = b0 + PER * lane + j;
       n[j] = b < blocks ? counts[(size_t)b * r.experts + e] : 0;
-      s += n[j];
     }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) s += n[j];
     int inc = s;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -343,8 +345,8 @@ __global__ void __launch_bounds__(128) route_sum_kernel(const RouteArgs r, int* 
     }
     int at = sum + inc - s;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int b = b0 + 4 * lane + j;
+    for (int j = 0; j < PER; ++j) {
+      const int b = b0 + PER * lane + j;
       if (b < blocks) counts[(size_t)b * r.experts + e] = at;
       at += n[j];
     }
@@ -379,7 +381,7 @@ __global__ void __launch_bounds__(THREADS) route_place_kernel(const RouteArgs r,
   }
 }
 
-// tokens of a block: few enough that every SM has a block or two
+// Tokens of a block: few enough that every SM has a block or two.
 int block_tokens(const RouteArgs& r) {
   return r.tokens <= 32 * 304 ? 32 : r.tokens <= 64 * 304 ? 64 : MAX_BLOCK_TOKENS;
 }
