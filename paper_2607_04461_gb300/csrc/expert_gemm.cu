@@ -8,8 +8,8 @@
 // tokens its N side, any multiple of 16 up to 256, so that ragged groups cost at most 15 rows
 // of padding each. Every CTA reads the offsets, picks the widest tile T that the launch uses
 // (choose_width) and cuts each group into equal tiles no wider than that; clusters take the
-// tiles in turn, an expert's weight rows fastest, which keeps its weights in L2 while its
-// tokens pass.
+// tiles in turn, weight rows fastest within a band of 16 MB of them (BAND_BYTES), then the
+// expert's tokens, then its next band: so the weights are read from memory once.
 //  * warp 0 loads weights, one TMA box of 128 rows x 64 k. Gated weights come as 16 gate rows
 //    and 16 up rows by turns (a 5-dimensional map over the two halves), so that the two values
 //    an output needs lie 16 lanes apart in one warp, and the weights stay as they are.
@@ -53,6 +53,12 @@ constexpr int TABLE_BYTES = (2 * (MAX_E + 8) * 4 + 127) / 128 * 128;
 constexpr int BAR_BYTES = 512;
 constexpr int RING_BYTES = SMEM_BYTES - BAR_BYTES - EPI_BYTES - TABLE_BYTES;
 static_assert(RING_BYTES % 128 == 0, "TMA tiles lie on 128-byte boundaries");
+// The weights that the clusters take before an expert's next tokens: a band of its weight tiles
+// that stays in L2 while all of the expert's tokens pass. us with bands of 16 / 32 / 64 MB / all
+// of an expert: 2 experts of 120 MB, 380 rows each 70.7 / 71.3 / 74.3 / 87.4; 4 of 147 MB, 2000
+// rows each 673 / 678 / 708 / 779; 8 of 73 MB, 3000 rows each 1037 / 1051 / 1120 / 1144; 8 of
+// 28 MB, 390 rows each 71.6 / 72.0 / 71.4 / 71.8.
+constexpr int64_t BAND_BYTES = 16ll << 20;
 constexpr int PART_BLOCKS = 7;          // K blocks of one accumulator, for fp32 results
 constexpr int F32_T = 128;              // widest tile then (its sums wait in registers)
 
@@ -115,16 +121,14 @@ struct Tile {
 // tiles before each group's.
 struct TileIter {
   const int *off, *first;
-  int t, step, n_ft, n_tiles, E, e;
-  __device__ TileIter(const int* off_, const int* first_, int c, int G, int n_ft_, int E_)
-      : off(off_), first(first_), t(c), step(G), n_ft(n_ft_), n_tiles(first_[E_] * n_ft_), E(E_),
-        e(0) {}
+  int t, step, n_ft, band, n_tiles, E, e;
+  __device__ TileIter(const int* off_, const int* first_, int c, int G, int n_ft_, int band_, int E_)
+      : off(off_), first(first_), t(c), step(G), n_ft(n_ft_), band(band_),
+        n_tiles(first_[E_] * n_ft_), E(E_), e(0) {}
   // (the whole warp, converged)
   __device__ bool next(Tile& k) {
     if (t >= n_tiles) return false;
     const int tt = t / n_ft, lane = threadIdx.x % 32;
-    k.f = t - tt * n_ft;
-    t += step;
     while (true) {  // the group that holds token tile tt: the first whose end lies behind it
       const unsigned m = __ballot_sync(0xffffffffu, e + lane < E && first[e + lane + 1] > tt);
       if (m) {
@@ -135,7 +139,11 @@ struct TileIter {
     }
     // the group's steps of 16 rows dealt out evenly: at most 15 rows of padding in all
     const int steps = (off[e + 1] - off[e] + T_STEP - 1) / T_STEP, nt = first[e + 1] - first[e];
-    const int j = tt - first[e], base = steps / nt, more = steps - base * nt;
+    const int u = t - first[e] * n_ft, f0 = u / (nt * band) * band, v = u - f0 * nt;
+    const int bw = n_ft - f0 < band ? n_ft - f0 : band;  // weight tiles of this band
+    const int j = v / bw, base = steps / nt, more = steps - base * nt;
+    k.f = f0 + v - j * bw;
+    t += step;
     k.e = e;
     k.w = (base + (j < more)) * T_STEP;
     k.r0 = off[e] + (j * base + (j < more ? j : more)) * T_STEP;
@@ -266,7 +274,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
   const int stages = RING_BYTES / stage_bytes < MAX_STAGES ? RING_BYTES / stage_bytes : MAX_STAGES;
   const int acc_cols = acc_cols_of(T);
   const int n_accs = TMEM_COLS / acc_cols < MAX_ACCS ? TMEM_COLS / acc_cols : MAX_ACCS;
-  TileIter ti(off, first, cluster, n_clusters, n_ft, E);
+  const int fit = (int)(BAND_BYTES / ((int64_t)2 * W_ROWS * g.k * sizeof(bf16)));
+  TileIter ti(off, first, cluster, n_clusters, n_ft, fit < 1 ? 1 : fit < n_ft ? fit : n_ft, E);
   Tile k;
 
   if (warp == 0) {
