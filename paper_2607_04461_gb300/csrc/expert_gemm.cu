@@ -205,7 +205,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
   }
   if (threadIdx.x >= 64 && threadIdx.x < 64 + 2 * WIDTHS) cost[threadIdx.x - 64] = 0;
   if (warp == 1) tmem_alloc_cg2(tmem_holder, TMEM_COLS);
-  griddep_wait();
+  // (copied rows: the offsets and all else but the rows were there before the copy began)
+  if (!g.copied) griddep_wait();
   griddep_launch();
   // ---- the groups and the tile width ----
   __syncthreads();
@@ -303,6 +304,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
     int stage = 0;
     uint32_t phase = 0;
     int turn = warp - 10;  // K blocks until this warp's next: they go round the loaders
+    griddep_wait();
     while (!failed && ti.next(k)) {
       const int half = k.w / 2, a0 = k.r0 + half * (int)rank, end = k.r0 + k.nv;
       int src[4] = {0, 0, 0, 0};
@@ -840,6 +842,7 @@ cudaError_t expert_copy_rows(ExpertArgs* g, bf16* ws, int* err, int num_sms, cud
   g->lda = g->k;
   g->a_rows = g->max_rows;
   g->index = nullptr;
+  g->copied = true;
   return e;
 }
 

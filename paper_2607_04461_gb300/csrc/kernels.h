@@ -161,6 +161,7 @@ struct ExpertArgs {
   void* out;
   int out_type;
   int64_t ldo;
+  bool copied;  // A was written by expert_copy_rows, the kernel before on the stream
 };
 // Bytes of scratch for the rows of A in expert order, where the product is faster on a copy of
 // them (else 0); expert_copy_rows makes that copy and points *g at it.
