@@ -823,15 +823,16 @@ cudaError_t expert_gemm_set_wait_limit(unsigned long long ns) { return fb_set_wa
 // product itself. A TMA gather costs its issuing warp 68 clocks per four rows whatever the form
 // of the loop, which four loaders hide up to tiles of about 192 rows (two, with fp32 results, 96);
 // the copy is one more launch, 2 to 3 us that the product's start does not hide, and 4 bytes per
-// element. Measured (us, gathered /
-// copied): 8 experts, 8960 x 1536, 64 rows a group 41.5 / 46.0, 128 45.2 / 48.7, 195 52.0 / 52.2,
-// 256 66 / 60, 390 84 / 72, 6240 1061 / 836; 64 experts, 1024 x 1536 gated, 130 rows 78.5 / 84,
-// 300 126 / 123; fp32, 64 rows 25.4 / 29.9, 130 38.9 / 34.5. Weight rows that are few read each
-// token few times and never pay for the copy: 8 experts, 512 x 1536, 390 rows a group 11.8 / 15.2,
-// 4000 47.8 / 74.6; 1536 x 8960 87 / 94, 654 / 726 (1536 x 1536 21.4 / 21.1, 124 / 129); 2048 x
-// 1536 25.5 / 22.8, 170 / 162; fp32, 512 x 1536, 390 rows 15.5 / 16.0, 768 x 1536 23.8 / 21.2. (Six or eight loaders: 965 at 6240
-// rows, but every further warp slows all others; copies by cp.async into the ring 2278: the issuer
-// then needs a proxy fence per K block, which waits for the SM's copies in flight.)
+// element. Measured (us, gathered / copied): 8 experts, 8960 x 1536, 64 rows a group 41.7 / 43.7,
+// 128 45.6 / 46.5, 195 52.6 / 49.8, 256 68 / 61, 390 87 / 76, 6240 1084 / 899; 64 experts,
+// 1024 x 1536 gated, 130 rows 73.0 / 79.9, 200 87 / 90, 300 129 / 124; fp32, 8 experts,
+// 4096 x 1536, 64 rows 25.8 / 26.6, 96 28.6 / 30.2, 130 38.0 / 36.1. Weight rows that are few read
+// each token few times and do not pay for the copy: 8 experts, 512 x 1536, 390 rows a group
+// 11.8 / 15.2, 4000 47.8 / 74.6; 1536 x 8960 87 / 94, 654 / 726 (1536 x 1536 21.4 / 21.1,
+// 124 / 129); 2048 x 1536 25.5 / 22.8, 170 / 162; fp32, 512 x 1536, 390 rows 15.5 / 16.0,
+// 768 x 1536 23.8 / 21.2. (Six or eight loaders: 965 at 6240 rows, but every further warp slows
+// all others; copies by cp.async into the ring 2278: the issuer then needs a proxy fence per K
+// block, which waits for the SM's copies in flight.)
 size_t expert_gemm_ws_bytes(const ExpertArgs& g) {
   const bool f32 = g.out_type == FB_F32;
   const long long most = f32 ? 96 : 192;  // rows a group, on average

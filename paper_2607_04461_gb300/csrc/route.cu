@@ -5,8 +5,8 @@
 // on how a sum was ordered. A NaN or -inf logit is never chosen, +inf counts as the largest
 // finite value; a token without a logit left, or with valid = 0, goes nowhere.
 //
-// A worker, eight lanes up to 64 experts and a warp past that, holds a token's logits as integers
-// in the order of the values, the next token's on their way, and takes the largest k times.
+// A worker, 8, 16 or 32 lanes (see route()), holds a token's logits as integers in the order of
+// the values, the next token's on their way, and takes the largest k times.
 // Pairs are ranked without atomics whose order could change them: a worker counts its own tokens
 // in order, a block adds its workers' counts up, and
 //  * up to CLUSTER_TOKENS tokens a cluster of eight blocks does all in one launch, reading each

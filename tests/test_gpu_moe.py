@@ -633,3 +633,40 @@ def test_two_models_at_once():
     for t in ts:
         t.join()
     assert not failed, failed
+
+
+@pytest.mark.parametrize("sizes", [[200, 300, 0], [0, 1000], [193, 193]])
+@pytest.mark.parametrize("n,act", [(1600, "none"), (1544, "gelu"), (800, "swiglu")])
+@pytest.mark.parametrize("out_t", [BF, F32])
+def test_experts_copied_rows_of_wide_experts(model, sizes, n, act, out_t):
+    """Weight rows enough that large groups' rows are copied first."""
+    experts_case(model, sizes, n, 136, act=act, out_t=out_t, spare=7, pad=8, seed=41)
+
+
+def test_experts_bad_index_in_copied_rows_of_wide_experts(model):
+    a, w = torch.randn(50, 64, device="cuda").to(BF), torch.randn(2, 1600, 64, device="cuda").to(BF)
+    out = torch.zeros(1000, 1600, dtype=BF, device="cuda")
+    off = torch.tensor([0, 400, 1000], dtype=torch.int32, device="cuda")
+    idx = torch.zeros(1000, dtype=torch.int32, device="cuda")
+    for bad in (-1, 50):
+        idx[999] = bad
+        with pytest.raises(fb.FlashBonError) as e:
+            model.op_expert_gemm(fb.make_experts(a, w, off, out, index=idx))
+        assert e.value.status == fb.FB_EINVAL
+    idx[999] = 49
+    for offsets in ([0, 1000, 400], [0, 400, 1001], [0, -1, 1000]):
+        bad_off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+        with pytest.raises(fb.FlashBonError) as e:
+            model.op_expert_gemm(fb.make_experts(a, w, bad_off, out, index=idx))
+        assert e.value.status == fb.FB_EINVAL
+    model.op_expert_gemm(fb.make_experts(a, w, off, out, index=idx))
+    want = a[idx.long()].double()
+    want = torch.cat([want[:400] @ w[0].double().T, want[400:] @ w[1].double().T])
+    check(out, want, 4 * 1.2e-7 * want.abs().max() * torch.ones_like(want), BF)
+
+
+@pytest.mark.parametrize("n,k", [(1200, 8960), (520, 40000), (2100 // 8 * 8, 8000)])
+@pytest.mark.parametrize("sizes", [[300, 17, 0, 520], [700, 600]])
+def test_experts_weights_in_bands(model, n, k, sizes):
+    """Experts of more weights than the product takes before it turns to the next tokens."""
+    experts_case(model, sizes, n, k, seed=42)
