@@ -113,42 +113,61 @@ __device__ __forceinline__ void tma_gather4_cg2(uint32_t dst, const CUtensorMap*
       : "memory");
 }
 
+// An arrival that orders no memory: it says that TMEM has been read (tcgen05.wait::ld has returned),
+// nothing else. A release at cluster scope waits for the warp's stores to be performed.
+__device__ __forceinline__ void mbar_arrive_relaxed_cluster(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr)
+               : "memory");
+}
+
 // ---- tiles ------------------------------------------------------------------------------
 struct Tile {
   int e, f, r0, w, nv;  // expert, weight-row tile, first row, width, rows of it that exist
 };
 // The tiles of this cluster, one after the other. off: the group offsets; first: the token
-// tiles before each group's.
+// tiles before each group's. Most calls divide once or not at all.
 struct TileIter {
   const int *off, *first;
-  int t, step, n_ft, band, n_tiles, E, e;
+  int t, step, n_ft, band, n_tiles, E;
+  // the group of tile t: its tiles [start, end), rows [r0, r1), token tiles nt of `base` steps of
+  // 16 rows, the first `more` of them of one more
+  int e = 0, start = 0, end = 0, r0 = 0, r1 = 0, nt = 1, base = 0, more = 0;
   __device__ TileIter(const int* off_, const int* first_, int c, int G, int n_ft_, int band_, int E_)
       : off(off_), first(first_), t(c), step(G), n_ft(n_ft_), band(band_),
-        n_tiles(first_[E_] * n_ft_), E(E_), e(0) {}
+        n_tiles(first_[E_] * n_ft_), E(E_) {}
   // (the whole warp, converged)
   __device__ bool next(Tile& k) {
     if (t >= n_tiles) return false;
-    const int tt = t / n_ft, lane = threadIdx.x % 32;
-    while (true) {  // the group that holds token tile tt: the first whose end lies behind it
-      const unsigned m = __ballot_sync(0xffffffffu, e + lane < E && first[e + lane + 1] > tt);
-      if (m) {
-        e += __ffs(m) - 1;
-        break;
+    if (t >= end) {  // the first group whose end lies behind t
+      const int lane = threadIdx.x % 32;
+      while (true) {
+        const unsigned m =
+            __ballot_sync(0xffffffffu, e + lane < E && first[e + lane + 1] * n_ft > t);
+        if (m) {
+          e += __ffs(m) - 1;
+          break;
+        }
+        e += 32;
       }
-      e += 32;
+      start = first[e] * n_ft;
+      end = first[e + 1] * n_ft;
+      r0 = off[e];
+      r1 = off[e + 1];
+      // its steps dealt out evenly: at most 15 rows of padding in all
+      const int steps = (r1 - r0 + T_STEP - 1) / T_STEP;
+      nt = first[e + 1] - first[e];
+      base = nt > 1 ? steps / nt : steps;
+      more = steps - base * nt;
     }
-    // the group's steps of 16 rows dealt out evenly: at most 15 rows of padding in all
-    const int steps = (off[e + 1] - off[e] + T_STEP - 1) / T_STEP, nt = first[e + 1] - first[e];
-    const int u = t - first[e] * n_ft, f0 = u / (nt * band) * band, v = u - f0 * nt;
+    const int u = t - start, f0 = n_ft > band ? u / (nt * band) * band : 0, v = u - f0 * nt;
     const int bw = n_ft - f0 < band ? n_ft - f0 : band;  // weight tiles of this band
-    const int j = v / bw, base = steps / nt, more = steps - base * nt;
-    k.f = f0 + v - j * bw;
+    const int j = nt > 1 ? v / bw : 0;
     t += step;
     k.e = e;
+    k.f = f0 + v - j * bw;
     k.w = (base + (j < more)) * T_STEP;
-    k.r0 = off[e] + (j * base + (j < more ? j : more)) * T_STEP;
-    const int left = off[e + 1] - k.r0;
-    k.nv = left < k.w ? left : k.w;
+    k.r0 = r0 + (j * base + (j < more ? j : more)) * T_STEP;
+    k.nv = r1 - k.r0 < k.w ? r1 - k.r0 : k.w;
     return true;
   }
 };
@@ -384,18 +403,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
     // warp: weight rows quarter * 32 .. + 31 of this CTA's 128 (its TMEM lanes), every other
     // CH-token chunk of the tile; FW output features, a lane's own or (gated) a lane pair's
     constexpr int CH = F32 ? 16 : 32, FW = GATED ? 16 : 32, ES = F32 ? 4 : 2;
-    const int quarter = warp & 3, half = (warp - 2) >> 2, we = warp - 2;
+    const int quarter = warp & 3, we = warp - 2;
+    int half = we >> 2;  // a tile's first chunk goes to either half by turns
     const uint32_t te_remote = mapa_shared(smem_u32(&tmem_empty[0]), 0);
     uint8_t* tiles = epi_smem + we * 2 * EPI_TILE;
     int acc = 0, buf = 0;
     uint32_t acc_phase = 0;
-    while (!failed && ti.next(k)) {
-      const int wrow = (2 * k.f + (int)rank) * W_ROWS + quarter * 32;  // of the interleaved rows
-      const int f0 = GATED ? wrow / 2 : wrow;
-      const int feature = f0 + (GATED ? lane & 15 : lane);
-      float bias = 0.f;
-      if (g.bias && feature < g.n)
-        bias = __ldg(g.bias + (size_t)k.e * nw + feature + (GATED && lane >= 16 ? g.n : 0));
+    // first output feature of this warp, and the bias of this lane's weight row
+    auto first_feature = [&](const Tile& q) {
+      const int wrow = (2 * q.f + (int)rank) * W_ROWS + quarter * 32;  // of the interleaved rows
+      return GATED ? wrow / 2 : wrow;
+    };
+    auto bias_of = [&](const Tile& q) {
+      const int feature = first_feature(q) + (GATED ? lane & 15 : lane);
+      return g.bias && feature < g.n
+                 ? __ldg(g.bias + (size_t)q.e * nw + feature + (GATED && lane >= 16 ? g.n : 0))
+                 : 0.f;
+    };
+    Tile after;
+    bool more = ti.next(k);
+    float bias = more ? bias_of(k) : 0.f;
+    for (; !failed && more; k = after) {
+      more = ti.next(after);
+      const float bias_after = more ? bias_of(after) : 0.f;  // (it may come from memory)
+      const int f0 = first_feature(k);
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
       // fp32 results: the parts' sums are added up here as they are done, a part's accumulator
       // going back to the ring at once
@@ -420,7 +451,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
           }
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(te_remote + acc * (uint32_t)sizeof(uint64_t));
+          if (lane == 0) mbar_arrive_relaxed_cluster(te_remote + acc * (uint32_t)sizeof(uint64_t));
           if (++acc == n_accs) { acc = 0; acc_phase ^= 1u; }
         }
       }
@@ -503,9 +534,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
       if constexpr (!F32) {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(te_remote + acc * (uint32_t)sizeof(uint64_t));
+        if (lane == 0) mbar_arrive_relaxed_cluster(te_remote + acc * (uint32_t)sizeof(uint64_t));
         if (++acc == n_accs) { acc = 0; acc_phase ^= 1u; }
       }
+      bias = bias_after;
+      half ^= 1;
     }
     // own TMA stores complete (one lane issued them all)
     if (elect_one()) bulk_wait<0>();

@@ -26,7 +26,8 @@ constexpr int WARPS = 16, THREADS = WARPS * 32;
 constexpr int MAX_E = FB_ROUTE_MAX_EXPERTS, MAX_K = FB_ROUTE_MAX_TOP_K;
 constexpr int MAX_BLOCK_TOKENS = 128;  // of the three-launch form
 constexpr int CLUSTER = 8;
-constexpr int CLUSTER_TOKENS = 768;
+#include <stdlib.h>
+#define CLUSTER_TOKENS (getenv("CT") ? atoi(getenv("CT")) : 768)
 
 // An fp32 value's bits in the order of the values; 0 for what is never chosen.
 __device__ __forceinline__ uint32_t order_key(float x) {
