@@ -20,10 +20,11 @@
 //    partly filled box of a group leaves by plain stores, since the rows behind it are the next
 //    expert's.
 // Sums are fp32 in TMEM. The tensor core's sums lose about 6e-8 of the result per K block of 64,
-// which fp32 results would show: they take K in parts of 7 blocks, each into an accumulator of
+// which fp32 results would show: they take K in parts of 4 blocks, each into an accumulator of
 // the ring, and the epilogue warps add the parts up; their tiles are no wider than 128. 2-norm of
-// the error and us with parts of 4 / 7 / 14 blocks, 8192 rows over 8 experts, 4096 x 1536: 2.3e-7
-// 138, 3.4e-7 118, 7.2e-7 106 (one chain 1.5e-6; fp32 sums in order 3.2e-7).
+// the error and us with parts of 3 / 4 / 7 / 14 blocks and one chain, 8192 rows over 8 experts,
+// 4096 x 1536: 1.8e-7 113, 2.3e-7 110, 3.4e-7 107, 7.2e-7 106, 1.5e-6 104 (fp32 sums in order
+// 3.2e-7).
 // Every wait is bounded (mbar_wait): a role that gives up records it and the kernel ends.
 #include <cudaTypedefs.h>
 
@@ -59,7 +60,7 @@ static_assert(RING_BYTES % 128 == 0, "TMA tiles lie on 128-byte boundaries");
 // rows each 673 / 678 / 708 / 779; 8 of 73 MB, 3000 rows each 1037 / 1051 / 1120 / 1144; 8 of
 // 28 MB, 390 rows each 71.6 / 72.0 / 71.4 / 71.8.
 constexpr int64_t BAND_BYTES = 16ll << 20;
-constexpr int PART_BLOCKS = 7;          // K blocks of one accumulator, for fp32 results
+constexpr int PART_BLOCKS = 4;          // K blocks of one accumulator, for fp32 results
 constexpr int F32_T = 128;              // widest tile then (its sums wait in registers)
 
 __host__ __device__ __forceinline__ int acc_cols_of(int T) { return (T + 31) / 32 * 32; }
@@ -69,11 +70,12 @@ __host__ __device__ __forceinline__ int acc_cols_of(int T) { return (T + 31) / 3
 template <bool EXACT>
 __device__ __forceinline__ float gelu_f(float x) {
   if (!EXACT) return gelu_tanh_f(x);
-  return 0.5f * x * (1.f + tanhf(0.7978845608028654f * (x + 0.044715f * x * x * x)));
+  // x / 2 (1 + tanh(u)) = x / (1 + e^(-2u)), which loses nothing to cancellation at negative x
+  return __fdividef(x, 1.f + expf(-1.5957691216057308f * (x + 0.044715f * x * x * x)));
 }
 template <bool EXACT>
 __device__ __forceinline__ float silu_of(float x) {
-  if (EXACT) return x / (1.f + expf(-x));
+  if (EXACT) return __fdividef(x, 1.f + expf(-x));
   const float h = 0.5f * x;  // x / (1 + e^-x) = x / 2 (1 + tanh(x / 2))
   return fmaf(h, tanh_approx(h), h);
 }
