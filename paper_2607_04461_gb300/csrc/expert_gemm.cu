@@ -16,9 +16,10 @@
 //  * warps 10 and up load token rows, a K block each by turns: boxes of 64 and 8 consecutive
 //    rows, or with an index four rows of anywhere at a time (tile::gather4).
 //  * warp 1 issues the MMAs, warps 2-9 of both CTAs run the epilogue: bias and activation on
-//    TMEM columns, results through a shared-memory tile and TMA boxes of 16 tokens; the last,
+//    TMEM columns, bf16 results through a shared-memory tile and TMA boxes of 16 tokens (the last,
 //    partly filled box of a group leaves by plain stores, since the rows behind it are the next
-//    expert's.
+//    expert's), fp32 results straight to memory (us, straight / through tiles, 8000 rows over 8
+//    experts: fp32, 4096 x 512 gated 87 / 103, 4096 x 1536 107 / 110; bf16, 4096 x 512 39 / 36).
 // Sums are fp32 in TMEM. The tensor core's sums lose about 6e-8 of the result per K block of 64,
 // which fp32 results would show: they take K in parts of 4 blocks, each into an accumulator of
 // the ring, and the epilogue warps add the parts up; their tiles are no wider than 128. 2-norm of
@@ -48,12 +49,14 @@ struct Warps {
 constexpr int MAX_T = 256, T_STEP = 16, WIDTHS = MAX_T / T_STEP;
 constexpr int MAX_E = FB_ROUTE_MAX_EXPERTS;
 constexpr int SMEM_BYTES = 229888;      // (room for a normalisation block beside it, as the GEMM's)
-constexpr int EPI_TILE = 2048;          // an epilogue warp's tile: CHUNK tokens x 32 rows
+constexpr int EPI_TILE = 2048;          // an epilogue warp's tile: 32 tokens x 32 rows, bf16
 constexpr int EPI_BYTES = 8 * 2 * EPI_TILE;
 constexpr int TABLE_BYTES = (2 * (MAX_E + 8) * 4 + 127) / 128 * 128;
 constexpr int BAR_BYTES = 512;
-constexpr int RING_BYTES = SMEM_BYTES - BAR_BYTES - EPI_BYTES - TABLE_BYTES;
-static_assert(RING_BYTES % 128 == 0, "TMA tiles lie on 128-byte boundaries");
+__host__ __device__ constexpr int ring_bytes(bool f32) {  // (fp32 results use no tiles)
+  return SMEM_BYTES - BAR_BYTES - TABLE_BYTES - (f32 ? 0 : EPI_BYTES);
+}
+static_assert(ring_bytes(false) % 128 == 0, "TMA tiles lie on 128-byte boundaries");
 // The weights that the clusters take before an expert's next tokens: a band of its weight tiles
 // that stays in L2 while all of the expert's tokens pass. us with bands of 16 / 32 / 64 MB / all
 // of an expert: 2 experts of 120 MB, 380 rows each 70.7 / 71.3 / 74.3 / 87.4; 4 of 147 MB, 2000
@@ -185,10 +188,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
     if (threadIdx.x == 0) fb_report(err, FB_DEVERR_BAD_ARG);
     return;
   }
+  constexpr int RING_BYTES = ring_bytes(F32);
   uint8_t* epi_smem = smem + RING_BYTES;
-  int* off = reinterpret_cast<int*>(epi_smem + EPI_BYTES);
+  int* off = reinterpret_cast<int*>(smem + SMEM_BYTES - BAR_BYTES - TABLE_BYTES);
   int* first = off + MAX_E + 8;
-  uint64_t* full = reinterpret_cast<uint64_t*>(epi_smem + EPI_BYTES + TABLE_BYTES);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + SMEM_BYTES - BAR_BYTES);
   uint64_t* empty = full + MAX_STAGES;
   uint64_t* tmem_full = empty + MAX_STAGES;
   uint64_t* tmem_empty = tmem_full + MAX_ACCS;
@@ -222,7 +226,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
     tma_prefetch_desc(&tmW);
     tma_prefetch_desc(&tmA);
     if (!GATHER) tma_prefetch_desc(&tmA8);
-    tma_prefetch_desc(&tmO);
+    if (!F32) tma_prefetch_desc(&tmO);
   }
   if (threadIdx.x >= 64 && threadIdx.x < 64 + 2 * WIDTHS) cost[threadIdx.x - 64] = 0;
   if (warp == 1) tmem_alloc_cg2(tmem_holder, TMEM_COLS);
@@ -404,7 +408,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
     // ---------------- epilogue (warps 2..9 of both CTAs) ----------------
     // warp: weight rows quarter * 32 .. + 31 of this CTA's 128 (its TMEM lanes), every other
     // CH-token chunk of the tile; FW output features, a lane's own or (gated) a lane pair's
-    constexpr int CH = F32 ? 16 : 32, FW = GATED ? 16 : 32, ES = F32 ? 4 : 2;
+    constexpr int CH = F32 ? 16 : 32, FW = GATED ? 16 : 32;
     const int quarter = warp & 3, we = warp - 2;
     int half = we >> 2;  // a tile's first chunk goes to either half by turns
     const uint32_t te_remote = mapa_shared(smem_u32(&tmem_empty[0]), 0);
@@ -428,7 +432,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
     for (; !failed && more; k = after) {
       more = ti.next(after);
       const float bias_after = more ? bias_of(after) : 0.f;  // (it may come from memory)
-      const int f0 = first_feature(k);
+      const int f0 = first_feature(k), feature = f0 + (GATED ? lane & 15 : lane);
+      // tokens j and j + 1 of a gated chunk: lanes 0-15 form j's outputs, lanes 16-31 j + 1's
+      auto gated = [&](float x0, float x1) {
+        const float got = __shfl_xor_sync(0xffffffffu, lane < 16 ? x1 : x0, 16);
+        const float gate = lane < 16 ? x0 : got, up = lane < 16 ? got : x1;
+        return (g.act == FB_ACT_SWIGLU ? silu_of<F32>(gate) : gelu_f<F32>(gate)) * up;
+      };
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
       // fp32 results: the parts' sums are added up here as they are done, a part's accumulator
       // going back to the ring at once
@@ -475,29 +485,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
 #pragma unroll
           for (int j = 0; j < CH; ++j) v[j] = __uint_as_float(r[j]);
         }
+        if constexpr (F32) {
+          // straight to memory, 32 or (gated, two tokens at once) 16 features of a token
+          const int n = k.nv - t0;
+          float* at = reinterpret_cast<float*>(g.out) +
+                      (size_t)(k.r0 + t0 + (GATED ? lane >> 4 : 0)) * g.ldo + feature;
+          if (GATED) {
+#pragma unroll
+            for (int j = 0; j < CH; j += 2, at += 2 * g.ldo) {
+              const float y = gated(v[j] + bias, v[j + 1] + bias);
+              if (j + (lane >> 4) < n && feature < g.n) *at = y;
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < CH; ++j, at += g.ldo) {
+              const float x = v[j] + bias;
+              if (j < n && feature < g.n) *at = g.act == FB_ACT_GELU ? gelu_f<true>(x) : x;
+            }
+          }
+          continue;
+        }
         uint8_t* tile = tiles + buf * EPI_TILE;
         buf ^= 1;
         if (elect_one()) bulk_wait_read<1>();  // the store from this tile two chunks ago
         __syncwarp();
         if (GATED) {
-          // tokens j and j + 1: lanes 0-15 form j's outputs, lanes 16-31 j + 1's
 #pragma unroll
-          for (int j = 0; j < CH; j += 2) {
-            const float x0 = v[j] + bias, x1 = v[j + 1] + bias;
-            const float got = __shfl_xor_sync(0xffffffffu, lane < 16 ? x1 : x0, 16);
-            const float gate = lane < 16 ? x0 : got, up = lane < 16 ? got : x1;
-            const float y = (g.act == FB_ACT_SWIGLU ? silu_of<F32>(gate) : gelu_f<F32>(gate)) * up;
-            if (F32)
-              reinterpret_cast<float*>(tile)[j * 16 + lane] = y;
-            else
-              reinterpret_cast<bf16*>(tile)[j * 16 + lane] = __float2bfloat16(y);
-          }
-        } else if (F32) {
-#pragma unroll
-          for (int j = 0; j < CH; ++j) {
-            const float x = v[j] + bias;
-            reinterpret_cast<float*>(tile)[j * 32 + lane] = g.act == FB_ACT_GELU ? gelu_f<true>(x) : x;
-          }
+          for (int j = 0; j < CH; j += 2)
+            reinterpret_cast<bf16*>(tile)[j * 16 + lane] =
+                __float2bfloat16(gated(v[j] + bias, v[j + 1] + bias));
         } else {
           // two tokens' values of each lane's feature as one 4-byte store per lane: lanes
           // exchange with their neighbour, even lanes then hold two features of token j, odd
@@ -517,18 +533,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
         if (elect_one()) {
 #pragma unroll
           for (int b = 0; b < CH; b += 16)
-            if (b + 16 <= n) tma_store_2d(&tmO, smem_u32(tile) + b * FW * ES, f0, k.r0 + t0 + b);
+            if (b + 16 <= n) tma_store_2d(&tmO, smem_u32(tile) + b * FW * 2, f0, k.r0 + t0 + b);
           bulk_commit();
         }
         if (n % 16) {  // 16 bytes at a time: n is a multiple of 8 features
-          constexpr int PIECES = FW * ES / 16, PE = 16 / ES;
+          constexpr int PIECES = FW / 8;
           const int b = n / 16 * 16;
           for (int i = lane; i < (n - b) * PIECES; i += 32) {
             const int tok = b + i / PIECES, c = i % PIECES;
-            if (f0 + c * PE < g.n)
-              *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(g.out) +
-                                        ((size_t)(k.r0 + t0 + tok) * g.ldo + f0 + c * PE) * ES) =
-                  *reinterpret_cast<const uint4*>(tile + tok * FW * ES + c * 16);
+            if (f0 + c * 8 < g.n)
+              *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(g.out) +
+                                        (size_t)(k.r0 + t0 + tok) * g.ldo + f0 + c * 8) =
+                  *reinterpret_cast<const uint4*>(tile + tok * FW * 2 + c * 16);
           }
           __syncwarp();
         }
@@ -754,7 +770,7 @@ PFN_cuTensorMapEncodeTiled_v12000 encoder() {
 }
 
 template <int R>
-bool make_map(CUtensorMap* map, const void* ptr, bool f32, const cuuint64_t (&dims)[R],
+bool make_map(CUtensorMap* map, const void* ptr, const cuuint64_t (&dims)[R],
               const cuuint64_t (&stride_elems)[R - 1], const cuuint32_t (&box)[R], bool swizzle) {
   auto enc = encoder();
   if (!enc) return false;
@@ -762,10 +778,9 @@ bool make_map(CUtensorMap* map, const void* ptr, bool f32, const cuuint64_t (&di
   cuuint32_t estr[R];
   for (int i = 0; i < R; ++i) {
     estr[i] = 1;
-    if (i) strides[i - 1] = stride_elems[i - 1] * (f32 ? 4 : 2);
+    if (i) strides[i - 1] = stride_elems[i - 1] * 2;
   }
-  return enc(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, R,
-             const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, R, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
              swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
              swizzle ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -814,16 +829,16 @@ cudaError_t launch(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st) 
   if (e != cudaSuccess) return e;
   typedef cuuint64_t u64;
   const u64 K = g.k, N = g.n, E = g.experts;
-  CUtensorMap mw, ma, ma8{}, mo;  // ma8: unused with an index
+  CUtensorMap mw, ma, ma8{}, mo{};  // ma8: unused with an index, mo: with fp32 results
   const bool w_ok =
-      GATED ? make_map<5>(&mw, g.W, false, {K, 16, 2, N / 16, E}, {K, N * K, 16 * K, 2 * N * K},
+      GATED ? make_map<5>(&mw, g.W, {K, 16, 2, N / 16, E}, {K, N * K, 16 * K, 2 * N * K},
                           {BK, 16, 2, W_ROWS / 32, 1}, true)
-            : make_map<3>(&mw, g.W, false, {K, N, E}, {K, N * K}, {BK, W_ROWS, 1}, true);
+            : make_map<3>(&mw, g.W, {K, N, E}, {K, N * K}, {BK, W_ROWS, 1}, true);
   const u64 rows = g.a_rows, lda = g.lda, orows = g.max_rows, ldo = g.ldo;
   if (!w_ok ||
-      !make_map<2>(&ma, g.A, false, {K, rows}, {lda}, {BK, GATHER ? 1u : 64u}, true) ||
-      (!GATHER && !make_map<2>(&ma8, g.A, false, {K, rows}, {lda}, {BK, 8}, true)) ||
-      !make_map<2>(&mo, g.out, F32, {N, orows}, {ldo}, {GATED ? 16u : 32u, 16}, false))
+      !make_map<2>(&ma, g.A, {K, rows}, {lda}, {BK, GATHER ? 1u : 64u}, true) ||
+      (!GATHER && !make_map<2>(&ma8, g.A, {K, rows}, {lda}, {BK, 8}, true)) ||
+      (!F32 && !make_map<2>(&mo, g.out, {N, orows}, {ldo}, {GATED ? 16u : 32u, 16}, false)))
     return cudaErrorInvalidValue;
   const int occ = resident_clusters<GATED, F32, GATHER>(num_sms);
   const int mc = occ < num_sms / 2 ? occ : num_sms / 2;
