@@ -9,8 +9,8 @@
 // the values, the next token's on their way, and takes the largest k times.
 // Pairs are ranked without atomics whose order could change them: a worker counts its own tokens
 // in order, a block adds its workers' counts up, and
-//  * up to CLUSTER_TOKENS tokens a cluster of eight blocks does all in one launch, reading each
-//    other's counts through distributed shared memory (one block up to 32 tokens);
+//  * few tokens (in_cluster) are one launch of a cluster of eight blocks, which read each other's
+//    counts through distributed shared memory (one block up to 32 tokens);
 //  * more tokens take three launches: choice and counts by blocks of up to 128 tokens, the
 //    blocks' counts added up expert by expert, and the pairs put in their places.
 // One token over 8 experts 2.5 us, 1560 5.9, 49920 over 64 (top 8) 26: bound by the latency of the
@@ -26,8 +26,14 @@ constexpr int WARPS = 16, THREADS = WARPS * 32;
 constexpr int MAX_E = FB_ROUTE_MAX_EXPERTS, MAX_K = FB_ROUTE_MAX_TOP_K;
 constexpr int MAX_BLOCK_TOKENS = 128;  // of the three-launch form
 constexpr int CLUSTER = 8;
-#include <stdlib.h>
-#define CLUSTER_TOKENS (getenv("CT") ? atoi(getenv("CT")) : 768)
+
+// Whether one launch of a cluster takes all tokens. us, cluster / three launches, top 8 of 8
+// experts, 512 tokens 5.8 / 7.2, 768 7.8 / 7.2 (top 2 5.1 / 6.3); of 64, 384 tokens 7.2 / 7.6,
+// 512 8.7 / 7.9; of 256, 256 tokens 8.3 / 10.2, 384 11.0 / 10.3 (top 2 7.6 / 8.2); of 512, 256
+// tokens 12.6 / 14.5, 384 17.1 / 14.5.
+bool in_cluster(const RouteArgs& r) {
+  return r.tokens <= (r.experts <= 8 ? 768 : r.experts <= 256 ? 384 : 256);
+}
 
 // An fp32 value's bits in the order of the values; 0 for what is never chosen.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -389,7 +395,7 @@ int block_tokens(const RouteArgs& r) {
 
 template <int L, int R>
 cudaError_t run(const RouteArgs& r, int* counts, cudaStream_t st) {
-  if (r.tokens <= CLUSTER_TOKENS) {
+  if (in_cluster(r)) {
     const int share = (r.tokens + CLUSTER - 1) / CLUSTER;
     if (r.tokens <= 32)
       return launch_k(route_block_kernel<L, R>, dim3(1), dim3(THREADS),
@@ -410,12 +416,12 @@ cudaError_t run(const RouteArgs& r, int* counts, cudaStream_t st) {
 }  // namespace
 
 size_t route_ws_bytes(const RouteArgs& r) {
-  if (r.tokens <= CLUSTER_TOKENS) return 0;
+  if (in_cluster(r)) return 0;
   const size_t bt = block_tokens(r);
   return ((r.tokens + bt - 1) / bt + 1) * r.experts * sizeof(int);
 }
 
-int route_launches(const RouteArgs& r) { return r.tokens <= CLUSTER_TOKENS ? 1 : 3; }
+int route_launches(const RouteArgs& r) { return in_cluster(r) ? 1 : 3; }
 
 cudaError_t route(const RouteArgs& r0, void* ws, cudaStream_t st) {
   RouteArgs r = r0;

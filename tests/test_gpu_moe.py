@@ -485,7 +485,8 @@ def test_stream_budget_repeat_and_counters(model):
         model.set_stream(None)
     after = model.stats()
     n = {k: after[k]["launches"] - before[k]["launches"] for k in ("sandwich_norm", "route", "expert_gemm")}
-    assert n == {"sandwich_norm": 3, "route": 6, "expert_gemm": 6}
+    # (700 tokens over 32 experts are routed in three launches)
+    assert n == {"sandwich_norm": 3, "route": 18, "expert_gemm": 6}
 
 
 # ---- all of it ------------------------------------------------------------------------
