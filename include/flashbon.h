@@ -467,8 +467,8 @@ fb_status fb_op_expert_gemm(fb_model* m, const fb_experts* g);
  * before it); s->a, the next block's input, may be the same buffer. s->y, slot and weight
  * must be NULL (the call fills them in). router_w: bf16 [router_rows][dim], router_rows a
  * multiple of 8 and at least `experts`; rows behind `experts` are ignored (padded to a
- * multiple of 128 the product runs on the tensor cores where dim % 64 == 0). hidden and dim
- * are multiples of 16. valid: as in fb_op_route, or NULL. The
+ * multiple of 128 the product of more than 32 rows runs on the tensor cores where
+ * dim % 64 == 0). hidden and dim are multiples of 16. valid: as in fb_op_route, or NULL. The
  * scratch buffers are the model's and grow on demand (FB_ENOMEM). */
 typedef struct fb_moe {
   int dim, hidden, experts, top_k, renorm, act, router_rows;

@@ -1829,8 +1829,21 @@ fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const ui
   lay_out();
   CKS(expert_args(up, &gu));
   CKS(expert_args(down, &gd));
-  CKS(run_gemm(m, gemm_args((int)T, moe->router_rows, moe->dim, (const bf16*)a,
-                            (const bf16*)moe->router_w, nullptr, EPI_RESID, ws + o_log)));
+  // The router's product: few rows as a group of streamed weights, more as a GEMM (us of the whole
+  // call, 8 experts of 2048 gated at width 1536, group / GEMM: 1 row 31.1 / 38.9; as a group of
+  // tiles 64 rows 74.8 / 70.1, 1560 108.5 / 106.4).
+  if (T <= 32 && reinterpret_cast<uintptr_t>(moe->router_w) % 16 == 0) {
+    ExpertArgs gr{1, (moe->experts + 7) / 8 * 8, moe->dim, (int)T, (int)T, (const bf16*)a, moe->dim};
+    gr.W = (const bf16*)moe->router_w;
+    gr.act = FB_ACT_NONE;
+    gr.out = ws + o_log;
+    gr.out_type = FB_F32;
+    gr.ldo = moe->router_rows;
+    CKS(run_experts(m, gr, nullptr));  // (no index, no copy)
+  } else {
+    CKS(run_gemm(m, gemm_args((int)T, moe->router_rows, moe->dim, (const bf16*)a,
+                              (const bf16*)moe->router_w, nullptr, EPI_RESID, ws + o_log)));
+  }
   CKS(run_route(m, r, ws + o_cnt));
   CKS(run_experts(m, gu, ws + o_rows));
   CKS(run_experts(m, gd, nullptr));  // (no index, no copy)

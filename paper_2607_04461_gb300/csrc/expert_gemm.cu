@@ -618,7 +618,8 @@ __global__ void __launch_bounds__(FEW_THREADS, BLOCKS) expert_few_kernel(const E
     __syncwarp();
     for (int e0 = 0; e0 < g.experts; e0 += 32) {
       const int e = e0 + lane;
-      const int a = e < g.experts ? g.offsets[e] : 0, b = e < g.experts ? g.offsets[e + 1] : 0;
+      const int a = e >= g.experts ? 0 : g.offsets ? g.offsets[e] : 0;
+      const int b = e >= g.experts ? 0 : g.offsets ? g.offsets[e + 1] : g.max_rows;
       const unsigned some = __ballot_sync(0xffffffffu, b > a);
       const int at = seen + __popc(some & ((1u << lane) - 1));
       if (b > a && at == want) {
@@ -859,7 +860,9 @@ cudaError_t choose(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st) 
   // x k, gated): 2 x 4096 x 1536 gated 8.2 / 11.1, 2 x 1536 x 8960 11.3 / 28.9, 4 x 8960 x 1536
   // 13.5 / 15.4, 8 x 8960 x 1536 35.1 / 30.9, 8 x 1536 x 4096 11.4 / 16.4, 16 x 1536 x 4096
   // 19.3 / 21.2, 16 x 8960 x 1536 60.6 / 38.6; 2 experts, 32 x 2048 x 2048 5.6 / 11.2, 64 11.9 / 11.5.
-  if (g.max_rows <= 32 && groups * n_ft <= num_sms / 2 * (g.max_rows <= 8 ? 2 : 1))
+  // (Without offsets it is always these.)
+  if (!g.offsets ||
+      (g.max_rows <= 32 && groups * n_ft <= num_sms / 2 * (g.max_rows <= 8 ? 2 : 1)))
     return launch_few<GATED, F32>(g, err, st);
   return g.index ? launch<GATED, F32, true>(g, err, num_sms, st)
                  : launch<GATED, F32, false>(g, err, num_sms, st);

@@ -154,7 +154,7 @@ struct ExpertArgs {
   int experts, n, k, max_rows, a_rows;
   const bf16* A;
   int64_t lda;
-  const int32_t *index, *offsets;
+  const int32_t *index, *offsets;  // (offsets null: one group of max_rows, at most 32)
   const bf16* W;
   const float* bias;
   int act;

@@ -671,3 +671,19 @@ def test_experts_bad_index_in_copied_rows_of_wide_experts(model):
 def test_experts_weights_in_bands(model, n, k, sizes):
     """Experts of more weights than the product takes before it turns to the next tokens."""
     experts_case(model, sizes, n, k, seed=42)
+
+
+@pytest.mark.parametrize("T,E", [(2, 3), (31, 64), (40, 100), (1000, 512), (17000, 8)])
+def test_moe_forward_router_sizes(model, T, E):
+    """Few and many rows and experts: the router's product takes other forms."""
+    test_moe_forward(model, T, 256, 64, E, min(E, 2), "gelu", 128)
+
+
+def test_moe_forward_router_on_two_sms(model):
+    """As few SMs as a budget can name, and experts for more tiles than these take at once."""
+    try:
+        model.set_sm_budget(2)
+        test_moe_forward(model, 20, 256, 64, 500, 2, "gelu", 8)
+        test_moe_forward(model, 40, 256, 64, 500, 2, "gelu", 8)
+    finally:
+        model.set_sm_budget(0)
