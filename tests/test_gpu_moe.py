@@ -9,7 +9,8 @@ Tolerances, from the arithmetic:
   * rounding to bf16: 2^-8 of the value (8 significant bits, half a unit of the last one).
   * products: a 64-wide K block is four MMAs, each of which may cut the running sum by one
     fp32 unit, 1.2e-7 of it. The largest result stands for the running sum.
-  * bf16 results of GELU and SiLU take the hardware tanh, 2^-10.9 of tanh, which x / 2 multiplies.
+  * bf16 results of GELU and SiLU may be off by 2^-10.9 of the tanh that x / 2 multiplies, as with
+    the hardware tanh; that they keep bf16's precision where that cancels has a test of its own.
 """
 import math
 
@@ -687,3 +688,41 @@ def test_moe_forward_router_on_two_sms(model):
         test_moe_forward(model, 40, 256, 64, 500, 2, "gelu", 8)
     finally:
         model.set_sm_budget(0)
+
+
+def activation_rows(act, out_t, rows):
+    """Outputs of one expert at chosen values v before the activation, and v's two parts in float64.
+    A row of `a` has one element that is not zero, so that products and sums are exact."""
+    n, k = 2048, 64
+    grid = torch.cat([torch.linspace(-20, 4, n - 256), torch.linspace(-90, 90, 256)]).to(BF)
+    gated = act in ("swiglu", "geglu")
+    w = torch.zeros(1, 2 * n if gated else n, k, dtype=BF, device="cuda")
+    w[0, :n, 0] = grid.cuda()
+    if gated:
+        w[0, n:, 0] = torch.tensor([1.0, -2.5, 0.375, 96.0]).repeat(n // 4).to(BF).cuda()
+    a = torch.zeros(rows, k, dtype=BF, device="cuda")
+    a[:, 0] = torch.tensor([1.0, 0.75, 0.5, -1.0]).repeat(rows)[:rows].to(BF)
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    out = torch.full((rows, n), 3.0, device="cuda").to(out_t)
+    return a, w, off, out, a[:, :1].double() * w[0, :n, 0].double(), \
+        a[:, :1].double() * w[0, n:, 0].double() if gated else None
+
+
+@pytest.mark.parametrize("act", ["gelu", "swiglu", "geglu"])
+@pytest.mark.parametrize("out_t", [BF, F32])
+@pytest.mark.parametrize("rows", [4, 70])
+def test_experts_activations_keep_their_precision(model, act, out_t, rows):
+    """Every result within its type's rounding and a few fp32 units, the small ones at negative
+    arguments too, where x / 2 (1 + tanh) cancels. x sigmoid(z), z = x or the tanh form's 2 u:
+    z is off by up to 8 roundings, 2^-24 each, which the exponential turns into a relative error of
+    8 |z| 2^-24; the exponential, 1 + it, the quotient and the product with `up` add less than 16
+    units. Past z = -86 the quotient's divisor passes 2^125 and the result may be 0."""
+    a, w, off, out, v, up = activation_rows(act, out_t, rows)
+    model.op_expert_gemm(fb.make_experts(a, w, off, out, act=act))
+    torch.cuda.synchronize()
+    z = v if act == "swiglu" else 2 * math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3)
+    want = v / (1 + torch.exp(-z))
+    tol = 2.0 ** -24 * (16 + 8 * z.abs().clamp(max=90)) * want.abs() + (z < -86) * want.abs()
+    if up is not None:
+        want, tol = want * up, tol * up.abs()
+    check(out, want, tol + 1e-37, out_t)
