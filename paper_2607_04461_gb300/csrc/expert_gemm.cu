@@ -640,27 +640,29 @@ __global__ void __launch_bounds__(FEW_THREADS, BLOCKS) expert_few_kernel(const E
   // the blockIdx.x / blocks_n-th group that has rows
   const int want = blockIdx.x / blocks_n;
   if (warp == 0) {
-    int seen = 0;
+    int seen = 0, at_e = -1, at_r0 = 0, at_r1 = 0;  // the group, in the lane that comes upon it
     bool bad = false;
-    if (lane == 0) found[0] = -1;
-    __syncwarp();
     for (int e0 = 0; e0 < g.experts; e0 += 32) {
       const int e = e0 + lane;
       const int a = e >= g.experts ? 0 : g.offsets ? g.offsets[e] : 0;
       const int b = e >= g.experts ? 0 : g.offsets ? g.offsets[e + 1] : g.max_rows;
       const unsigned some = __ballot_sync(0xffffffffu, b > a);
-      const int at = seen + __popc(some & ((1u << lane) - 1));
-      if (b > a && at == want) {
-        found[0] = e;
-        found[1] = a;
-        found[2] = b;
+      if (b > a && seen + __popc(some & ((1u << lane) - 1)) == want) {
+        at_e = e;
+        at_r0 = a;
+        at_r1 = b;
       }
       seen += __popc(some);
       bad = bad || b < a || a < 0 || b > g.max_rows || (e == 0 && a != 0);
     }
-    if (__any_sync(0xffffffffu, bad) && lane == 0) {
-      fb_report(err, FB_DEVERR_BAD_INDEX);
-      found[0] = -1;
+    // one lane writes, once, and no group out of a table that holds anything bad
+    const bool refused = __any_sync(0xffffffffu, bad);
+    const unsigned has = __ballot_sync(0xffffffffu, at_e >= 0);
+    if (lane == (has ? __ffs(has) - 1 : 0)) {
+      found[0] = refused ? -1 : at_e;
+      found[1] = at_r0;
+      found[2] = at_r1;
+      if (refused) fb_report(err, FB_DEVERR_BAD_INDEX);
     }
   }
   __syncthreads();

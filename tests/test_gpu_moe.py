@@ -726,3 +726,25 @@ def test_experts_activations_keep_their_precision(model, act, out_t, rows):
     if up is not None:
         want, tol = want * up, tol * up.abs()
     check(out, want, tol + 1e-37, out_t)
+
+
+@pytest.mark.parametrize("rows", [12, 200, 8000])
+@pytest.mark.parametrize("at,value", [(1, 1 << 30), (7, 1 << 30), (7, -4), (33, 1 << 30), (40, 1 << 30),
+                                      (40, 0), (0, 2)])
+def test_experts_bad_offsets_write_nothing(model, rows, at, value):
+    """One bad offset among many good ones, met by any lane that looks: no group is taken out of
+    such a table, in the streamed form, in tiles and with copied rows."""
+    n = 1600 if rows == 8000 else 256
+    a, w = torch.randn(rows, 64, device="cuda").to(BF), torch.randn(40, n, 64, device="cuda").to(BF)
+    off = (torch.arange(41) * rows // 40).int()
+    good = off.cuda()
+    off[at] = value
+    idx = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    for index in (None, idx):
+        out = torch.full((rows, n), 3.0, device="cuda").to(BF)
+        with pytest.raises(fb.FlashBonError) as e:
+            model.op_expert_gemm(fb.make_experts(a, w, off.cuda(), out, index=index))
+        assert e.value.status == fb.FB_EINVAL
+        assert torch.all(out == 3.0)
+        model.op_expert_gemm(fb.make_experts(a, w, good, out, index=index))
+        assert torch.all((out != 3.0).any(1))
