@@ -281,19 +281,24 @@ enum {
   FB_K_SANDWICH,      /* norms around a block, gate, scaled residual, expert combination */
   FB_K_ROUTE,         /* router: top-k experts, rows sorted by expert */
   FB_K_EXPERT,        /* products grouped by expert */
-  FB_K_COUNT
+  FB_K_COUNT,
+  FB_K_BASE_COUNT = FB_K_SANDWICH /* the kinds that fb_get_stats copies, in every version */
 };
 typedef struct fb_kstat {
   uint64_t launches;
   double ms, flops, bytes;
 } fb_kstat;
 /* fb_set_timing: `on` is a bit mask; bit k records CUDA events around every launch of
- * class k (FB_K_*), 0 stops timing. fb_get_stats waits for the model's stream and
- * copies the FB_K_COUNT counters (launch counts and algorithmic work are always kept,
- * times only for timed classes); fb_reset_stats zeroes them; fb_kernel_name gives a
- * class's name ("?" outside [0, FB_K_COUNT)). FB_EINVAL for a NULL model or output. */
+ * class k (FB_K_*), 0 stops timing. fb_get_stats_n waits for the model's stream and
+ * copies the counters of the first n classes, zeros behind class FB_K_COUNT - 1 (launch
+ * counts and algorithmic work are always kept, times only for timed classes); call it with
+ * n = FB_K_COUNT, which grows as classes are added. fb_get_stats copies the first
+ * FB_K_BASE_COUNT of them, whatever the version: it has no way to know of more room.
+ * fb_reset_stats zeroes all; fb_kernel_name gives a class's name ("?" outside [0,
+ * FB_K_COUNT)). FB_EINVAL for a NULL model or output, or n < 0. */
 fb_status fb_set_timing(fb_model* m, int on);
-fb_status fb_get_stats(fb_model* m, fb_kstat* out /* [FB_K_COUNT] */);
+fb_status fb_get_stats(fb_model* m, fb_kstat* out /* [FB_K_BASE_COUNT] */);
+fb_status fb_get_stats_n(fb_model* m, fb_kstat* out /* [n] */, int n);
 fb_status fb_reset_stats(fb_model* m);
 const char* fb_kernel_name(int kind);
 

@@ -1670,13 +1670,16 @@ fb_status fb_set_timing(fb_model* m, int mask) {
   return FB_OK;
 }
 
-fb_status fb_get_stats(fb_model* m, fb_kstat* out) {
+fb_status fb_get_stats_n(fb_model* m, fb_kstat* out, int n) {
   if (!m || !out) return fail(FB_EINVAL, "null argument");
+  if (n < 0) return fail(FB_EINVAL, "n=%d", n);
   CK(cudaStreamSynchronize(m->st));
   collect_timings(m);
-  memcpy(out, m->stats, sizeof m->stats);
+  for (int k = 0; k < n; ++k) out[k] = k < FB_K_COUNT ? m->stats[k] : fb_kstat{};
   return FB_OK;
 }
+
+fb_status fb_get_stats(fb_model* m, fb_kstat* out) { return fb_get_stats_n(m, out, FB_K_BASE_COUNT); }
 
 fb_status fb_reset_stats(fb_model* m) {
   if (!m) return fail(FB_EINVAL, "model is NULL");

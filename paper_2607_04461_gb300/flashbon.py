@@ -95,7 +95,8 @@ ACTS = {"none": 0, "gelu": 1, "swiglu": 2, "geglu": 3}
 
 EXPORTS = ["fb_weights_count", "fb_weights_entry", "fb_init_model", "fb_free", "fb_set_stream",
            "fb_encode_text", "fb_draft", "fb_refine", "fb_plan_from_phi", "fb_block_forward",
-           "fb_last_error", "fb_set_timing", "fb_get_stats", "fb_reset_stats", "fb_kernel_name",
+           "fb_last_error", "fb_set_timing", "fb_get_stats", "fb_get_stats_n", "fb_reset_stats",
+           "fb_kernel_name",
            "fb_op_gemm", "fb_op_attention", "fb_draft_ex", "fb_refine_ex", "fb_select_elo",
            "fb_set_op_repeat", "fb_gemm_streamk_noalloc", "fb_state_bytes", "fb_state_offload",
            "fb_state_wait", "fb_set_sm_budget", "fb_sm_split_create", "fb_sm_split_info",
@@ -141,6 +142,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "fb_set_timing": (I, [P, I]),
         "fb_set_op_repeat": (I, [P, I]),
         "fb_get_stats": (I, [P, P]),
+        "fb_get_stats_n": (I, [P, P, I]),
         "fb_reset_stats": (I, [P]),
         "fb_kernel_name": (ctypes.c_char_p, [I]),
         "fb_op_gemm": (I, [P, I, I, I, P, P, P, I, P, P, P, P, P, I]),
@@ -519,7 +521,7 @@ def fb_probe_mma_mix(form: int, loaders: int = 0, loader_gap: int = 0) -> float:
 
 def fb_get_stats(model: int) -> dict:
     arr = (fb_kstat * len(KERNEL_KINDS))()
-    _check(load_library().fb_get_stats(model, ctypes.cast(arr, ctypes.c_void_p)))
+    _check(load_library().fb_get_stats_n(model, ctypes.cast(arr, ctypes.c_void_p), len(arr)))
     return {KERNEL_KINDS[i]: dict(launches=int(arr[i].launches), ms=arr[i].ms,
                                   flops=arr[i].flops, bytes=arr[i].bytes)
             for i in range(len(KERNEL_KINDS))}

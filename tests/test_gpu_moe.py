@@ -12,6 +12,7 @@ Tolerances, from the arithmetic:
   * bf16 results of GELU and SiLU may be off by 2^-10.9 of the tanh that x / 2 multiplies, as with
     the hardware tanh; that they keep bf16's precision where that cancels has a test of its own.
 """
+import ctypes
 import math
 
 import numpy as np
@@ -748,3 +749,22 @@ def test_experts_bad_offsets_write_nothing(model, rows, at, value):
         assert torch.all(out == 3.0)
         model.op_expert_gemm(fb.make_experts(a, w, good, out, index=index))
         assert torch.all((out != 3.0).any(1))
+
+
+def test_stats_keep_to_the_room_that_they_have(model):
+    """fb_get_stats writes the ten kinds that it had before there were more; fb_get_stats_n as
+    many as it is told."""
+    lib, size = fb.load_library(), ctypes.sizeof(fb.fb_kstat)
+    arr = (fb.fb_kstat * 16)()
+    p = ctypes.cast(arr, ctypes.c_void_p)
+    for call, kinds in ((lambda: lib.fb_get_stats(model.handle, p), 10),
+                        (lambda: lib.fb_get_stats_n(model.handle, p, 0), 0),
+                        (lambda: lib.fb_get_stats_n(model.handle, p, 12), 12),
+                        (lambda: lib.fb_get_stats_n(model.handle, p, 15), 15)):
+        ctypes.memset(arr, 0xa5, 16 * size)
+        assert call() == fb.FB_OK
+        raw = bytes(arr)
+        assert raw[kinds * size:] == b"\xa5" * ((16 - kinds) * size)
+        assert all(a.launches == s["launches"] for a, s in zip(arr[:kinds], model.stats().values()))
+        assert all(a.launches == 0 for a in arr[len(fb.KERNEL_KINDS):kinds])
+    assert lib.fb_get_stats_n(model.handle, p, -1) == fb.FB_EINVAL
