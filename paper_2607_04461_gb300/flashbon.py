@@ -581,7 +581,9 @@ _FLOATS = ("bfloat16", "float32")
 
 
 def _row_stride(x):
-    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1])
+    """Elements from a row to the next; one row alone has no stride of its own (torch's may be
+    anything), and its width will do."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
 
 
 def _type(x):

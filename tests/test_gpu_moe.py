@@ -768,3 +768,19 @@ def test_stats_keep_to_the_room_that_they_have(model):
         assert all(a.launches == s["launches"] for a, s in zip(arr[:kinds], model.stats().values()))
         assert all(a.launches == 0 for a in arr[len(fb.KERNEL_KINDS):kinds])
     assert lib.fb_get_stats_n(model.handle, p, -1) == fb.FB_EINVAL
+
+
+def test_one_row_of_a_wider_matrix(model):
+    """A matrix of one row has no row stride: a view of an odd-sized buffer is taken."""
+    k, n = 64, 128
+    buf, obuf = torch.randn(3, k + 3, device="cuda").to(BF), torch.zeros(2, n + 5, dtype=BF, device="cuda")
+    w = torch.randn(1, n, k, device="cuda").to(BF)
+    off = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    model.op_expert_gemm(fb.make_experts(buf[:1, :k], w, off, obuf[:1, :n]))
+    want = buf[:1, :k].double() @ w[0].double().T
+    check(obuf[:1, :n], want, 4 * 1.2e-7 * want.abs().max() * torch.ones_like(want), BF)
+    assert torch.all(obuf[0, n:] == 0) and torch.all(obuf[1] == 0)
+    one = torch.randn(k, device="cuda").to(BF).expand(1, k)  # (a row repeated: stride 0)
+    model.op_expert_gemm(fb.make_experts(one, w, off, obuf[:1, :n]))
+    want = one.double() @ w[0].double().T
+    check(obuf[:1, :n], want, 4 * 1.2e-7 * want.abs().max() * torch.ones_like(want), BF)
