@@ -447,9 +447,10 @@ fb_status fb_op_route(fb_model* m, const fb_route* r);
  * once as they are stored. n and k are multiples of 8 (gated: n of 16), lda and ldo too; a, w
  * and out are 16-byte aligned. Large groups of indexed rows are copied to a scratch buffer of
  * the model first (it grows on demand: FB_ENOMEM). FB_EINVAL for other sizes, experts
- * outside [1, FB_ROUTE_MAX_EXPERTS], max_rows outside [0, FB_ROUTE_MAX_PAIRS], or, found on
- * the device, offsets that are not as above or an index outside [0, a_rows) (the outputs are
- * then not usable). */
+ * outside [1, FB_ROUTE_MAX_EXPERTS], max_rows outside [0, FB_ROUTE_MAX_PAIRS], an expert's
+ * weight rows (n or 2 n) or k past FB_EXPERT_MAX_SIZE, or, found on the device, offsets that
+ * are not as above or an index outside [0, a_rows) (the outputs are then not usable). */
+#define FB_EXPERT_MAX_SIZE (1 << 30)
 typedef struct fb_experts {
   int experts, n, k, max_rows, a_rows;
   const void* a;

@@ -510,6 +510,10 @@ fb_status expert_args(const fb_experts& g, ExpertArgs* out) {
   const int nm = g.act >= FB_ACT_SWIGLU ? 16 : 8;
   if (g.n < 1 || g.k < 1 || g.n % nm || g.k % 8)
     return fail(FB_EINVAL, "n=%d must be a multiple of %d, k=%d of 8", g.n, nm, g.k);
+  // (the kernels count weight rows and K in int, past the last one by less than a tile)
+  if (g.n > FB_EXPERT_MAX_SIZE / (g.act >= FB_ACT_SWIGLU ? 2 : 1) || g.k > FB_EXPERT_MAX_SIZE)
+    return fail(FB_EINVAL, "n=%d k=%d: an expert's weight rows and k may be %d at most", g.n, g.k,
+                FB_EXPERT_MAX_SIZE);
   if (!g.offsets || (g.max_rows > 0 && (!g.a || !g.w || !g.out)))
     return fail(FB_EINVAL, "null argument");
   if (!known_type(g.out_type)) return fail(FB_EINVAL, "out must be FB_BF16 or FB_F32");

@@ -102,3 +102,19 @@ def test_make_functions_check_their_tensors():
         fb.make_sandwich(torch.zeros(2, 8))
     with pytest.raises(TypeError, match="CUDA"):
         fb.make_experts(torch.zeros(2, 8), torch.zeros(1, 8, 8), None, torch.zeros(2, 8))
+
+
+@pytest.mark.parametrize("bad", [
+    dict(n=(1 << 30) + 8, ldo=(1 << 30) + 8), dict(n=(1 << 31) - 8, ldo=1 << 31),
+    dict(n=(1 << 29) + 16, ldo=1 << 30, act=2), dict(n=1 << 30, ldo=1 << 30, act=3),
+    dict(k=(1 << 30) + 8, lda=(1 << 30) + 8), dict(k=(1 << 31) - 8, lda=1 << 31),
+])
+def test_experts_sizes_past_the_kernels_counters(lib, bad):
+    """Weight rows or a K that the kernels' 32-bit counters would not hold."""
+    assert lib.fb_op_expert_gemm(P, ctypes.byref(experts(**bad))) == fb.FB_EINVAL
+    assert b"at most" in lib.fb_last_error()
+    moe = fb.fb_moe(dim=64, hidden=(1 << 29) + 16, experts=4, top_k=2, router_rows=8, router_w=P,
+                    w1=P, w2=P, act=2)
+    assert lib.fb_moe_forward(P, ctypes.byref(moe), P, None,
+                              ctypes.byref(sandwich(y=None))) == fb.FB_EINVAL
+    assert b"at most" in lib.fb_last_error()
