@@ -784,3 +784,145 @@ def test_one_row_of_a_wider_matrix(model):
     model.op_expert_gemm(fb.make_experts(one, w, off, obuf[:1, :n]))
     want = one.double() @ w[0].double().T
     check(obuf[:1, :n], want, 4 * 1.2e-7 * want.abs().max() * torch.ones_like(want), BF)
+
+
+def route_sorted(x, valid, k, renorm):
+    """route64 for many tokens at once."""
+    x = x.float().cpu().numpy().astype(np.float64)
+    T, E = x.shape
+    x = np.where(np.isnan(x), -np.inf, np.minimum(x, np.finfo(np.float32).max))
+    if valid is not None:
+        x[valid.cpu().numpy() == 0] = -np.inf
+    expert = np.argsort(-x, axis=1, kind="stable")[:, :k]
+    top = np.take_along_axis(x, expert, 1)
+    none = top == -np.inf
+    shift = np.where(none[:, :1], 0, top[:, :1])
+    e = np.where(none, 0, np.exp(top - shift))
+    total = e.sum(1, keepdims=True) if renorm else np.exp(x - shift).sum(1, keepdims=True)
+    weight = e / np.where(none[:, :1], 1, total)
+    flat = np.where(none, E, expert).reshape(-1)
+    order = np.argsort(flat, kind="stable")
+    offsets = np.searchsorted(flat[order], np.arange(E + 1))
+    token = np.where(flat[order] == E, -1, order // k)
+    slot = np.empty(T * k, dtype=np.int64)
+    slot[order] = np.arange(T * k)
+    return (np.where(none, -1, expert), weight, np.where(none, -1, slot.reshape(T, k)), token, offsets)
+
+
+@pytest.mark.parametrize("T,k,dtype,pad", [(12289, 1, F32, 0), (12300, 8, BF, 0), (20000, 8, F32, 0),
+                                           (12289, 16, F32, 4), (20000, 16, BF, 3)])
+@pytest.mark.parametrize("E", [9, 16, 17, 32, 33, 64, 100, 128, 200, 256, 300])
+def test_route_of_a_pool(model, T, E, k, dtype, pad):
+    """Several lanes a token, several experts a lane, with ties, masked experts, padding tokens and
+    rows of any stride."""
+    g = gen(T + E + k)
+    k = min(k, E)
+    x = torch.randn(T, E, generator=g, device="cuda")
+    x = torch.where(torch.rand(T, E, generator=g, device="cuda") < 0.4, (2 * x).round() / 2, x)
+    x[::3][torch.rand(x[::3].shape, generator=g, device="cuda") < 0.7] = -math.inf
+    x[5:8], x[9, 1], x[9, 3] = float("nan"), math.inf, math.inf
+    x[11], x[12, :] = -math.inf, 0.25
+    x[12345 % T:] += 0.5
+    valid = (torch.rand(T, generator=g, device="cuda") < 0.8).to(torch.uint8)
+    x[valid == 0] = float("nan")
+    x = x.to(dtype)
+    if pad:
+        x = padded(x, pad, float("nan"))
+    out = route_buffers(T, E, k)
+    for v, renorm in ((valid, False), (None, True)):
+        want = route_sorted(x, v, k, renorm)
+        model.op_route(fb.make_route(x, *out, valid=v, renorm=renorm))
+        for name, got, w in zip(("expert", "weight", "slot", "token", "offsets"), out, want):
+            if name != "weight":
+                assert np.array_equal(got.cpu().numpy(), w), name
+        tol = 6e-8 * (4 + E / 32 + 5 + 40)  # (as in route_case; a lane's own terms number E / 8 at most)
+        tol = tol + 6e-8 * E / 8
+        assert (np.abs(out[1].cpu().numpy() - want[1]) <= tol * want[1] + 1e-37).all()
+
+
+@pytest.mark.parametrize("rows", [3, 700, 2500])
+@pytest.mark.parametrize("D", [200, 256, 412, 512, 700, 768, 1000, 1024, 1280, 1500, 1536, 2000, 2048,
+                               2816, 4000, 4096, 5120, 8192, 12000])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_sandwich_forms(model, rows, D, odd):
+    """Few, a middle number and many rows of every width's form, aligned and not, in modulation
+    groups (which many rows take in segments) and with expert rows."""
+    sandwich_case(model, rows, D - odd, group=max(1, rows // 3 - 1), seed=rows + D)
+    sandwich_case(model, rows, D - odd, parts=2, post="layer", pre="rms", seed=rows - D, a_t=F32)
+
+
+def launches(model, kind):
+    return model.stats()[kind]["launches"]
+
+
+@pytest.mark.parametrize("T,E,k,H,act", [(500, 4, 2, 1600, "gelu"), (901, 4, 2, 800, "swiglu")])
+def test_moe_forward_copies_rows(model, T, E, k, H, act):
+    """Groups and experts so large that the layer's rows are copied to expert order first."""
+    before = launches(model, "small")
+    test_moe_forward(model, T, 256, H, E, k, act, 128)
+    assert launches(model, "small") == before + 1
+
+
+def test_copied_rows_back_to_back(model):
+    """Copies and products that follow one another without a wait reuse one scratch buffer: a
+    product starts beside the copy, the next copy behind the product."""
+    st = torch.cuda.Stream()
+    before = launches(model, "small")
+    try:
+        model.set_stream(st)
+        fb.fb_set_op_repeat(model.handle, 7)
+        with torch.cuda.stream(st):
+            experts_case(model, [900, 0, 700], 1600, 512, act="gelu", seed=50)
+            experts_case(model, [300, 450], 800, 512, act="swiglu", out_t=F32, seed=51)
+    finally:
+        fb.fb_set_op_repeat(model.handle, 1)
+        model.set_stream(None)
+    assert launches(model, "small") == before + 28
+
+
+def test_two_models_copy_rows_at_once():
+    import threading
+    failed = []
+
+    def work(seed):
+        try:
+            with fb.Model(synth.TINY, synth.make_weights(synth.TINY)) as m:
+                st = torch.cuda.Stream()
+                m.set_stream(st)
+                before = launches(m, "small")
+                with torch.cuda.stream(st):
+                    for i in range(6):
+                        experts_case(m, [500, 3, 700 + seed], 1600, 256, act="gelu", seed=seed + i)
+                assert launches(m, "small") == before + 12
+                m.set_stream(None)
+        except BaseException as e:  # noqa: BLE001
+            failed.append(e)
+    ts = [threading.Thread(target=work, args=(k,)) for k in (70, 90)]
+    for t in ts:
+        t.start()
+    for t in ts:
+        t.join()
+    assert not failed, failed
+
+
+@pytest.mark.parametrize("k", [4096, 8960])
+@pytest.mark.parametrize("sizes", [[4, 1], [20, 3], [200, 31]])
+@pytest.mark.parametrize("act", ["none", "swiglu"])
+def test_experts_fp32_sums_are_short(model, k, sizes, act):
+    """2-norm of the error of fp32 results. Four K blocks are 16 MMAs, the j-th of which cuts up to
+    one unit (half of one on average, 0.7 x 6e-8) off a running sum of sqrt(j / 16) of the part's:
+    16 x 2/3 x 4.3e-8 = 4.6e-7 of the part, and of the whole, as parts are independent. Up to 35
+    parts added in order round another 0.7 x 3.4e-8 sqrt(35) = 1.4e-7: together less than 6e-7
+    (one chain over K loses 6e-8 a K block: 3.8e-6 and 8.4e-6). The two factors of a gated result
+    carry that each, and 3e-7 by the activation: 1e-6."""
+    n = 512
+    nw = 2 * n if act == "swiglu" else n
+    a = torch.randn(sum(sizes), k, generator=gen(k), device="cuda").to(BF)
+    w = torch.empty(2, nw, k, dtype=BF, device="cuda").normal_(0, k ** -0.5, generator=gen(k + 1))
+    off = torch.tensor([0, sizes[0], sum(sizes)], dtype=torch.int32, device="cuda")
+    out = torch.zeros(sum(sizes), n, device="cuda")
+    model.op_expert_gemm(fb.make_experts(a, w, off, out, act=act))
+    want = torch.cat([act64(x.double() @ w[e].double().T, act, n)
+                      for e, x in enumerate((a[:sizes[0]], a[sizes[0]:]))])
+    err = ((out.double() - want).norm() / want.norm()).item()
+    assert err <= (6e-7 if act == "none" else 1e-6)
