@@ -926,3 +926,31 @@ def test_experts_fp32_sums_are_short(model, k, sizes, act):
                       for e, x in enumerate((a[:sizes[0]], a[sizes[0]:]))])
     err = ((out.double() - want).norm() / want.norm()).item()
     assert err <= (6e-7 if act == "none" else 1e-6)
+
+
+def test_experts_wait_runs_out_then_recovers(model):
+    """Tiles of 2048 K blocks, all at once, take their mainloop 0.67 ms, past a limit of a microsecond
+    on the epilogue's wait for it (whose clock is looked at every 64 polls, 0.3 ms): the call reports
+    it, and the next ones are as before."""
+    rows, n, k = 1024, 4864, 1 << 17
+    a = torch.randn(rows, k, generator=gen(80), device="cuda").to(BF)
+    w = torch.empty(1, n, k, dtype=BF, device="cuda").normal_(generator=gen(81))
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    out = torch.zeros(rows, n, dtype=BF, device="cuda")
+    args = fb.make_experts(a, w, off, out)
+    model.op_expert_gemm(args)
+    ref = out.clone()
+    torch.cuda.synchronize()
+    fb.fb_set_device_wait_limit(1000)
+    try:
+        with pytest.raises(fb.FlashBonError) as e:
+            model.op_expert_gemm(args)
+    finally:
+        fb.fb_set_device_wait_limit(0)
+    assert e.value.status == fb.FB_ECUDA and "device wait timed out" in str(e.value)
+    for _ in range(2):
+        out.zero_()
+        model.op_expert_gemm(args)
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref)
+    experts_case(model, [70, 3, 400], 512, 256, act="swiglu", seed=82)
