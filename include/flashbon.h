@@ -352,14 +352,17 @@ fb_status fb_op_attention(fb_model* m, const void* Q, int ldq, const void* K, in
  * (an engineering entry point: the paper's f_theta is a black box, and DiT variants whose
  * feed-forward is a mixture of experts, or whose blocks have a norm on both sides, need
  * these next to the calls above.) Inference only, like the rest of the library. The op
- * calls follow the single-op ones: DEVICE pointers, enqueued on the model's stream (on the
- * SMs of its budget), waited for. A matrix is row-major with a row stride in elements (ld*),
+ * calls follow the single-op ones: DEVICE pointers, enqueued on the model's stream, waited
+ * for. The products in tiles and the copy of their rows size their grids to the model's SM
+ * budget (fb_set_sm_budget); the other kernels launch a block for every so many rows, on
+ * whatever SMs the stream has. A matrix is row-major with a row stride in elements (ld*),
  * which may exceed its width; elements behind the width are neither read nor written.
  * Inputs and outputs do not overlap unless said so. fb_set_op_repeat applies. */
 enum { FB_BF16 = 0, FB_F32 = 1 };                              /* element types */
 enum { FB_NORM_NONE = 0, FB_NORM_RMS = 1, FB_NORM_LAYER = 2 }; /* norms over a row */
 /* Activations. The gated ones take 2 n weight rows, the n gate rows before the n up rows:
- * silu(gate) * up, gelu(gate) * up. GELU is the tanh form. */
+ * silu(gate) * up, gelu(gate) * up. GELU is the tanh form. Each is formed to a few units of
+ * fp32 (bf16 results: 2^-14) of its own value, also where that is small. */
 enum { FB_ACT_NONE = 0, FB_ACT_GELU = 1, FB_ACT_SWIGLU = 2, FB_ACT_GEGLU = 3 };
 
 /* fb_op_sandwich_norm: the norm behind a block, its gate, the scaled residual and the norm
