@@ -16,7 +16,9 @@ __global__ void __launch_bounds__(256) gemm_simt_kernel(const bf16* __restrict__
   __shared__ float Ws[TK][TN + 1];
   const int tid = threadIdx.x;
   const int ty = tid / 8, tx = tid % 8;  // rows ty, ty + 32; columns tx*8 .. tx*8+7
-  const int m0 = blockIdx.y * TM, n0 = blockIdx.x * TN;
+  // (all tiles on the grid's x, which holds 2^31; y would end at 65535 x 64 rows)
+  const int n_tiles = (N + TN - 1) / TN;
+  const int m0 = blockIdx.x / n_tiles * TM, n0 = blockIdx.x % n_tiles * TN;
   float acc[2][8] = {};
   for (int k0 = 0; k0 < K; k0 += TK) {
     for (int i = tid; i < TM * TK; i += 256) {
@@ -51,7 +53,9 @@ __global__ void __launch_bounds__(256) gemm_simt_kernel(const bf16* __restrict__
 
 cudaError_t gemm_simt(const GemmArgs& g, cudaStream_t st) {
   if (g.N % 8 != 0 || g.M < 1 || g.K < 1) return cudaErrorInvalidValue;
-  dim3 grid((g.N + TN - 1) / TN, (g.M + TM - 1) / TM);
+  const long long tiles = ((g.N + TN - 1LL) / TN) * ((g.M + TM - 1LL) / TM);
+  if (tiles > 0x7fffffffLL) return cudaErrorInvalidValue;
+  dim3 grid((unsigned)tiles);
   switch (g.kind) {
     case EPI_BF16:
       return launch_k(gemm_simt_kernel<EPI_BF16>, grid, dim3(256), 0, st, g.A, g.lda, g.W, g.ldw, g.M, g.N, g.K, g.epi);

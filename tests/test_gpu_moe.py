@@ -954,3 +954,32 @@ def test_experts_wait_runs_out_then_recovers(model):
         torch.cuda.synchronize()
         assert torch.equal(out, ref)
     experts_case(model, [70, 3, 400], 512, 256, act="swiglu", seed=82)
+
+
+def test_moe_forward_of_millions_of_rows(model):
+    """More rows than a grid's second dimension has tiles for, with a router weight that is not
+    padded: every row as in a call of few."""
+    T, D, H, E = 65535 * 64 + 70, 16, 16, 2
+    g = gen(90)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    router = torch.zeros(8, D, dtype=BF, device="cuda")
+    router[:E] = randn(E, D).to(BF)
+    moe = fb.make_moe(router, randn(E, H, D).to(BF), randn(E, D, H).to(BF), 1, renorm=True)
+    a, h = randn(T, D).to(BF), randn(T, D)
+    h_out, part = torch.zeros_like(h), torch.zeros(3000, D, device="cuda")
+    model.moe_forward(moe, a, fb.make_sandwich(h, h_out=h_out))
+    for r in (slice(0, 3000), slice(T - 3000, T)):
+        model.moe_forward(moe, a[r].contiguous(), fb.make_sandwich(h[r].contiguous(), h_out=part))
+        torch.cuda.synchronize()
+        assert torch.equal(h_out[r], part)
+    assert torch.all((h_out != h).any(1))
+
+
+def test_gemm_of_millions_of_rows(model):
+    M = 65535 * 64 + 70
+    A, W = torch.randn(M, 8, device="cuda").to(BF), torch.randn(8, 8, device="cuda").to(BF)
+    out = torch.zeros(M, 8, device="cuda")
+    fb.fb_op_gemm(model.handle, M, 8, 8, A, W, None, 2, out)
+    want = A.double() @ W.double().T
+    # (eight products and sums of fp32, each off by 2^-24 of at most the terms' sizes)
+    assert ((out.double() - want).abs() <= 16 * 2 ** -24 * (A.double().abs() @ W.double().abs().T)).all()
