@@ -66,6 +66,13 @@ static_assert(ring_bytes(false) % 128 == 0, "TMA tiles lie on 128-byte boundarie
 constexpr int64_t BAND_BYTES = 16ll << 20;
 constexpr int PART_BLOCKS = 4;          // K blocks of one accumulator, for fp32 results
 constexpr int F32_T = 128;              // widest tile then (its sums wait in registers)
+// bf16 results of a longer K take the fp32 results' way (F32 in the templates: sums in parts, a
+// thread's results straight to memory). One chain loses up to 6e-9 of the result per element of K
+// where all terms have one sign, and keeps the epilogue waiting for all of it: 2-norm of the error
+// of such bf16 results, one chain / parts (rounding alone 1.1e-3 to 1.8e-3), K = 65536 1.82e-3 /
+// 1.78e-3, 2^18 2.4e-3 / 1.73e-3, 2^20 6.2e-3 / 1.29e-3, 2^23 4.9e-2 / 4e-4.
+constexpr int LONG_K = 1 << 17;
+bool in_parts(const ExpertArgs& g) { return g.out_type == FB_F32 || g.k > LONG_K; }
 
 __host__ __device__ __forceinline__ int acc_cols_of(int T) { return (T + 31) / 32 * 32; }
 
@@ -110,6 +117,9 @@ __device__ __forceinline__ float silu_of(float x) {
   if (EXACT) return __fdividef(x, 1.f + expf(-x));
   return x * rcp_approx(1.f + ex2_approx(-LOG2E * x));
 }
+
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(bf16* p, float x) { *p = __float2bfloat16(x); }
 
 // ---- TMA --------------------------------------------------------------------------------
 __device__ __forceinline__ void tma_load_3d_cg2(uint32_t dst, const CUtensorMap* map, uint32_t bar,
@@ -516,21 +526,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<F32, GATHER>::
         if constexpr (F32) {
           // straight to memory, 32 or (gated, two tokens at once) 16 features of a token
           const int n = k.nv - t0;
-          float* at = reinterpret_cast<float*>(g.out) +
-                      (size_t)(k.r0 + t0 + (GATED ? lane >> 4 : 0)) * g.ldo + feature;
-          if (GATED) {
+          const size_t first_at = (size_t)(k.r0 + t0 + (GATED ? lane >> 4 : 0)) * g.ldo + feature;
+          auto store = [&](auto* at) {
+            if (GATED) {
 #pragma unroll
-            for (int j = 0; j < CH; j += 2, at += 2 * g.ldo) {
-              const float y = gated(v[j] + bias, v[j + 1] + bias);
-              if (j + (lane >> 4) < n && feature < g.n) *at = y;
-            }
-          } else {
+              for (int j = 0; j < CH; j += 2, at += 2 * g.ldo) {
+                const float y = gated(v[j] + bias, v[j + 1] + bias);
+                if (j + (lane >> 4) < n && feature < g.n) put(at, y);
+              }
+            } else {
 #pragma unroll
-            for (int j = 0; j < CH; ++j, at += g.ldo) {
-              const float x = v[j] + bias;
-              if (j < n && feature < g.n) *at = g.act == FB_ACT_GELU ? gelu_f<true>(x) : x;
+              for (int j = 0; j < CH; ++j, at += g.ldo) {
+                const float x = v[j] + bias;
+                if (j < n && feature < g.n) put(at, g.act == FB_ACT_GELU ? gelu_f<true>(x) : x);
+              }
             }
-          }
+          };
+          if (g.out_type == FB_F32)
+            store(reinterpret_cast<float*>(g.out) + first_at);
+          else
+            store(reinterpret_cast<bf16*>(g.out) + first_at);
           continue;
         }
         uint8_t* tile = tiles + buf * EPI_TILE;
@@ -757,10 +772,10 @@ __global__ void __launch_bounds__(FEW_THREADS, BLOCKS) expert_few_kernel(const E
       else if (g.act == FB_ACT_GELU)
         v = gelu_f<F32>(v);
       const size_t at = (size_t)(p0 + row) * g.ldo + f0 + f;
-      if (F32)
-        reinterpret_cast<float*>(g.out)[at] = v;
+      if (F32 && g.out_type == FB_F32)
+        put(reinterpret_cast<float*>(g.out) + at, v);
       else
-        reinterpret_cast<bf16*>(g.out)[at] = __float2bfloat16(v);
+        put(reinterpret_cast<bf16*>(g.out) + at, v);
     }
   }
 }
@@ -917,7 +932,7 @@ cudaError_t expert_gemm_set_wait_limit(unsigned long long ns) { return fb_set_wa
 // all others; copies by cp.async into the ring 2278: the issuer then needs a proxy fence per K
 // block, which waits for the SM's copies in flight.)
 size_t expert_gemm_ws_bytes(const ExpertArgs& g) {
-  const bool f32 = g.out_type == FB_F32;
+  const bool f32 = in_parts(g);
   const long long most = f32 ? 96 : 192;  // rows a group, on average
   const int nw = g.act >= FB_ACT_SWIGLU ? 2 * g.n : g.n;
   const bool copy = g.index && nw > (f32 ? 512 : 1536) && g.max_rows > most * g.experts;
@@ -944,7 +959,7 @@ cudaError_t expert_copy_rows(ExpertArgs* g, bf16* ws, int* err, int num_sms, cud
 cudaError_t expert_gemm(const ExpertArgs& g, int* err, int num_sms, cudaStream_t st) {
   if (g.max_rows == 0) return cudaSuccess;
   if (num_sms < 2) return cudaErrorInvalidValue;
-  const bool f32 = g.out_type == FB_F32;
+  const bool f32 = in_parts(g);
   if (g.act >= FB_ACT_SWIGLU)
     return f32 ? choose<true, true>(g, err, num_sms, st) : choose<true, false>(g, err, num_sms, st);
   return f32 ? choose<false, true>(g, err, num_sms, st) : choose<false, false>(g, err, num_sms, st);

@@ -983,3 +983,24 @@ def test_gemm_of_millions_of_rows(model):
     want = A.double() @ W.double().T
     # (eight products and sums of fp32, each off by 2^-24 of at most the terms' sizes)
     assert ((out.double() - want).abs() <= 16 * 2 ** -24 * (A.double().abs() @ W.double().abs().T)).all()
+
+
+@pytest.mark.parametrize("k", [(1 << 20) + 40, 1 << 21])
+@pytest.mark.parametrize("rows", [8, 40])
+@pytest.mark.parametrize("act", ["none", "swiglu"])
+def test_experts_very_long_sums_bf16(model, k, rows, act):
+    """bf16 results of a K so long that one chain of the tensor core loses more than their rounding,
+    6e-9 of the result per element where all terms have one sign. Sums in parts: 16 cuts of up to
+    2^-23 in each, and the parts (at most k / 192, in the streamed form) added in order, half of
+    2^-24 each."""
+    g = gen(k + rows)
+    a = torch.randn(rows, k, generator=g, device="cuda").abs().to(BF)
+    w = torch.empty(1, 32, k, dtype=BF, device="cuda").normal_(generator=g).abs_()
+    n = 16 if act == "swiglu" else 32
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    out = torch.zeros(rows, n, dtype=BF, device="cuda")
+    model.op_expert_gemm(fb.make_experts(a, w, off, out, act=act))
+    v = sum(a[:, i:i + (1 << 19)].double() @ w[0, :, i:i + (1 << 19)].double().T
+            for i in range(0, k, 1 << 19))
+    want = act64(v, act, n)
+    check(out, want, (2 if act == "swiglu" else 1) * (16 * 2 ** -23 + k / 192 * 2 ** -25) * want, BF)
