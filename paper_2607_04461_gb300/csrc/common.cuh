@@ -135,8 +135,8 @@ __device__ __forceinline__ float tanh_approx(float x) {
 }
 // GELU, tanh form: 0.5 x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))), evaluated as
 // h + h tanh(x (k0 + k1 x^2)) with h = x / 2 (five fp32 operations and one tanh). The
-// hardware tanh (max relative error about 2^-11) is well inside the bf16 rounding of the
-// GEMM output that it feeds.
+// hardware tanh (max relative error about 2^-11) is inside the bf16 rounding of results at
+// x > -1; below, where the two terms cancel, the result is off by up to |x| 2^-12.
 __device__ __forceinline__ float gelu_tanh_f(float x) {
   const float k0 = 0.7978845608028654f;              // sqrt(2/pi)
   const float k1 = 0.7978845608028654f * 0.044715f;  // sqrt(2/pi) * 0.044715

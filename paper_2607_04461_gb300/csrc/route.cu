@@ -13,9 +13,10 @@
 //    counts through distributed shared memory (one block up to 32 tokens);
 //  * more tokens take three launches: choice and counts by blocks of up to 128 tokens, the
 //    blocks' counts added up expert by expert, and the pairs put in their places.
-// One token over 8 experts 2.5 us, 1560 5.9, 49920 over 64 (top 8) 26: bound by the latency of the
-// chains and launches up to a few thousand tokens, then by the choice's instructions (46 % of the
-// issue slots in its kernel); the 19 MB that the last one moves would take 2.8.
+// One token over 8 experts 2.7 us, 1560 5.9, 49920 over 64 (top 8) 26: bound by the latency of the
+// chains and launches up to a few thousand tokens, then by the choice, 390 blocks in two rounds of
+// 304 (46 registers: two an SM) at 46 % of the issue slots, and the two launches behind it; the
+// 19 MB that the last one moves would take 2.8.
 #include <float.h>
 
 #include "kernels.h"
