@@ -281,6 +281,8 @@ enum {
   FB_K_SANDWICH,      /* norms around a block, gate, scaled residual, expert combination */
   FB_K_ROUTE,         /* router: top-k experts, rows sorted by expert */
   FB_K_EXPERT,        /* products grouped by expert */
+  FB_K_CROSS,         /* attention to encoder states of any length (fb_op_cross_attention) */
+  FB_K_ADAPTER,       /* projections with low-rank adapters, with their low-rank parts */
   FB_K_COUNT,
   FB_K_BASE_COUNT = FB_K_SANDWICH /* the kinds that fb_get_stats copies, in every version */
 };
@@ -486,6 +488,90 @@ typedef struct fb_moe {
 } fb_moe;
 fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const uint8_t* valid,
                          const fb_sandwich* s);
+
+/* ---- several requests in one batch ------------------------------------------------------
+ * (engineering entry points: the paper drafts the candidates of one prompt at a time. A pool
+ * that serves several requests has a prompt of its own length and an adapter of its own for
+ * each.) Inference only. The op calls follow the ones above: DEVICE pointers of the model's
+ * device, enqueued on the model's stream, waited for; grids are sized to the model's SM budget;
+ * a matrix is row-major with a row stride in elements, elements behind its width are neither
+ * read nor written; inputs and outputs do not overlap unless said so; fb_set_op_repeat applies.
+ *
+ * fb_op_cross_attention: attention to encoder states of another length. Sequence s has the query
+ * rows q_offsets[s] .. q_offsets[s + 1] - 1 and attends to the keys and values kv_offsets[u] ..
+ * kv_offsets[u + 1] - 1 of states u = kv_of[s] (kv_of NULL: u = s), which other sequences may
+ * share. With G = heads / kv_heads, for each of its rows r and heads h:
+ *   out[r][h] = sum_j w_j v[j][h / G],  w = softmax over j of scale * q[r][h] . k[j][h / G]
+ * over the keys j of u with valid[j] != 0 (valid NULL: all of them). What keys and values with
+ * valid[j] = 0 hold, NaN and infinities too, has no influence. Where no key is left, out[r] is
+ * zero. q and out: bf16 [q_rows][heads * head_dim], k and v: bf16 [kv_rows][kv_heads * head_dim],
+ * head_dim 64 or 128, valid: [kv_rows], scale finite and positive (0: 1 / sqrt(head_dim)). Scores,
+ * maxima and sums are fp32; a key's weight is rounded to bf16 for its product with v, the result
+ * once as it is stored. q_offsets [seqs + 1], kv_offsets [states + 1] (each rising from 0 to at
+ * most q_rows or kv_rows) and kv_of [seqs] are read on the device; rows of no sequence are not
+ * written. Row strides are multiples of 8, q, k, v and out 16-byte aligned. FB_EINVAL for other
+ * sizes, seqs outside [0, FB_CROSS_MAX_SEQS], states < 0 or below seqs without kv_of, heads not a
+ * multiple of kv_heads, G past FB_CROSS_MAX_GROUP, rows outside [0, FB_CROSS_MAX_ROWS], or, found
+ * on the device, offsets that are not as above or a kv_of outside [0, states) (the outputs are
+ * then not usable). The scratch for the parts of long states is the model's and grows on demand
+ * (FB_ENOMEM). */
+#define FB_CROSS_MAX_SEQS 4096
+#define FB_CROSS_MAX_GROUP 128
+#define FB_CROSS_MAX_HEADS 4096
+#define FB_CROSS_MAX_ROWS (1 << 26)
+typedef struct fb_cross {
+  int seqs, states, heads, kv_heads, head_dim, q_rows, kv_rows;
+  const void* q;
+  int64_t ldq;
+  const void* k;
+  int64_t ldk;
+  const void* v;
+  int64_t ldv;
+  const int32_t *q_offsets, *kv_offsets, *kv_of;
+  const uint8_t* valid;
+  float scale;
+  void* out;
+  int64_t ldo;
+} fb_cross;
+fb_status fb_op_cross_attention(fb_model* m, const fb_cross* c);
+
+/* fb_op_adapter_gemm: a projection shared by all rows, with a low-rank adapter for each segment of
+ * them. Rows offsets[i] .. offsets[i + 1] - 1 of x are segment i, e = adapter[i] its adapter (-1:
+ * none; segments may share one):
+ *   y   = x w^T + bias + scale[e] * (x a_e^T) b_e^T
+ *   out = act(y), or with resid or gate:  resid + gate * act(y)   (NULL: 0 and 1)
+ * x: bf16 [rows][k], w: bf16 [n][k], a: bf16 [adapters][rank][k], b: bf16 [adapters][n][rank],
+ * bias and gate: fp32 [n] or NULL, scale: fp32 [adapters] or NULL (1), act FB_ACT_NONE or
+ * FB_ACT_GELU, out bf16, or fp32 (which resid and gate need), resid: fp32 [rows][n], may be out
+ * (same stride). Adapters of a smaller rank are padded with zeros. Sums are fp32, rounded once as
+ * they are stored; x a_e^T passes through the tensor cores as a sum of bf16 values, two of them
+ * for bf16 results and three for fp32 ones. offsets [segments + 1] (rising from 0 to at most rows)
+ * and adapter [segments] are read on the device; rows from offsets[segments] on are not written.
+ * n, k, rank and the row strides are multiples of 8; x, w, a, b and out are 16-byte aligned.
+ * FB_EINVAL for other sizes, segments outside [0, FB_ADAPTER_MAX_SEGMENTS], adapters < 1, rank past
+ * FB_ADAPTER_MAX_RANK, rows outside [0, FB_ADAPTER_MAX_ROWS], n or k past FB_EXPERT_MAX_SIZE, or,
+ * found on the device, offsets that are not as above or an adapter outside [-1, adapters) (the
+ * outputs are then not usable). The scratch for the low-rank part is the model's and grows on
+ * demand (FB_ENOMEM). */
+#define FB_ADAPTER_MAX_SEGMENTS 1024
+#define FB_ADAPTER_MAX_RANK 256
+#define FB_ADAPTER_MAX_ROWS (1 << 26)
+typedef struct fb_adapters {
+  int rows, n, k, rank, adapters, segments;
+  const void* x;
+  int64_t ldx;
+  const void *w, *a, *b;
+  const float *bias, *scale;
+  const int32_t *offsets, *adapter;
+  int act;
+  const float* resid;
+  int64_t ldr;
+  const float* gate;
+  void* out;
+  int out_type;
+  int64_t ldo;
+} fb_adapters;
+fb_status fb_op_adapter_gemm(fb_model* m, const fb_adapters* g);
 
 /* ---- allocation-free stream-K GEMM (an engineering entry point: the paper has no
  * counterpart; it computes what fb_op_gemm with impl 4 computes) ---------------------

@@ -11,6 +11,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -205,7 +206,7 @@ struct fb_model {
   // launches; reset after a device error)
   float* attn_ws = nullptr;
   int* attn_flags = nullptr;
-  // scratch of fb_op_expert_gemm and fb_moe_forward, grown on demand
+  // scratch of the mixture-of-experts calls and of the ones for several requests, grown on demand
   uint8_t* moe_ws = nullptr;
   size_t moe_bytes = 0;
   // statistics
@@ -526,6 +527,95 @@ fb_status expert_args(const fb_experts& g, ExpertArgs* out) {
   if (g.max_rows > 0 && g.a_rows < 1) return fail(FB_EINVAL, "a is empty");
   *out = {g.experts, g.n, g.k, g.max_rows, g.a_rows, (const bf16*)g.a, g.lda, g.index, g.offsets,
           (const bf16*)g.w, g.bias, g.act, g.out, g.out_type, g.ldo};
+  return FB_OK;
+}
+
+// ---- several requests in one batch ------------------------------------------------------
+// The model's device for the time of a call, whatever the calling thread's current one is.
+struct DeviceScope {
+  int before = -1;
+  explicit DeviceScope(int dev) {
+    if (cudaGetDevice(&before) != cudaSuccess || before == dev || cudaSetDevice(dev) != cudaSuccess)
+      before = -1;
+  }
+  ~DeviceScope() {
+    if (before >= 0) cudaSetDevice(before);
+  }
+};
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+fb_status cross_args(const fb_cross& c, CrossArgs* out) {
+  if (c.seqs < 0 || c.seqs > FB_CROSS_MAX_SEQS || c.states < 0 || (!c.kv_of && c.states < c.seqs))
+    return fail(FB_EINVAL, "seqs=%d must be in [0, %d], states=%d at least seqs without kv_of",
+                c.seqs, FB_CROSS_MAX_SEQS, c.states);
+  if (c.heads < 1 || c.heads > FB_CROSS_MAX_HEADS || c.kv_heads < 1 || c.heads % c.kv_heads ||
+      c.heads / c.kv_heads > FB_CROSS_MAX_GROUP)
+    return fail(FB_EINVAL, "heads=%d must be in [1, %d] and 1 to %d times kv_heads=%d", c.heads,
+                FB_CROSS_MAX_HEADS, FB_CROSS_MAX_GROUP, c.kv_heads);
+  if (c.head_dim != 64 && c.head_dim != 128)
+    return fail(FB_EINVAL, "head_dim=%d must be 64 or 128", c.head_dim);
+  if (c.q_rows < 0 || c.q_rows > FB_CROSS_MAX_ROWS || c.kv_rows < 0 || c.kv_rows > FB_CROSS_MAX_ROWS)
+    return fail(FB_EINVAL, "q_rows=%d kv_rows=%d outside [0, %d]", c.q_rows, c.kv_rows,
+                FB_CROSS_MAX_ROWS);
+  if (!(c.scale >= 0.f) || c.scale > FLT_MAX) return fail(FB_EINVAL, "scale must be finite and positive");
+  if (!c.q_offsets || !c.kv_offsets || (c.q_rows > 0 && (!c.q || !c.out)) ||
+      (c.kv_rows > 0 && (!c.k || !c.v)))
+    return fail(FB_EINVAL, "null argument");
+  const int64_t wq = (int64_t)c.heads * c.head_dim, wk = (int64_t)c.kv_heads * c.head_dim;
+  if (c.ldq < wq || c.ldo < wq || c.ldk < wk || c.ldv < wk || c.ldq % 8 || c.ldo % 8 || c.ldk % 8 ||
+      c.ldv % 8)
+    return fail(FB_EINVAL, "row strides must be multiples of 8, at least the heads' width");
+  for (const void* p : {c.q, c.k, c.v, (const void*)c.out})
+    if (!aligned16(p)) return fail(FB_EINVAL, "16-byte alignment required");
+  static_cast<fb_cross&>(*out) = c;
+  if (c.scale == 0.f) out->scale = 1.f / sqrtf((float)c.head_dim);
+  return FB_OK;
+}
+
+// (the work of rows whose sequences all attend to the mean number of keys)
+fb_status run_cross(fb_model* m, const CrossArgs& c) {
+  const double wq = (double)c.heads * c.head_dim, wk = (double)c.kv_heads * c.head_dim;
+  const double keys = c.states ? (double)c.kv_rows / c.states : 0;
+  KTimer t(m, FB_K_CROSS, 4.0 * wq * c.q_rows * keys, 4.0 * (wq * c.q_rows + wk * c.kv_rows));
+  CK(cross_attention(c, m->derr, m->num_sms, m->st));
+  return FB_OK;
+}
+
+fb_status adapter_args(const fb_adapters& g, AdapterArgs* out) {
+  if (g.segments < 0 || g.segments > FB_ADAPTER_MAX_SEGMENTS || g.adapters < 1)
+    return fail(FB_EINVAL, "segments=%d must be in [0, %d], adapters=%d at least 1", g.segments,
+                FB_ADAPTER_MAX_SEGMENTS, g.adapters);
+  if (g.rows < 0 || g.rows > FB_ADAPTER_MAX_ROWS)
+    return fail(FB_EINVAL, "rows=%d outside [0, %d]", g.rows, FB_ADAPTER_MAX_ROWS);
+  if (g.n < 1 || g.k < 1 || g.rank < 1 || g.n % 8 || g.k % 8 || g.rank % 8 ||
+      g.rank > FB_ADAPTER_MAX_RANK || g.n > FB_EXPERT_MAX_SIZE || g.k > FB_EXPERT_MAX_SIZE)
+    return fail(FB_EINVAL, "n=%d k=%d (at most %d) and rank=%d (at most %d) must be multiples of 8",
+                g.n, g.k, FB_EXPERT_MAX_SIZE, g.rank, FB_ADAPTER_MAX_RANK);
+  if (g.act != FB_ACT_NONE && g.act != FB_ACT_GELU)
+    return fail(FB_EINVAL, "act=%d must be FB_ACT_NONE or FB_ACT_GELU", g.act);
+  if (!known_type(g.out_type)) return fail(FB_EINVAL, "out must be FB_BF16 or FB_F32");
+  if ((g.resid || g.gate) && g.out_type != FB_F32)
+    return fail(FB_EINVAL, "resid and gate need an fp32 out");
+  if (!g.offsets || (g.segments > 0 && !g.adapter) ||
+      (g.rows > 0 && (!g.x || !g.w || !g.a || !g.b || !g.out)))
+    return fail(FB_EINVAL, "null argument");
+  if (g.ldx < g.k || g.ldo < g.n || g.ldx % 8 || g.ldo % 8 || (g.resid && (g.ldr < g.n || g.ldr % 8)))
+    return fail(FB_EINVAL, "row strides must be multiples of 8, at least k and n");
+  for (const void* p : {g.x, g.w, g.a, g.b, (const void*)g.out, (const void*)g.resid})
+    if (!aligned16(p)) return fail(FB_EINVAL, "16-byte alignment required");
+  static_cast<fb_adapters&>(*out) = g;
+  return FB_OK;
+}
+
+// (the work of rows that all have an adapter, every one of them in use)
+fb_status run_adapters(fb_model* m, const AdapterArgs& g, uint8_t* ws) {
+  const double r = g.rows, n = g.n, k = g.k;
+  KTimer t(m, FB_K_ADAPTER, 2.0 * r * (n * k + g.rank * (n + k)),
+           2.0 * (r * k + n * k + (double)g.adapters * g.rank * (n + k)) +
+               r * n * (type_bytes(g.out_type) + (g.resid ? 4 : 0)),
+           adapter_launches(g));
+  CK(adapter_gemm(g, ws, m->derr, m->num_sms, m->st));
   return FB_OK;
 }
 
@@ -1696,7 +1786,8 @@ fb_status fb_reset_stats(fb_model* m) {
 const char* fb_kernel_name(int kind) {
   static const char* names[FB_K_COUNT] = {"gemm_tc", "gemm_simt", "attn_self", "attn_cross",
                                           "ln_mod", "qk_norm_rope", "proxy_add", "patch_embed",
-                                          "head_euler", "small", "sandwich_norm", "route", "expert_gemm"};
+                                          "head_euler", "small", "sandwich_norm", "route", "expert_gemm",
+                                          "cross_attention", "adapter_gemm"};
   return (kind >= 0 && kind < FB_K_COUNT) ? names[kind] : "?";
 }
 
@@ -1855,6 +1946,29 @@ fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const ui
   CKS(run_experts(m, gu, ws + o_rows));
   CKS(run_experts(m, gd, nullptr));  // (no index, no copy)
   CKS(run_sandwich(m, s));
+  return end_call(m);
+}
+
+fb_status fb_op_cross_attention(fb_model* m, const fb_cross* c) {
+  if (!m || !c) return fail(FB_EINVAL, "null argument");
+  CrossArgs a;
+  CKS(cross_args(*c, &a));
+  if (a.q_rows == 0 || a.seqs == 0) return FB_OK;
+  const DeviceScope on(m->dev);
+  CKS(begin_call(m));
+  for (int r = 0; r < m->op_repeat; ++r) CKS(run_cross(m, a));
+  return end_call(m);
+}
+
+fb_status fb_op_adapter_gemm(fb_model* m, const fb_adapters* g) {
+  if (!m || !g) return fail(FB_EINVAL, "null argument");
+  AdapterArgs a;
+  CKS(adapter_args(*g, &a));
+  if (a.rows == 0 || a.segments == 0) return FB_OK;
+  const DeviceScope on(m->dev);
+  CKS(begin_call(m));
+  CKS(ensure_moe(m, adapter_ws_bytes(a)));
+  for (int r = 0; r < m->op_repeat; ++r) CKS(run_adapters(m, a, m->moe_ws));
   return end_call(m);
 }
 

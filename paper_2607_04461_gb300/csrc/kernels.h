@@ -171,6 +171,15 @@ cudaError_t expert_gemm(const ExpertArgs& g, int* err, int num_sms, cudaStream_t
 // Sets the expert_gemm unit's device wait limit on the current device (ns).
 cudaError_t expert_gemm_set_wait_limit(unsigned long long ns);
 
+// ---- several requests in one batch (flashbon.h has the definitions) ---------------------
+struct CrossArgs : fb_cross {};  // scale filled in
+cudaError_t cross_attention(const CrossArgs& c, int* err, int num_sms, cudaStream_t st);
+struct AdapterArgs : fb_adapters {};
+// ws: adapter_ws_bytes of scratch
+size_t adapter_ws_bytes(const AdapterArgs& g);
+int adapter_launches(const AdapterArgs& g);
+cudaError_t adapter_gemm(const AdapterArgs& g, void* ws, int* err, int num_sms, cudaStream_t st);
+
 // ---- measurement probe ----------------------------------------------------------------
 // One CTA per entry of `grid`, each timing (SM clock cycles, cycles[cta]) `reps` tcgen05.mma
 // kind::f16 instructions of M = 128, K = 16 and width N (64, 128 or 256) issued by each of

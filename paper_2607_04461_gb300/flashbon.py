@@ -22,7 +22,7 @@ LIB_PATH = os.path.join(_HERE, "libflashbon.so")
 FB_OK, FB_EINVAL, FB_ENOMEM, FB_ECUDA, FB_EPLAN, FB_ESTATE = range(6)
 KERNEL_KINDS = ["gemm_tc", "gemm_simt", "attn_self", "attn_cross", "ln_mod", "qk_norm_rope",
                 "proxy_add", "patch_embed", "head_euler", "small", "sandwich_norm", "route",
-                "expert_gemm"]
+                "expert_gemm", "cross_attention", "adapter_gemm"]
 K = {name: i for i, name in enumerate(KERNEL_KINDS)}
 
 
@@ -89,6 +89,25 @@ class fb_moe(ctypes.Structure):
         (n, ctypes.c_void_p) for n in ("router_w", "w1", "w2", "b1", "b2")]
 
 
+class fb_cross(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("seqs", "states", "heads", "kv_heads", "head_dim",
+                                            "q_rows", "kv_rows")] + [
+        ("q", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("k", ctypes.c_void_p),
+        ("ldk", ctypes.c_int64), ("v", ctypes.c_void_p), ("ldv", ctypes.c_int64),
+        ("q_offsets", ctypes.c_void_p), ("kv_offsets", ctypes.c_void_p),
+        ("kv_of", ctypes.c_void_p), ("valid", ctypes.c_void_p), ("scale", ctypes.c_float),
+        ("out", ctypes.c_void_p), ("ldo", ctypes.c_int64)]
+
+
+class fb_adapters(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "n", "k", "rank", "adapters", "segments")] + [
+        ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64)] + [
+        (n, ctypes.c_void_p) for n in ("w", "a", "b", "bias", "scale", "offsets", "adapter")] + [
+        ("act", ctypes.c_int), ("resid", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+        ("gate", ctypes.c_void_p), ("out", ctypes.c_void_p), ("out_type", ctypes.c_int),
+        ("ldo", ctypes.c_int64)]
+
+
 FB_BF16, FB_F32 = 0, 1
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 ACTS = {"none": 0, "gelu": 1, "swiglu": 2, "geglu": 3}
@@ -105,7 +124,7 @@ EXPORTS = ["fb_weights_count", "fb_weights_entry", "fb_init_model", "fb_free", "
            "fb_test_request_handover", "fb_test_attention_split", "fb_test_plan_traffic",
            "fb_probe_mma_rate", "fb_probe_mma_gap", "fb_probe_mufu", "fb_probe_tmem_load",
            "fb_probe_mma_mix", "fb_op_sandwich_norm", "fb_op_route", "fb_op_expert_gemm",
-           "fb_moe_forward"]
+           "fb_moe_forward", "fb_op_cross_attention", "fb_op_adapter_gemm"]
 
 PAIR_VERIFIER = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
                                  ctypes.POINTER(ctypes.c_int))
@@ -169,6 +188,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "fb_op_route": (I, [P, ctypes.POINTER(fb_route)]),
         "fb_op_expert_gemm": (I, [P, ctypes.POINTER(fb_experts)]),
         "fb_moe_forward": (I, [P, ctypes.POINTER(fb_moe), P, P, ctypes.POINTER(fb_sandwich)]),
+        "fb_op_cross_attention": (I, [P, ctypes.POINTER(fb_cross)]),
+        "fb_op_adapter_gemm": (I, [P, ctypes.POINTER(fb_adapters)]),
         "fb_probe_mma_rate": (I, [I, I, I, ctypes.POINTER(ctypes.c_double)]),
         "fb_probe_mma_gap": (I, [I, ctypes.POINTER(ctypes.c_double)]),
         "fb_probe_mufu": (I, [I, ctypes.POINTER(ctypes.c_double)]),
@@ -715,6 +736,78 @@ def fb_moe_forward(model: int, moe: fb_moe, a, sandwich: fb_sandwich, valid=None
         _tensor("valid", valid, ("uint8",), (sandwich.rows,)), ctypes.byref(sandwich)))
 
 
+# ---- several requests in one batch --------------------------------------------------------
+
+def _one_device(**tensors):
+    """All tensors lie on one device (the library reads them on the model's)."""
+    found = {name: x.device.index for name, x in tensors.items() if x is not None}
+    if len(set(found.values())) > 1:
+        raise ValueError(f"tensors on several devices: {found}")
+
+
+def make_cross(q, k, v, out, q_offsets, kv_offsets, head_dim=128, kv_of=None, valid=None, scale=0.0):
+    """fb_cross for fb_op_cross_attention. q and out [q_rows][heads * head_dim], k and v
+    [kv_rows][kv_heads * head_dim] bf16 (k and v may be columns of one buffer); q_offsets [seqs + 1],
+    kv_offsets [states + 1] and kv_of [seqs] (None: sequence s attends to states s) int32; valid
+    [kv_rows] uint8, 0 where a key is padding, or None; scale 0: 1 / sqrt(head_dim)."""
+    if q.dim() != 2 or k.dim() != 2 or q.shape[1] % head_dim or k.shape[1] % head_dim:
+        raise ValueError(f"q and k: rows of whole heads of {head_dim}")
+    wq, wk = q.shape[1], k.shape[1]
+    c = fb_cross(seqs=q_offsets.shape[0] - 1, states=kv_offsets.shape[0] - 1, heads=wq // head_dim,
+                 kv_heads=wk // head_dim, head_dim=head_dim, q_rows=q.shape[0], kv_rows=k.shape[0],
+                 scale=scale)
+    bf16 = ("bfloat16",)
+    c.q, c.ldq = _tensor("q", q, bf16, (None, wq), True), _row_stride(q)
+    c.k, c.ldk = _tensor("k", k, bf16, (None, wk), True), _row_stride(k)
+    c.v, c.ldv = _tensor("v", v, bf16, (k.shape[0], wk), True), _row_stride(v)
+    c.out, c.ldo = _tensor("out", out, bf16, (q.shape[0], wq), True), _row_stride(out)
+    c.q_offsets = _tensor("q_offsets", q_offsets, ("int32",), (None,))
+    c.kv_offsets = _tensor("kv_offsets", kv_offsets, ("int32",), (None,))
+    c.kv_of = _tensor("kv_of", kv_of, ("int32",), (c.seqs,))
+    c.valid = _tensor("valid", valid, ("uint8",), (k.shape[0],))
+    _one_device(q=q, k=k, v=v, out=out, q_offsets=q_offsets, kv_offsets=kv_offsets, kv_of=kv_of,
+                valid=valid)
+    c._keep = (q, k, v, out, q_offsets, kv_offsets, kv_of, valid)
+    return c
+
+
+def make_adapters(x, w, a, b, offsets, adapter, out, scale=None, bias=None, act="none", resid=None,
+                  gate=None):
+    """fb_adapters for fb_op_adapter_gemm. x [rows][k], w [n][k], a [adapters][rank][k], b
+    [adapters][n][rank] bf16; offsets [segments + 1] and adapter [segments] (-1: none) int32; scale
+    [adapters], bias and gate [n], resid [rows][n] fp32 or None; out [rows][n] bf16 or fp32 (may be
+    resid); act "none" or "gelu"."""
+    rows, (n, k), (adapters, rank) = x.shape[0], w.shape, a.shape[:2]
+    g = fb_adapters(rows=rows, n=n, k=k, rank=rank, adapters=adapters, segments=offsets.shape[0] - 1,
+                    act=ACTS[act])
+    bf16, f32 = ("bfloat16",), ("float32",)
+    g.x, g.ldx = _tensor("x", x, bf16, (None, k), True), _row_stride(x)
+    g.w = _tensor("w", w, bf16, (n, k))
+    g.a = _tensor("a", a, bf16, (adapters, rank, k))
+    g.b = _tensor("b", b, bf16, (adapters, n, rank))
+    g.scale = _tensor("scale", scale, f32, (adapters,))
+    g.bias = _tensor("bias", bias, f32, (n,))
+    g.gate = _tensor("gate", gate, f32, (n,))
+    g.offsets = _tensor("offsets", offsets, ("int32",), (None,))
+    g.adapter = _tensor("adapter", adapter, ("int32",), (g.segments,))
+    if resid is not None:
+        g.resid, g.ldr = _tensor("resid", resid, f32, (rows, n), True), _row_stride(resid)
+    g.out, g.out_type = _tensor("out", out, _FLOATS, (rows, n), True), _type(out)
+    g.ldo = _row_stride(out)
+    _one_device(x=x, w=w, a=a, b=b, scale=scale, bias=bias, gate=gate, offsets=offsets,
+                adapter=adapter, resid=resid, out=out)
+    g._keep = (x, w, a, b, offsets, adapter, out, scale, bias, resid, gate)
+    return g
+
+
+def fb_op_cross_attention(model: int, args: fb_cross) -> None:
+    _check(load_library().fb_op_cross_attention(model, ctypes.byref(args)))
+
+
+def fb_op_adapter_gemm(model: int, args: fb_adapters) -> None:
+    _check(load_library().fb_op_adapter_gemm(model, ctypes.byref(args)))
+
+
 class Model:
     """Owns an fb_model handle; methods forward to the fb_* functions."""
 
@@ -785,6 +878,12 @@ class Model:
 
     def moe_forward(self, moe, a, sandwich, valid=None):
         fb_moe_forward(self.handle, moe, a, sandwich, valid)
+
+    def op_cross_attention(self, args):
+        fb_op_cross_attention(self.handle, args)
+
+    def op_adapter_gemm(self, args):
+        fb_op_adapter_gemm(self.handle, args)
 
     def set_timing(self, mask):
         fb_set_timing(self.handle, mask)

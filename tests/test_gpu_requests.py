@@ -1,0 +1,463 @@
+"""The operators for several requests in one batch, through the public calls, against their
+definitions in float64.
+
+Tolerances, from the arithmetic (A = sum_j w_j |v_j|, the size of an attention result's terms):
+  * cross attention: a key's weight and the result are rounded to bf16, 2^-8 of the term each:
+    2^-8 (A + |o|). A score's fp32 sum may lose one unit, 1.2e-7 of its terms' sum, per 16 of
+    head_dim; with the rounding of the exponent's argument (2^-24 of at most |scale s| + |m|) and
+    the hardware exponential (2^-22) that is an absolute error d of the exponent, and 2 d A of the
+    result (numerator and sum).
+  * adapters: a product's fp32 sum may lose one unit, 1.2e-7 of its terms' sum, per 16 of K, and as
+    much for each other operation on the way (bias, scale, the two sums' sum, activation: 16 of
+    them at most). t = x A^T is a sum of two (fp32 results: three) bf16 values: 2^-16 (2^-24) of
+    t, times |B|. bf16 results: 2^-8 of the value more. GELU's slope is at most 1.13, and its
+    own error 2^-14 of the value for bf16 results.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2607_04461_gb300 import flashbon as fb
+from paper_2607_04461_gb300 import synth
+
+pytestmark = pytest.mark.gpu
+
+BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+NAN = float("nan")
+
+
+@pytest.fixture(scope="module")
+def model():
+    m = fb.Model(synth.TINY, synth.make_weights(synth.TINY))
+    yield m
+    m.close()
+
+
+def gen(seed):
+    return torch.Generator("cuda").manual_seed(seed)
+
+
+def whole(x):
+    return torch.tensor(x, dtype=I32, device="cuda")
+
+
+def offsets(lengths):
+    at = [0]
+    for n in lengths:
+        at.append(at[-1] + n)
+    return at
+
+
+def padded(x, pad, fill=NAN):
+    if not pad:
+        return x
+    wide = torch.full((x.shape[0], x.shape[1] + pad), fill, dtype=x.dtype, device="cuda")
+    wide[:, :x.shape[1]] = x
+    return wide[:, :x.shape[1]]
+
+
+# ---- cross attention ------------------------------------------------------------------
+
+class Cross:
+    """Inputs, the result in float64 and its tolerance."""
+
+    def __init__(self, queries, keys, heads=2, kv_heads=None, D=128, kv_of=None, valid=None, pad=0,
+                 seed=0, scale=0.0, spread=1.0, extra_rows=3, packed=True):
+        g = gen(seed)
+        kv_heads = kv_heads or heads
+        self.heads, self.kv_heads, self.D, self.scale = heads, kv_heads, D, scale
+        self.q_at, self.k_at = offsets(queries), offsets(keys)
+        self.of = list(range(len(queries))) if kv_of is None else list(kv_of)
+        rows, kv_rows = self.q_at[-1] + extra_rows, self.k_at[-1] + extra_rows
+        randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+        self.q = padded((spread * randn(rows, heads * D)).to(BF), pad)
+        kv = (randn(kv_rows, 2 * kv_heads * D)).to(BF)
+        kv[self.k_at[-1]:] = NAN  # rows of no states
+        self.valid = None
+        if valid is not None:
+            self.valid = (valid if torch.is_tensor(valid) else
+                          (torch.rand(kv_rows, generator=g, device="cuda") >= valid)).to(torch.uint8).cuda()
+            masked = self.valid == 0
+            kv[masked] = torch.where(torch.rand(kv[masked].shape, generator=g, device="cuda") < 0.5,
+                                     NAN, math.inf).to(BF)
+        if packed:
+            kv = padded(kv, pad)
+            self.k, self.v = kv[:, :kv_heads * D], kv[:, kv_heads * D:]
+        else:
+            self.k, self.v = (padded(x.contiguous(), pad) for x in kv.chunk(2, 1))
+        self.kv_of = None if kv_of is None else whole(self.of)
+        self.out = padded(torch.full((rows, heads * D), 7.0, dtype=BF, device="cuda"), pad)
+        self.args = fb.make_cross(self.q, self.k, self.v, self.out, whole(self.q_at), whole(self.k_at),
+                                  head_dim=D, kv_of=self.kv_of, valid=self.valid, scale=scale)
+
+    def want(self):
+        D, G = self.D, self.heads // self.kv_heads
+        scale = self.scale or 1 / math.sqrt(D)
+        o = torch.full(self.out.shape, 7.0, dtype=torch.float64, device="cuda")
+        tol = torch.zeros_like(o)
+        for s, u in enumerate(self.of):
+            r = slice(self.q_at[s], self.q_at[s + 1])
+            keys = torch.arange(self.k_at[u], self.k_at[u + 1], device="cuda")
+            if self.valid is not None:
+                keys = keys[self.valid[keys] != 0]
+            o[r] = 0.0
+            if r.start == r.stop or len(keys) == 0:
+                continue
+            for h in range(self.heads):
+                c, kc = slice(h * D, (h + 1) * D), slice(h // G * D, (h // G + 1) * D)
+                q, k, v = self.q[r, c].double(), self.k[keys, kc].double(), self.v[keys, kc].double()
+                x = scale * (q @ k.T)
+                w = torch.softmax(x, 1)
+                o[r, c], size = w @ v, w @ v.abs()
+                d = 1.2e-7 * (D / 16) * scale * (q.abs() @ k.abs().T) + 2.0 ** -22 + \
+                    2.0 ** -23 * (x.abs() + x.abs().amax(1, keepdim=True))
+                tol[r, c] = 2.0 ** -8 * (size + o[r, c].abs()) + 2 * d.amax(1, keepdim=True) * size
+        return o, tol
+
+    def check(self, model):
+        model.op_cross_attention(self.args)
+        want, tol = self.want()
+        got = self.out.double()
+        bad = ~((got - want).abs() <= tol)
+        assert not bad.any(), (bad.nonzero()[:5].tolist(), got[bad][:5], want[bad][:5], tol[bad][:5])
+        if self.out.stride(0) > self.out.shape[1]:  # what lies between the rows is as it was
+            whole_rows = self.out.as_strided((self.out.shape[0] - 1, self.out.stride(0)), self.out.stride())
+            assert whole_rows[:, self.out.shape[1]:].isnan().all()
+
+
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("queries,keys", [
+    ([1], [1]), ([1], [512]), ([3], [2]), ([1, 1, 1, 1], [5, 128, 129, 1000]), ([128], [128]),
+    ([129], [127]), ([256], [16]), ([257], [17]), ([31, 33], [33, 31]), ([300, 5, 260], [15, 640, 130]),
+    ([0, 7, 0], [4, 0, 9]), ([0, 200, 1], [0, 300, 0]), ([5], [0]), ([1041], [77]), ([130] * 5, [512, 1, 64, 250, 113]),
+])
+def test_cross_lengths(model, D, queries, keys):
+    Cross(queries, keys, D=D, seed=len(queries)).check(model)
+
+
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (4, 2), (3, 1), (12, 4), (5, 1), (8, 8), (64, 1), (100, 1), (128, 1)])
+def test_cross_head_groups(model, D, heads, kv_heads):
+    Cross([1, 40, 9, 130], [70, 200, 0, 33], heads=heads, kv_heads=kv_heads, D=D, seed=heads).check(model)
+
+
+@pytest.mark.parametrize("D", [128, 64])
+def test_cross_shared_states(model, D):
+    """Sequences that share a prompt, prompts out of order, one that nobody asks."""
+    Cross([20, 1, 300, 7, 0, 130], [100, 257, 30, 3], kv_of=[1, 0, 1, 3, 0, 1], D=D, seed=3).check(model)
+
+
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("valid", [0.0, 0.3, 0.9, 1.0])
+@pytest.mark.parametrize("queries,keys", [([1], [700]), ([200, 33], [300, 129]), ([9, 9, 300], [1, 16, 128])])
+def test_cross_masked_keys(model, D, valid, queries, keys):
+    """Keys and values that are masked hold NaN and infinities; at 1.0 no key is left."""
+    Cross(queries, keys, heads=4, kv_heads=2, D=D, valid=valid, seed=int(valid * 10)).check(model)
+
+
+@pytest.mark.parametrize("first", [True, False])
+def test_cross_masked_tiles(model, first):
+    """Whole stretches of keys masked before or behind the ones that are left."""
+    valid = torch.ones(700 + 3)
+    valid[:400] = 0
+    Cross([150, 2], [640, 60], valid=valid if first else valid.flip(0), seed=5).check(model)
+
+
+@pytest.mark.parametrize("pad,packed", [(8, True), (24, False), (0, False)])
+def test_cross_strides(model, pad, packed):
+    Cross([33, 200], [64, 190], heads=3, pad=pad, packed=packed, seed=7).check(model)
+    Cross([1, 6], [64, 190], heads=6, kv_heads=3, D=64, pad=pad, packed=packed, seed=8).check(model)
+
+
+@pytest.mark.parametrize("scale,spread", [(1.0, 1.0), (0.01, 1.0), (0.0, 12.0)])
+def test_cross_scales(model, scale, spread):
+    """Flat and peaked rows, scores of hundreds."""
+    Cross([70, 140], [300, 65], scale=scale, spread=spread, seed=9).check(model)
+
+
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("queries,heads,kv_heads", [([1], 8, 1), ([1], 4, 4), ([300], 2, 2), ([5, 700], 2, 1)])
+def test_cross_long_states(model, D, queries, heads, kv_heads):
+    """Long states, whose keys several SMs share."""
+    Cross(queries, [9001] + [300] * (len(queries) - 1), heads=heads, kv_heads=kv_heads, D=D, seed=11).check(model)
+
+
+def test_cross_many_sequences(model):
+    rng = torch.Generator().manual_seed(1)
+    queries = torch.randint(0, 4, (700,), generator=rng).tolist()
+    keys = torch.randint(0, 60, (700,), generator=rng).tolist()
+    Cross(queries, keys, heads=2, kv_heads=1, D=64, seed=12).check(model)
+
+
+def test_cross_same_result_every_time_and_on_few_sms(model):
+    """The same bits on every call, with a repeat count, and on a budget of few SMs within the
+    tolerance."""
+    c = Cross([1, 513, 64], [4000, 700, 129], heads=4, kv_heads=2, valid=0.1, seed=13)
+    c.check(model)
+    first = c.out.clone()
+    fb.fb_set_op_repeat(model.handle, 3)
+    try:
+        c.out.fill_(7.0)
+        c.check(model)
+    finally:
+        fb.fb_set_op_repeat(model.handle, 1)
+    assert torch.equal(first, c.out)
+    model.set_sm_budget(8)
+    try:
+        c.out.fill_(7.0)
+        c.check(model)
+    finally:
+        model.set_sm_budget(0)
+
+
+def test_cross_on_another_stream(model):
+    side = torch.cuda.Stream()
+    c = Cross([70, 3], [200, 90], seed=14)
+    torch.cuda.synchronize()
+    model.set_stream(side.cuda_stream)
+    try:
+        c.check(model)
+    finally:
+        model.set_stream(None)
+
+
+@pytest.mark.parametrize("q_at,k_at,of", [
+    ([0, 5, 3], [0, 4, 8], None), ([1, 2, 3], [0, 4, 8], None), ([0, 5, 300], [0, 4, 8], None),
+    ([0, 2, 5], [0, 9, 8], None), ([0, 2, 5], [2, 4, 8], None), ([0, 2, 5], [0, 4, 900], None),
+    ([0, 2, 5], [0, 4, 8], [0, 2]), ([0, 2, 5], [0, 4, 8], [-1, 0]), ([0, -3, 5], [0, 4, 8], None),
+    ([0, 2, -5], [0, 4, 8], None), ([0, 2, 5], [0, -4, 8], None),
+])
+def test_cross_bad_offsets(model, q_at, k_at, of):
+    """Refused on the device; the model stays usable."""
+    c = Cross([2, 3], [4, 4], kv_of=None if of is None else [0, 1], seed=15)
+    q_bad, k_bad, of_bad = whole(q_at), whole(k_at), None if of is None else whole(of)
+    args = fb.make_cross(c.q, c.k, c.v, c.out, q_bad, k_bad, kv_of=of_bad)
+    with pytest.raises(fb.FlashBonError) as e:
+        model.op_cross_attention(args)
+    assert e.value.status == fb.FB_EINVAL
+    c.out.fill_(7.0)
+    c.check(model)
+
+
+# ---- adapters -------------------------------------------------------------------------
+
+class Adapters:
+    def __init__(self, segments, of, N=256, K=192, rank=8, adapters=None, act="none", out_t=BF,
+                 resid=False, gate=False, bias=True, scale=True, pad=0, seed=0, extra_rows=3,
+                 in_place=False, big=1.0):
+        g = gen(seed)
+        randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+        adapters = adapters or max(max(of, default=0), 0) + 1
+        self.at, self.of, self.act = offsets(segments), list(of), act
+        rows = self.at[-1] + extra_rows
+        self.x = padded(randn(rows, K).to(BF), pad)
+        self.w = (randn(N, K) * K ** -0.5).to(BF)
+        self.a = (big * randn(adapters, rank, K) * K ** -0.5).to(BF)
+        self.b = (randn(adapters, N, rank) * rank ** -0.5).to(BF)
+        unused = [e for e in range(adapters) if e not in of]
+        self.a[unused] = NAN  # nobody's adapters
+        self.b[unused] = NAN
+        self.scale = 0.5 + torch.rand(adapters, generator=g, device="cuda") if scale else None
+        self.bias = randn(N) if bias else None
+        self.gate = randn(N) if gate else None
+        self.out = padded(torch.full((rows, N), 7.0, dtype=out_t, device="cuda"), pad)
+        self.resid = None
+        if resid:
+            self.resid = self.out if in_place else padded(randn(rows, N), pad)
+            if in_place:
+                self.out.copy_(randn(rows, N))
+        self.before = self.out.clone()
+        self.resid_before = None if self.resid is None else self.resid.clone()
+        self.args = fb.make_adapters(self.x, self.w, self.a, self.b, whole(self.at), whole(self.of),
+                                     self.out, scale=self.scale, bias=self.bias, act=act,
+                                     resid=self.resid, gate=self.gate)
+
+    def want(self):
+        f32 = self.out.dtype == F32
+        K, N = self.w.shape[1], self.w.shape[0]
+        x = self.x.double()
+        y, size = x @ self.w.double().T, x.abs() @ self.w.double().abs().T
+        if self.bias is not None:
+            y, size = y + self.bias.double(), size + self.bias.double().abs()
+        unit = 1.2e-7 * (K / 16 + 16)
+        tol = unit * size
+        for i, e in enumerate(self.of):
+            if e < 0:
+                continue
+            r = slice(self.at[i], self.at[i + 1])
+            s = 1.0 if self.scale is None else self.scale[e].double()
+            a, b = self.a[e].double(), self.b[e].double()
+            t, t_size = x[r] @ a.T, x[r].abs() @ a.abs().T
+            y[r] += s * (t @ b.T)
+            tol[r] += s * (unit * t_size @ b.abs().T + (2.0 ** (-24 if f32 else -16) + 1.2e-7 * (b.shape[1] / 16 + 4))
+                           * (t.abs() @ b.abs().T))
+        if self.act == "gelu":
+            z = 2 * math.sqrt(2 / math.pi) * (y + 0.044715 * y ** 3)
+            y = y * torch.sigmoid(z)
+            tol = 1.13 * tol + (16 * 1.2e-7 if f32 else 2.0 ** -14) * y.abs() + 1e-30
+        if self.gate is not None:
+            y, tol = y * self.gate.double(), tol * self.gate.double().abs() + 1.2e-7 * (y * self.gate.double()).abs()
+        if self.resid is not None:
+            y = self.resid_before.double() + y
+            tol = tol + 1.2e-7 * (self.resid_before.double().abs() + y.abs())
+        tol = tol + (2.0 ** -24 if f32 else 2.0 ** -8) * y.abs()
+        end = self.at[-1]
+        y[end:], tol[end:] = self.before[end:].double(), 0.0
+        return y, tol
+
+    def check(self, model):
+        model.op_adapter_gemm(self.args)
+        self.compare()
+
+    def compare(self):
+        want, tol = self.want()
+        got = self.out.double()
+        bad = ~((got - want).abs() <= tol)
+        assert not bad.any(), (int(bad.sum()), bad.nonzero()[:5].tolist(), got[bad][:5], want[bad][:5], tol[bad][:5])
+        if self.out.stride(0) > self.out.shape[1]:
+            whole_rows = self.out.as_strided((self.out.shape[0] - 1, self.out.stride(0)), self.out.stride())
+            assert whole_rows[:, self.out.shape[1]:].isnan().all()
+
+
+@pytest.mark.parametrize("out_t", [BF, F32])
+@pytest.mark.parametrize("segments,of", [
+    ([1], [0]), ([1], [-1]), ([2, 1], [1, 0]), ([1] * 9, [0, 1, 2, -1, 2, 2, 0, -1, 1]), ([33], [0]),
+    ([16, 17], [0, 1]), ([0, 5, 0, 0, 11, 0], [0, 1, 2, -1, 0, 1]), ([300], [0]), ([129, 1, 257], [1, -1, 0]),
+    ([40] * 6, [0, 1, 2, 3, 4, 5]), ([1] * 70, list(range(70))), ([3] * 50, [i % 7 - 1 for i in range(50)]),
+    ([600, 2, 2, 2], [0, 1, 0, -1]), ([2000], [0]), ([700, 900, 31], [1, 0, -1]),
+])
+def test_adapter_segments(model, out_t, segments, of):
+    Adapters(segments, of, out_t=out_t, seed=len(segments)).check(model)
+
+
+@pytest.mark.parametrize("out_t", [BF, F32])
+@pytest.mark.parametrize("segments,of", [([5], [0]), ([1] * 40, [i % 3 for i in range(40)]), ([200, 150], [0, 1])])
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 64, 72, 128, 200, 256])
+def test_adapter_ranks(model, out_t, segments, of, rank):
+    Adapters(segments, of, out_t=out_t, rank=rank, seed=rank).check(model)
+
+
+@pytest.mark.parametrize("out_t", [BF, F32])
+@pytest.mark.parametrize("segments,of", [([1], [0]), ([20], [0]), ([1] * 40, [i % 3 for i in range(40)]), ([260, 90], [0, 1])])
+@pytest.mark.parametrize("N,K", [(8, 8), (8, 520), (264, 8), (1000, 1032), (136, 64), (520, 72), (2048, 4104)])
+def test_adapter_odd_sizes(model, out_t, segments, of, N, K):
+    Adapters(segments, of, N=N, K=K, out_t=out_t, seed=N + K).check(model)
+
+
+@pytest.mark.parametrize("segments,of", [([1], [0]), ([7, 9], [0, -1]), ([1] * 40, [i % 4 - 1 for i in range(40)]), ([300, 140], [1, 0])])
+@pytest.mark.parametrize("kw", [
+    dict(act="gelu"), dict(act="gelu", out_t=F32), dict(out_t=F32, resid=True, gate=True),
+    dict(out_t=F32, resid=True, gate=True, in_place=True), dict(out_t=F32, resid=True),
+    dict(out_t=F32, gate=True, act="gelu"), dict(bias=False, scale=False), dict(pad=8), dict(pad=24, out_t=F32),
+    dict(pad=8, out_t=F32, resid=True, gate=True, act="gelu"), dict(big=30.0), dict(extra_rows=0),
+])
+def test_adapter_epilogues(model, segments, of, kw):
+    Adapters(segments, of, N=328, K=448, rank=16, seed=21, **kw).check(model)
+
+
+def test_adapter_same_result_every_time_and_on_few_sms(model):
+    for segments, of in (([1] * 50, [i % 5 for i in range(50)]), ([400, 300, 9], [0, -1, 1]), ([6], [0])):
+        c = Adapters(segments, of, N=1536, K=1536, rank=16, seed=22)
+        c.check(model)
+        first = c.out.clone()
+        fb.fb_set_op_repeat(model.handle, 3)
+        try:
+            c.check(model)
+        finally:
+            fb.fb_set_op_repeat(model.handle, 1)
+        assert torch.equal(first, c.out)
+        model.set_sm_budget(8)
+        try:
+            c.check(model)
+        finally:
+            model.set_sm_budget(0)
+
+
+def test_adapter_on_another_stream(model):
+    side = torch.cuda.Stream()
+    c = Adapters([70, 3], [0, 1], seed=23)
+    torch.cuda.synchronize()
+    model.set_stream(side.cuda_stream)
+    try:
+        c.check(model)
+    finally:
+        model.set_stream(None)
+
+
+@pytest.mark.parametrize("rows", [4, 40, 400])
+@pytest.mark.parametrize("at,of", [
+    ([0, 3, 2], [0, 0]), ([1, 2, 3], [0, 0]), ([0, 3, 5000], [0, 0]), ([0, 2, 4], [0, 2]), ([0, 2, 4], [-2, 0]),
+    ([0, -1, 4], [0, 0]), ([0, 2, -4], [0, 0]),
+])
+def test_adapter_bad_segments(model, rows, at, of):
+    """Refused on the device; the model stays usable."""
+    c = Adapters([rows // 2, rows // 2], [0, 1], seed=24)
+    args = fb.make_adapters(c.x, c.w, c.a, c.b, whole(at), whole(of), c.out)
+    with pytest.raises(fb.FlashBonError) as e:
+        model.op_adapter_gemm(args)
+    assert e.value.status == fb.FB_EINVAL
+    c.out.copy_(c.before)
+    c.check(model)
+
+
+def test_scratch_failure_leaves_the_model_usable():
+    with fb.Model(synth.TINY, synth.make_weights(synth.TINY)) as m:
+        c = Adapters([300, 200], [0, 1], N=512, K=512, rank=16, seed=25)
+        fb.fb_test_fail_alloc(0)
+        try:
+            with pytest.raises(fb.FlashBonError) as e:
+                m.op_adapter_gemm(c.args)
+            assert e.value.status == fb.FB_ENOMEM
+        finally:
+            fb.fb_test_fail_alloc(-1)
+        c.out.copy_(c.before)
+        c.check(m)
+
+
+# ---- together -------------------------------------------------------------------------
+
+def test_cross_sublayer_of_several_requests(model):
+    """The cross-attention part of a block for four requests, each with its own prompt and adapter
+    (one without): keys and values from the prompts, queries, attention, the projection back into
+    the gated residual stream; two candidates a request share its prompt."""
+    D, H, rank, T = 256, 2, 16, 150
+    prompts, adapter = [77, 5, 130, 31], [0, -1, 2, 1]
+    g = gen(31)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    weights = {n: (randn(o, i) * i ** -0.5).to(BF) for n, o, i in
+               (("q", D, D), ("kv", 2 * D, 192), ("o", D, D))}
+    low = {n: ((randn(3, rank, w.shape[1]) * w.shape[1] ** -0.5).to(BF),
+               (0.3 * randn(3, w.shape[0], rank) * rank ** -0.5).to(BF)) for n, w in weights.items()}
+    h = randn(8 * T, D)
+    a = h.to(BF)
+    ctx = randn(sum(prompts), 192).to(BF)
+    gate = randn(D)
+    rows_at, per_candidate = whole(offsets([2 * T] * 4)), whole(offsets([T] * 8))
+    ctx_at, e = whole(offsets(prompts)), whole(adapter)
+    q, kv, o, out = (torch.zeros(n, w, dtype=t, device="cuda") for n, w, t in
+                     ((8 * T, D, BF), (sum(prompts), 2 * D, BF), (8 * T, D, BF), (8 * T, D, F32)))
+    model.op_adapter_gemm(fb.make_adapters(ctx, weights["kv"], *low["kv"], ctx_at, e, kv))
+    model.op_adapter_gemm(fb.make_adapters(a, weights["q"], *low["q"], rows_at, e, q))
+    model.op_cross_attention(fb.make_cross(q, kv[:, :D], kv[:, D:], o, per_candidate, ctx_at,
+                                           kv_of=whole([0, 0, 1, 1, 2, 2, 3, 3])))
+    model.op_adapter_gemm(fb.make_adapters(o, weights["o"], *low["o"], rows_at, e, out, resid=h, gate=gate))
+
+    def project(x, name, i):
+        y = x @ weights[name].double().T
+        if adapter[i] >= 0:
+            la, lb = (t[adapter[i]].double() for t in low[name])
+            y = y + x @ la.T @ lb.T
+        return y
+
+    at = offsets(prompts)
+    for i in range(4):
+        rows = slice(2 * T * i, 2 * T * (i + 1))
+        keys = project(ctx[at[i]:at[i + 1]].double(), "kv", i)
+        query = project(a[rows].double(), "q", i)
+        y = torch.cat([torch.softmax(query[:, c] @ keys[:, c].T / math.sqrt(128), 1) @ keys[:, D:][:, c]
+                       for c in (slice(0, 128), slice(128, 256))], 1)
+        step = gate.double() * project(y, "o", i)
+        err = (out[rows].double() - h[rows].double() - step).norm() / step.norm()
+        # four roundings to bf16 on the way (k, v, q, weights, o), 2^-8 each at most
+        assert err < 5 * 2.0 ** -8, (i, err)
