@@ -574,11 +574,11 @@ fb_status cross_args(const fb_cross& c, CrossArgs* out) {
 }
 
 // (the work of rows whose sequences all attend to the mean number of keys)
-fb_status run_cross(fb_model* m, const CrossArgs& c) {
+fb_status run_cross(fb_model* m, const CrossArgs& c, uint8_t* ws) {
   const double wq = (double)c.heads * c.head_dim, wk = (double)c.kv_heads * c.head_dim;
   const double keys = c.states ? (double)c.kv_rows / c.states : 0;
   KTimer t(m, FB_K_CROSS, 4.0 * wq * c.q_rows * keys, 4.0 * (wq * c.q_rows + wk * c.kv_rows));
-  CK(cross_attention(c, m->derr, m->num_sms, m->st));
+  CK(cross_attention(c, ws, m->attn_flags, m->derr, m->num_sms, m->st));
   return FB_OK;
 }
 
@@ -1956,7 +1956,8 @@ fb_status fb_op_cross_attention(fb_model* m, const fb_cross* c) {
   if (a.q_rows == 0 || a.seqs == 0) return FB_OK;
   const DeviceScope on(m->dev);
   CKS(begin_call(m));
-  for (int r = 0; r < m->op_repeat; ++r) CKS(run_cross(m, a));
+  CKS(ensure_moe(m, cross_ws_bytes(a, m->num_sms)));
+  for (int r = 0; r < m->op_repeat; ++r) CKS(run_cross(m, a, m->moe_ws));
   return end_call(m);
 }
 
@@ -2071,6 +2072,7 @@ fb_status fb_set_device_wait_limit(unsigned long long ns) {
   CK(gemm_tc_set_wait_limit(ns));
   CK(attention_tc_set_wait_limit(ns));
   CK(expert_gemm_set_wait_limit(ns));
+  CK(cross_set_wait_limit(ns));
   return FB_OK;
 }
 

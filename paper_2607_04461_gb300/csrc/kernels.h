@@ -173,7 +173,12 @@ cudaError_t expert_gemm_set_wait_limit(unsigned long long ns);
 
 // ---- several requests in one batch (flashbon.h has the definitions) ---------------------
 struct CrossArgs : fb_cross {};  // scale filled in
-cudaError_t cross_attention(const CrossArgs& c, int* err, int num_sms, cudaStream_t st);
+// ws: cross_ws_bytes of scratch; counters: [num_sms][8], zero between launches
+size_t cross_ws_bytes(const CrossArgs& c, int num_sms);
+cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* err, int num_sms,
+                            cudaStream_t st);
+// Sets the cross unit's device wait limit on the current device (ns).
+cudaError_t cross_set_wait_limit(unsigned long long ns);
 struct AdapterArgs : fb_adapters {};
 // ws: adapter_ws_bytes of scratch
 size_t adapter_ws_bytes(const AdapterArgs& g);
