@@ -614,7 +614,7 @@ fb_status run_adapters(fb_model* m, const AdapterArgs& g, uint8_t* ws) {
   KTimer t(m, FB_K_ADAPTER, 2.0 * r * (n * k + g.rank * (n + k)),
            2.0 * (r * k + n * k + (double)g.adapters * g.rank * (n + k)) +
                r * n * (type_bytes(g.out_type) + (g.resid ? 4 : 0)),
-           adapter_launches(g));
+           adapter_launches(g, m->num_sms));
   CK(adapter_gemm(g, ws, m->derr, m->num_sms, m->st));
   return FB_OK;
 }
@@ -1968,7 +1968,7 @@ fb_status fb_op_adapter_gemm(fb_model* m, const fb_adapters* g) {
   if (a.rows == 0 || a.segments == 0) return FB_OK;
   const DeviceScope on(m->dev);
   CKS(begin_call(m));
-  CKS(ensure_moe(m, adapter_ws_bytes(a)));
+  CKS(ensure_moe(m, adapter_ws_bytes(a, m->num_sms)));
   for (int r = 0; r < m->op_repeat; ++r) CKS(run_adapters(m, a, m->moe_ws));
   return end_call(m);
 }
@@ -2073,6 +2073,7 @@ fb_status fb_set_device_wait_limit(unsigned long long ns) {
   CK(attention_tc_set_wait_limit(ns));
   CK(expert_gemm_set_wait_limit(ns));
   CK(cross_set_wait_limit(ns));
+  CK(adapter_set_wait_limit(ns));
   return FB_OK;
 }
 

@@ -181,9 +181,11 @@ cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* er
 cudaError_t cross_set_wait_limit(unsigned long long ns);
 struct AdapterArgs : fb_adapters {};
 // ws: adapter_ws_bytes of scratch
-size_t adapter_ws_bytes(const AdapterArgs& g);
-int adapter_launches(const AdapterArgs& g);
+size_t adapter_ws_bytes(const AdapterArgs& g, int num_sms);
+int adapter_launches(const AdapterArgs& g, int num_sms);
 cudaError_t adapter_gemm(const AdapterArgs& g, void* ws, int* err, int num_sms, cudaStream_t st);
+// Sets the adapter unit's device wait limit on the current device (ns).
+cudaError_t adapter_set_wait_limit(unsigned long long ns);
 
 // ---- measurement probe ----------------------------------------------------------------
 // One CTA per entry of `grid`, each timing (SM clock cycles, cycles[cta]) `reps` tcgen05.mma
