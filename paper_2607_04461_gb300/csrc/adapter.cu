@@ -16,13 +16,14 @@
 // (tcgen05, cta_group::2; weight rows are the MMA's M side, rows of x its N side, any multiple of 16
 // up to 256): the scheme of the products grouped by expert, with the segments as groups.
 //  * warp 0 loads weights, one TMA box of 128 rows x 64 k: W, then B_e (or A_e).
-//  * warps 10 and 11 load rows of x, then of t, a K block each by turns.
-//  * warp 1 issues the MMAs, warps 2-9 of both CTAs run the epilogue.
+//  * warp 1 issues the MMAs, warps 2 and up of both CTAs run the epilogue.
+//  * the last two warps load rows of x, then of t, a K block each by turns.
 // fp32 results take K in parts of 4 blocks, each in an accumulator of its own, which the epilogue
 // adds up (the tensor core's sums lose about 6e-8 of the result per K block of 64). So do results of
 // a K past 2^17.
 // Every wait is bounded (mbar_wait): a role that gives up records it and the kernel ends.
 #include <atomic>
+#include <climits>
 
 #include "grouped.cuh"
 #include "kernels.h"
@@ -31,7 +32,13 @@ namespace {
 
 constexpr int TMEM_COLS = 512;
 constexpr int MAX_STAGES = 8, MAX_ACCS = 8;
-constexpr int THREADS = 384;
+// Warps: weight loader, MMA, epilogue, two row loaders. Sums in parts wait in the epilogue's registers,
+// 64 a thread, so that twelve warps hold a tile of 192 rows (a K block costs 256 + w clocks of
+// operands: the wider the better), where 128 registers are left to a thread.
+template <bool PARTS>
+struct Warps {
+  static constexpr int EPI = PARTS ? 12 : 8, GROUPS = EPI / 4, LOAD = 2 + EPI, THREADS = 32 * (4 + EPI);
+};
 constexpr int MAX_S = FB_ADAPTER_MAX_SEGMENTS;
 constexpr int SMEM_BYTES = 229888;  // (room for a block of the low-rank part beside it)
 constexpr int EPI_TILE = 2048;      // an epilogue warp's tile: 32 tokens x 32 rows, bf16
@@ -44,14 +51,15 @@ __host__ __device__ constexpr int ring_bytes(bool tiles) {
 static_assert(ring_bytes(true) % 128 == 0, "TMA tiles lie on 128-byte boundaries");
 constexpr int64_t BAND_BYTES = 16ll << 20;  // of weights before a segment's next rows (they stay in L2)
 constexpr int PART_BLOCKS = 4;              // K blocks of one accumulator, for sums in parts
-constexpr int F32_T = 128;                  // widest tile then (its sums wait in registers)
+constexpr int F32_T = 192;                  // widest tile then
 constexpr int LONG_K = 1 << 17;
 bool in_parts(const AdapterArgs& g) { return g.out_type == FB_F32 || g.k > LONG_K; }
 
 // How t's terms lie in a row of the scratch. Ranks up to 64 are rounded up to 16, the terms side by
 // side; larger ones to 64, 64 columns of each term by turns. Either way K block i of t is columns 64 i
 // and up, chunk j (16 columns) of it meets chunk (4 i + j) % chunks of B_e's box of 64 columns, and
-// the box is i / terms (the only one for ranks up to 64).
+// the box is i / terms (the only one for ranks up to 64). Chunks behind the last term are zeros, and meet
+// the zeros behind B_e's last column.
 struct Terms {
   int terms, rp, cols;  // rank as rounded up, columns of a row of t (whole K blocks)
   __host__ __device__ Terms(int rank, bool parts)
@@ -63,28 +71,47 @@ struct Terms {
   }
 };
 
+// Tensor maps: W (or A_e) and B_e in boxes of 128 rows, x and t in boxes of 64, 32, 16 and 8 rows (a
+// tile's half is a multiple of 8), results in boxes of 16 tokens.
+struct Maps {
+  CUtensorMap w, b, x[4], t[4], o;
+};
 struct TcArgs {
   int groups;               // segments, or (offsets null) one group of the first *end rows
   const int32_t *offsets, *end, *adapter;
   int adapters, rows, n, k; // n: weight rows
   int rank;
-  int slices;               // of K, DOWN: each forms a sum of its own
-  bf16* t;                  // DOWN with one slice: its terms
-  float* part;              // DOWN: [slice][rows][rp]
+  bf16* t;                  // DOWN
   const float* scale;       // DOWN
+  float* ws;                // parts of cut tiles (null: whole tiles only): two slots a cluster
+  int* counters;            // [clusters][ADAPTER_COUNTERS], zero between launches
   const float *bias, *delta, *resid, *gate;
   int64_t ldr, ldo;
   int act, out_type;
   void* out;
 };
 
+// Tiles cut between clusters, where whole ones would leave clusters idle in the last round (t alone
+// has few tiles): the clusters take equal stretches of the row of all tiles' K blocks, each weighted
+// by its tile's clocks, and a stretch may begin within a tile, four blocks from its ends at least.
+// Each cluster of a cut tile leaves its sums in the scratch; a counter tells who comes last, and
+// that one adds them up, in cluster order. Nobody waits.
+constexpr int MIN_BLOCKS = 4;
+struct Cut {
+  int on, clusters;         // clusters that work
+  int t0, k0, t1, k1;       // this cluster's stretch: from block k0 of tile t0 to block k1 of tile t1
+  unsigned u0, u1, units;   // where those tiles begin, all units
+};
+constexpr int WS_WARP = MAX_T / 2 * 32;  // floats of an epilogue warp's part, at most
+constexpr size_t WS_SLOT = 2 * 12 * (size_t)WS_WARP;
+constexpr int ADAPTER_COUNTERS = 2 * 12;  // of a cluster
+
 // DOWN: t = scale x A_e^T (n = rank), else the product.
 template <bool DOWN, bool PARTS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
-    adapter_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmB,
-                      const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmX8,
-                      const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmT8,
-                      const __grid_constant__ CUtensorMap tmO, const TcArgs g, int* err) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<PARTS>::THREADS, 1)
+    adapter_tc_kernel(const __grid_constant__ Maps maps, const TcArgs g, int* err) {
+  constexpr int THREADS = Warps<PARTS>::THREADS, EPI = Warps<PARTS>::EPI, GROUPS = Warps<PARTS>::GROUPS;
+  constexpr int LOAD = Warps<PARTS>::LOAD;
   constexpr bool TILES = !DOWN && !PARTS;  // results leave through shared-memory tiles
   extern __shared__ __align__(1024) uint8_t smem[];  // (operand tiles need the alignment)
   if ((smem_u32(smem) & 1023u) != 0) {
@@ -106,26 +133,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   int* width = bad + 1;
   unsigned* cost = reinterpret_cast<unsigned*>(width + 1);  // of each width, and its token tiles
   unsigned* count = cost + WIDTHS;
+  __shared__ Cut cut;
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t rank = cluster_ctarank();
   const int cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
-  // DOWN: one tile of weight rows, its K slices stand in the tile's place
-  const int n_ft = DOWN ? g.slices : (g.n + 2 * W_ROWS - 1) / (2 * W_ROWS);
+  const int n_ft = (g.n + 2 * W_ROWS - 1) / (2 * W_ROWS);  // (DOWN: 1)
   const int nk = (g.k + BK - 1) / BK, E = g.groups;
   const Terms terms(g.rank, PARTS);
   const int ext = g.adapter ? terms.blocks() : 0;
   const int chunks = terms.rp <= 64 ? terms.rp / 16 : 4, all_chunks = terms.terms * terms.rp / 16;
-  // K blocks kb0 .. of a tile, and how many; the ones of t behind those of x
-  auto k_range = [&](const Tile& q, int& kb0, int& blocks) {
-    if (DOWN) {
-      kb0 = (int)((int64_t)nk * q.f / g.slices);
-      blocks = (int)((int64_t)nk * (q.f + 1) / g.slices) - kb0;
-    } else {
-      kb0 = 0;
-      blocks = nk + (who[q.e] >= 0 ? ext : 0);
-    }
-  };
   bool failed = false;
 
   if (threadIdx.x == 0) {
@@ -137,14 +154,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     }
     for (int a = 0; a < MAX_ACCS; ++a) {
       mbar_init(&tmem_full[a], 1);
-      mbar_init(&tmem_empty[a], 16);  // 8 epilogue warps x 2 CTAs
+      mbar_init(&tmem_empty[a], 2 * EPI);  // the epilogue warps of both CTAs
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    tma_prefetch_desc(&tmW);
-    tma_prefetch_desc(&tmX);
-    tma_prefetch_desc(&tmX8);
-    if (!DOWN) tma_prefetch_desc(&tmB);
-    if (TILES) tma_prefetch_desc(&tmO);
+    tma_prefetch_desc(&maps.w);
+    tma_prefetch_desc(&maps.x[0]);
+    if (TILES) tma_prefetch_desc(&maps.o);
   }
   if (threadIdx.x >= 64 && threadIdx.x < 64 + 2 * WIDTHS) cost[threadIdx.x - 64] = 0;
   if (warp == 1) tmem_alloc_cg2(tmem_holder, TMEM_COLS);
@@ -169,6 +184,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     __syncthreads();
   }
   auto rows_of = [&](int e) { return DOWN && who[e] < 0 ? 0 : off[e + 1] - off[e]; };
+  const int all_blocks = nk + (DOWN ? 0 : ext);  // K blocks of a tile whose rows have an adapter
+  // a K block of group e's tiles in units of 32 clocks
+  auto weight = [&](int e) -> unsigned {
+    const int nt = first[e + 1] - first[e], w = nt ? (rows_of(e) + nt - 1) / nt : 0;
+    return (unsigned)(256 + w > 313 ? 256 + w : 313) / 32;
+  };
+  auto units_of = [&](int e) { return (unsigned)((first[e + 1] - first[e]) * n_ft) * all_blocks * weight(e); };
+  // where cluster c's stretch of `all` units begins: floor(c all / n)
+  auto stretch = [](unsigned c, unsigned all, unsigned n) { return all / n * c + all % n * c / n; };
   {
     // (nt tiles of widths that add up to r: 256 nt + r, see below)
     const int c = threadIdx.x % WIDTHS, T = T_STEP * (c + 1);
@@ -185,22 +209,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   }
   __syncthreads();
   if (warp == 0) {
-    // the width of the least estimated time in SM clocks: 256 + w clocks of operands, or 313 of
+    // The width of the least estimated time in SM clocks: 256 + w clocks of operands, or 313 of
     // issue, per K block; in the fullest cluster each tile but the first takes its mainloop or its
-    // epilogue
-    const int T = T_STEP * (lane + 1);
-    const float blocks = DOWN ? (float)nk / g.slices : (float)(nk + ext);
-    float est = 3e38f;
-    if (lane < WIDTHS && (!PARTS || T <= F32_T)) {
-      const float n = (float)count[lane] * n_ft, rounds = ceilf(n / n_clusters);
-      const float main = count[lane] ? (float)cost[lane] / count[lane] * blocks : 0.f;
+    // epilogue. Lanes 16 and up: the same with tiles cut into equal stretches, at least 12 K blocks
+    // a cluster, and what storing and adding up the last tile's parts takes.
+    const int T = T_STEP * (lane % WIDTHS + 1);
+    float est = 3e38f, ctas = n_clusters;
+    if (!PARTS || T <= F32_T) {
+      const float n = (float)count[lane % WIDTHS] * n_ft, rounds = ceilf(n / n_clusters);
+      const float main = n > 0.f ? (float)cost[lane % WIDTHS] / count[lane % WIDTHS] * all_blocks : 0.f;
       const float epi = TILES ? 2900.f + 12.f * T : 3300.f + 30.f * T;
-      est = main + (rounds - 1.f) * fmaxf(main, epi) + (TILES ? 16.f : 28.f) * T;
+      const float last = (TILES ? 16.f : 28.f) * T;
+      if (lane < WIDTHS) {
+        est = main + (rounds - 1.f) * fmaxf(main, epi) + last;
+      } else if (g.ws && all_blocks >= 4 * MIN_BLOCKS) {
+        ctas = fminf(ctas, fmaxf(1.f, floorf(n * all_blocks / 12.f)));
+        est = fmaxf(main, epi) * n / ctas + last + (DOWN ? 5000.f : 6000.f + 100.f * T);
+      }
     }
     float best = est;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) best = fminf(best, __shfl_xor_sync(0xffffffffu, best, o));
-    const int Tb = T_STEP * __ffs(__ballot_sync(0xffffffffu, est == best));
+    const int winner = __ffs(__ballot_sync(0xffffffffu, est == best)) - 1, Tb = T_STEP * (winner % WIDTHS + 1);
+    ctas = __shfl_sync(0xffffffffu, ctas, winner);
     int sum = 0;
     for (int e0 = 0; e0 <= E; e0 += 32) {
       const int e = e0 + lane;
@@ -213,7 +244,58 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       if (e <= E) first[e] = sum + s - n;
       sum += __shfl_sync(0xffffffffu, s, 31);
     }
-    if (lane == 0) *width = Tb;
+    __syncwarp();
+    if (lane == 0) {
+      *width = Tb;
+      cut.on = winner >= WIDTHS;
+      cut.clusters = (int)ctas;
+    }
+    if (winner >= WIDTHS) {
+      // all units, then the groups in which this cluster's stretch and the next one's begin
+      unsigned all = 0;
+      for (int e = lane; e < E; e += 32) all += units_of(e);
+      all = __reduce_add_sync(0xffffffffu, all);
+      if (lane == 0) cut.units = all;
+      const unsigned x0 = stretch(cluster, all, (unsigned)ctas), x1 = stretch(cluster + 1, all, (unsigned)ctas);
+      unsigned before = 0;
+      bool have0 = false, have1 = false;
+      if (lane == 0) {  // (behind the last tile)
+        cut.t0 = cut.t1 = first[E] * n_ft;
+        cut.k0 = cut.k1 = 0;
+      }
+      __syncwarp();
+      for (int e0 = 0; e0 < E && !(have0 && have1); e0 += 32) {
+        const int e = e0 + lane;
+        const unsigned mine = e < E ? units_of(e) : 0;
+        unsigned upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const unsigned v = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += v;
+        }
+        const unsigned u = before + upto - mine;
+        // the lane whose group a position lies in works it out
+        auto place = [&](unsigned x, int& t, int& kb, unsigned& u_t) {
+          const bool here = x >= u && x - u < mine;
+          if (here) {
+            const unsigned wt = weight(e), per = all_blocks * wt, v = x - u, q = v / per;
+            u_t = u + q * per;
+            kb = (int)((v - q * per) / wt);
+            t = first[e] * n_ft + (int)q;
+            if (kb < MIN_BLOCKS) {
+              kb = 0;
+            } else if (all_blocks - kb < MIN_BLOCKS) {
+              kb = 0;
+              ++t;
+            }
+          }
+          return __any_sync(0xffffffffu, here);
+        };
+        have0 = place(x0, cut.t0, cut.k0, cut.u0) || have0;
+        have1 = place(x1, cut.t1, cut.k1, cut.u1) || have1;
+        before += __shfl_sync(0xffffffffu, upto, 31);
+      }
+    }
   }
   tc_fence_before();
   cluster_sync();  // barriers initialised, TMEM allocated, tables written
@@ -224,46 +306,72 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   const int stages = RING_BYTES / stage_bytes < MAX_STAGES ? RING_BYTES / stage_bytes : MAX_STAGES;
   const int acc_cols = acc_cols_of(T);
   const int n_accs = TMEM_COLS / acc_cols < MAX_ACCS ? TMEM_COLS / acc_cols : MAX_ACCS;
-  const int fit = DOWN ? n_ft : (int)(BAND_BYTES / ((int64_t)2 * W_ROWS * g.k * sizeof(bf16)));
-  TileIter ti(off, first, cluster, n_clusters, n_ft, fit < 1 ? 1 : fit < n_ft ? fit : n_ft, E);
+  const int fit = (int)(BAND_BYTES / ((int64_t)2 * W_ROWS * g.k * sizeof(bf16)));
+  const bool split = cut.on != 0;
+  TileIter ti(off, first, split ? cluster < cut.clusters ? cut.t0 : INT_MAX - (1 << 20) : cluster,
+              split ? 1 : n_clusters, n_ft, fit < 1 ? 1 : fit < n_ft ? fit : n_ft, E);
   Tile k;
   int kb0, blocks;
+  // The next tile, and the K blocks kb0 .. kb0 + blocks - 1 of it that are this cluster's (t's behind
+  // x's; none where they are all t's and the tile has no adapter).
+  auto next_tile = [&](Tile& q, int& from, int& n) {
+    if (split && (ti.t > cut.t1 || (ti.t == cut.t1 && cut.k1 == 0))) return false;
+    const int t = ti.t;
+    if (!ti.next(q)) return false;
+    const int all = DOWN || who[q.e] < 0 ? nk : nk + ext;
+    const int a = split && t == cut.t0 ? cut.k0 : 0, b = split && t == cut.t1 ? cut.k1 : all;
+    from = a < all ? a : all;
+    n = (b < all ? b : all) - from;
+    return true;
+  };
+
+  // The clusters lo .. hi that hold parts of tile t of group e (cut.t0 or cut.t1): a stretch begins
+  // within it at least MIN_BLOCKS from its ends.
+  auto holders = [&](int t, int e, int& lo, int& hi) {
+    const unsigned wt = weight(e), u = t == cut.t0 && cut.k0 > 0 ? cut.u0 : cut.u1;
+    const unsigned most = cut.units / cut.clusters + 1;
+    auto from = [&](unsigned y) {  // the first cluster whose stretch begins at y or behind
+      unsigned c = y / most;
+      while (stretch(c, cut.units, cut.clusters) < y) ++c;
+      return (int)c;
+    };
+    lo = from(u + MIN_BLOCKS * wt) - 1;
+    hi = from(u + (all_blocks - MIN_BLOCKS + 1) * wt) - 1;
+  };
 
   if (warp == 0) {
     // ---------------- weights (both CTAs) ----------------
     int stage = 0;
     uint32_t phase = 0;
-    while (!failed && ti.next(k)) {
+    while (!failed && next_tile(k, kb0, blocks)) {
       const uint32_t bytes = 2 * (W_BYTES + k.w / 2 * BK * 2);
       const int e = who[k.e];
-      k_range(k, kb0, blocks);
-      for (int i = 0; i < blocks; ++i) {
+      for (int i = kb0; i < kb0 + blocks; ++i) {
         if (!mbar_wait_warp(&empty[stage], phase ^ 1u, err)) { failed = true; break; }
         if (elect_one()) {
           const uint32_t dst = smem_u32(smem) + stage * stage_bytes;
           const uint32_t fb = mapa_shared(smem_u32(&full[stage]), 0);
           if (rank == 0) mbar_expect_tx(&full[stage], bytes);
           if (DOWN)
-            tma_load_3d_cg2(dst, &tmW, fb, (kb0 + i) * BK, (int)rank * W_ROWS, e);
+            tma_load_3d_cg2(dst, &maps.w, fb, i * BK, (int)rank * W_ROWS, e);
           else if (i < nk)
-            tma_load_3d_cg2(dst, &tmW, fb, i * BK, (2 * k.f + (int)rank) * W_ROWS, 0);
+            tma_load_3d_cg2(dst, &maps.w, fb, i * BK, (2 * k.f + (int)rank) * W_ROWS, 0);
           else
-            tma_load_3d_cg2(dst, &tmB, fb, terms.rp <= 64 ? 0 : (i - nk) / terms.terms * BK,
+            tma_load_3d_cg2(dst, &maps.b, fb, terms.rp <= 64 ? 0 : (i - nk) / terms.terms * BK,
                             (2 * k.f + (int)rank) * W_ROWS, e);
         }
         if (++stage == stages) { stage = 0; phase ^= 1u; }
       }
     }
-  } else if (warp >= 10) {
+  } else if (warp >= LOAD) {
     // ---------------- rows of x and t (both CTAs) ----------------
     int stage = 0;
     uint32_t phase = 0;
-    int turn = warp - 10;  // K blocks until this warp's next: they go round the two
+    int turn = warp - LOAD;  // K blocks until this warp's next: they go round the two
     bool waited = DOWN;
-    while (!failed && ti.next(k)) {
+    while (!failed && next_tile(k, kb0, blocks)) {
       const int half = k.w / 2, a0 = k.r0 + half * (int)rank;
-      k_range(k, kb0, blocks);
-      for (int i = 0; i < blocks; ++i) {
+      for (int i = kb0; i < kb0 + blocks; ++i) {
         if (turn-- == 0) {
           turn = 1;
           if (!mbar_wait_warp(&empty[stage], phase ^ 1u, err)) { failed = true; break; }
@@ -275,11 +383,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
           if (elect_one()) {
             const uint32_t dst = smem_u32(smem) + stage * stage_bytes + W_BYTES;
             const uint32_t fb = mapa_shared(smem_u32(&full[stage]), 0);
-            const CUtensorMap *m64 = of_t ? &tmT : &tmX, *m8 = of_t ? &tmT8 : &tmX8;
-            const int x = (of_t ? i - nk : kb0 + i) * BK;
+            const CUtensorMap* m = of_t ? maps.t : maps.x;
+            const int x = (of_t ? i - nk : i) * BK;
             int r = 0;
-            for (; r + 64 <= half; r += 64) tma_load_rows_cg2(dst + r * (BK * 2), m64, fb, x, a0 + r);
-            for (; r < half; r += 8) tma_load_rows_cg2(dst + r * (BK * 2), m8, fb, x, a0 + r);
+            for (; r + 64 <= half; r += 64) tma_load_rows_cg2(dst + r * (BK * 2), m, fb, x, a0 + r);
+#pragma unroll
+            for (int b = 32, j = 1; b >= 8; b /= 2, ++j)
+              if (half & b) {
+                tma_load_rows_cg2(dst + r * (BK * 2), m + j, fb, x, a0 + r);
+                r += b;
+              }
           }
         }
         if (++stage == stages) { stage = 0; phase ^= 1u; }
@@ -292,53 +405,68 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       const uint32_t ring_lo = desc_lo_k(smem_u32(smem));
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
-      while (!failed && ti.next(k)) {
+      while (!failed && next_tile(k, kb0, blocks)) {
         const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(k.w >> 3) << 17) |
                                ((uint32_t)(2 * W_ROWS >> 4) << 24);
-        k_range(k, kb0, blocks);
-        // the tile's K parts, each in the ring's next accumulator
-        const int part_len = PARTS ? PART_BLOCKS : blocks;
-        for (int i = 0; !failed && i < blocks;) {
+        // The tile's K parts, each in the ring's next accumulator. All control flow goes by votes: the
+        // K range comes from shared memory, and what the compiler does not see to be the same in all
+        // lanes costs the MMAs' operands a move to a uniform register each (one K block 550 clocks
+        // whatever its width; see elect_one).
+        const int stop = kb0 + blocks;
+        int i = kb0, end = i;
+        bool more = __all_sync(0xffffffffu, i < stop);
+        while (!failed && more) {
           if (!mbar_wait_warp(&tmem_empty[acc], acc_phase ^ 1u, err)) { failed = true; break; }
           tc_fence_after();
           const uint32_t d_tmem = tmem_base + acc * acc_cols;
-          const int start = i, end = blocks - i < part_len ? blocks : i + part_len;
-          for (; i < end; ++i) {
+          end = PARTS && stop - i > PART_BLOCKS ? i + PART_BLOCKS : stop;
+          bool first = true, last = false;
+          while (!last) {
+            last = __all_sync(0xffffffffu, i + 1 >= end);
+            const bool straight = DOWN || terms.rp >= 64 || __all_sync(0xffffffffu, i < nk);
+            uint32_t cols = 0;  // t's chunks against B_e's: columns of each, 16 to a unit (see Terms)
+            if (!straight) {
+              int c = 4 * (i - nk);
+#pragma unroll
+              for (int j = 0; j < 4; ++j, ++c) cols |= (uint32_t)(c < all_chunks ? c % chunks : 3) << (8 * j);
+            }
             if (!mbar_wait_warp(&full[stage], phase, err)) { failed = true; break; }
             tc_fence_after();
             const uint32_t wlo = ring_lo + (uint32_t)(stage * (stage_bytes >> 4));
             const uint32_t alo = wlo + (W_BYTES >> 4);
-            if (DOWN || i < nk) {
+            if (straight) {
               if (elect_one()) {
 #pragma unroll
                 for (int j = 0; j < BK / 16; ++j)
                   tc_mma_cg2_lo(d_tmem, wlo + 2 * j, alo + 2 * j, DESC_HI, idesc,
-                                (i > start || j > 0) ? 1u : 0u);
+                                (!first || j > 0) ? 1u : 0u);
                 tc_commit_mc(&empty[stage], 0x3);
-                if (i + 1 == end) tc_commit_mc(&tmem_full[acc], 0x3);
+                if (last) tc_commit_mc(&tmem_full[acc], 0x3);
               }
-            } else if (elect_one()) {  // t: chunks of 16 columns against B_e's
-              const int c0 = 4 * (i - nk);
-#pragma unroll 1
-              for (int j = 0; j < 4 && c0 + j < all_chunks; ++j)
-                tc_mma_cg2_lo(d_tmem, wlo + 2 * ((c0 + j) % chunks), alo + 2 * j, DESC_HI, idesc,
-                              (i > start || j > 0) ? 1u : 0u);
+            } else if (elect_one()) {
+#pragma unroll
+              for (int j = 0; j < BK / 16; ++j)
+                tc_mma_cg2_lo(d_tmem, wlo + 2 * ((cols >> (8 * j)) & 3), alo + 2 * j, DESC_HI, idesc,
+                              (!first || j > 0) ? 1u : 0u);
               tc_commit_mc(&empty[stage], 0x3);
-              if (i + 1 == end) tc_commit_mc(&tmem_full[acc], 0x3);
+              if (last) tc_commit_mc(&tmem_full[acc], 0x3);
             }
+            first = false;
+            ++i;
             if (++stage == stages) { stage = 0; phase ^= 1u; }
           }
           if (++acc == n_accs) { acc = 0; acc_phase ^= 1u; }
+          more = __all_sync(0xffffffffu, i < stop);
         }
       }
     }
   } else {
     // ---------------- epilogue (warps 2..9 of both CTAs) ----------------
-    // warp: weight rows quarter * 32 .. + 31 of this CTA's 128 (its TMEM lanes), every other
+    // warp: weight rows quarter * 32 .. + 31 of this CTA's 128 (its TMEM lanes), every GROUPS-th
     // CH-token chunk of the tile
     constexpr int CH = PARTS ? 16 : 32;
     const int quarter = warp & 3, we = warp - 2;
-    int half = we >> 2;  // a tile's first chunk goes to either half by turns
+    int group = we >> 2;  // a tile's first chunk goes to each group of four warps by turns
     const uint32_t te_remote = mapa_shared(smem_u32(&tmem_empty[0]), 0);
     uint8_t* tiles = epi_smem + we * 2 * EPI_TILE;
     int acc = 0, buf = 0;
@@ -355,41 +483,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     };
     const int limit = DOWN ? terms.rp : g.n;  // features that are stored
     Tile after;
-    bool more = ti.next(k);
+    int kb_after = 0, blocks_after = 0, t_after = ti.t, t = 0;
+    bool more = next_tile(k, kb0, blocks);
     float bias = more ? bias_of(k) : 0.f;
-    for (; !failed && more; k = after) {
-      more = ti.next(after);
+    for (; !failed && more; k = after, kb0 = kb_after, blocks = blocks_after) {
+      t = t_after;  // the tile's number
+      t_after = ti.t;
+      more = next_tile(after, kb_after, blocks_after);
       const float bias_after = more ? bias_of(after) : 0.f;  // (it may come from memory)
       const int f0 = first_feature(k), feature = f0 + lane;
+      const int col0 = terms.column(0, feature), col1 = terms.column(1, feature), col2 = terms.column(2, feature);
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
       if (!waited) {
         griddep_wait();
         waited = true;
       }
-      k_range(k, kb0, blocks);
-      // the low-rank part of CH tokens from t0 on
-      auto add_delta = [&](float* v, int t0) {
-        if (DOWN || !g.delta) return;
-        const int n = k.nv - t0;
-        const float* from = g.delta + (size_t)(k.r0 + t0) * g.n + feature;
-        float d[CH];
-#pragma unroll
-        for (int j = 0; j < CH; ++j) d[j] = j < n && feature < g.n ? from[(size_t)j * g.n] : 0.f;
-#pragma unroll
-        for (int j = 0; j < CH; ++j) v[j] += d[j];
-      };
+      // a part of a cut tile: its first K block, or its last, is another cluster's
+      const bool partly = split && ((t == cut.t0 && cut.k0 > 0) || (t == cut.t1 && cut.k1 > 0));
+      if (partly) group = we >> 2;  // (every cluster's warps take the same chunks)
       // sums in parts: added up here as they are done, a part's accumulator going back at once
-      float sum[PARTS ? F32_T / 2 : 1];
+      float sum[PARTS ? F32_T / GROUPS : 1];
       bool ok = true;
-      const int parts = PARTS ? (blocks + PART_BLOCKS - 1) / PART_BLOCKS : 1;
+      const int parts = PARTS ? (blocks + PART_BLOCKS - 1) / PART_BLOCKS : blocks > 0;
+      if (PARTS && !DOWN && g.resid && f0 < limit) {  // its residual rows on their way into L2, a lane a row
+        for (int c = 0; c < F32_T / (GROUPS * CH); c += 2) {
+          const int row = (group + GROUPS * (c + lane / CH)) * CH + lane % CH;
+          if (row < k.nv)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(g.resid + (size_t)(k.r0 + row) * g.ldr + f0));
+        }
+      }
       for (int p = 0; p < parts; ++p) {
         ok = __all_sync(0xffffffffu, mbar_wait(&tmem_full[acc], acc_phase, err));
         if (!ok) break;
         tc_fence_after();
         if constexpr (PARTS) {
 #pragma unroll
-          for (int c = 0; c < F32_T / (2 * CH); ++c) {
-            const int t0 = (half + 2 * c) * CH;
+          for (int c = 0; c < F32_T / (GROUPS * CH); ++c) {
+            const int t0 = (group + GROUPS * c) * CH;
             if (t0 >= k.nv || f0 >= limit) break;
             uint32_t r[16];
             tmem_ld16(taddr + acc * acc_cols + t0, r);
@@ -406,113 +536,199 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         }
       }
       if (!ok) { failed = true; break; }
-      constexpr int UNROLL = PARTS ? F32_T / (2 * CH) : 1;  // (sum's indices are constants)
-#pragma unroll UNROLL
-      for (int c = 0; c < (PARTS ? F32_T : MAX_T) / (2 * CH); ++c) {
-        const int t0 = (half + 2 * c) * CH;
-        if (t0 >= k.nv || f0 >= limit) break;
-        float v[CH];
-        if constexpr (PARTS) {
+      int lo = 0, hi = 0;  // the clusters that hold the tile's parts
+      bool adds = false;   // this warp comes last and adds them up
+      auto part_of = [&](int c) {  // (a cluster holds two at most, one of them of a tile that begins with it)
+        return g.ws + (size_t)(c == lo ? 2 * c + 1 : 2 * c) * WS_SLOT + ((size_t)rank * EPI + we) * WS_WARP + lane;
+      };
+      if (partly) {
+        holders(t, k.e, lo, hi);
+        float* to = part_of(cluster);
+        if (f0 < limit) {
+          constexpr int UN = PARTS ? F32_T / (GROUPS * CH) : 1;
+#pragma unroll UN
+          for (int c = 0; c < (PARTS ? F32_T : MAX_T) / (GROUPS * CH); ++c) {
+            const int t0 = (group + GROUPS * c) * CH;
+            if (t0 >= k.nv) break;
+            if constexpr (PARTS) {
 #pragma unroll
-          for (int j = 0; j < CH; ++j) v[j] = sum[c * CH + j];
-        } else {
-          uint32_t r[32];
-          tmem_ld32(taddr + acc * acc_cols + t0, r);
-          tmem_ld_wait();
-          reg_fence32(r);
-#pragma unroll
-          for (int j = 0; j < CH; ++j) v[j] = __uint_as_float(r[j]);
-        }
-        const int n = k.nv - t0 < CH ? k.nv - t0 : CH;  // tokens of the chunk that exist
-        if constexpr (DOWN) {
-          const bool in = feature < g.n;  // (columns up to rp are zeros)
-          if (feature < terms.rp) {
-            const size_t row = k.r0 + t0;
-            if (g.slices > 1) {
-              float* at = g.part + ((size_t)k.f * g.rows + row) * terms.rp + feature;
-#pragma unroll
-              for (int j = 0; j < CH; ++j)
-                if (j < n) at[(size_t)j * terms.rp] = in ? v[j] * bias : 0.f;
+              for (int j = 0; j < CH; ++j) to[(c * CH + j) * 32] = blocks ? sum[c * CH + j] : 0.f;
             } else {
-              bf16* at = g.t + row * terms.cols;
+              uint32_t r[32];
+              tmem_ld32(taddr + acc * acc_cols + t0, r);
+              tmem_ld_wait();
+              reg_fence32(r);
 #pragma unroll
-              for (int j = 0; j < CH; ++j) {
-                if (j >= n) continue;
-                float x = in ? v[j] * bias : 0.f;
-                for (int s = 0; s < terms.terms; ++s) {
-                  const bf16 b = __float2bfloat16(x);
-                  at[(size_t)j * terms.cols + terms.column(s, feature)] = b;
-                  x -= __bfloat162float(b);
-                }
-              }
+              for (int j = 0; j < CH; ++j) to[(c * CH + j) * 32] = blocks ? __uint_as_float(r[j]) : 0.f;
             }
           }
-        } else if constexpr (PARTS) {
+        }
+        if (!PARTS && blocks) {  // the accumulator is read
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_relaxed_cluster(te_remote + acc * (uint32_t)sizeof(uint64_t));
+          if (++acc == n_accs) { acc = 0; acc_phase ^= 1u; }
+        }
+        __threadfence();
+        __syncwarp();
+        int* counter = g.counters + lo * ADAPTER_COUNTERS + (int)rank * EPI + we;
+        int came = 0;
+        if (lane == 0) came = atomicAdd(counter, 1);
+        adds = __shfl_sync(0xffffffffu, came, 0) == hi - lo;
+        if (adds) {
+          __threadfence();
+          if (lane == 0) *counter = 0;
+        }
+      }
+      // the results of CH tokens from t0 on
+      auto finish = [&](float* v, int t0) {
+        const int n = k.nv - t0 < CH ? k.nv - t0 : CH;  // tokens of the chunk that exist
+        const size_t row = k.r0 + t0;
+        const bool in = feature < g.n;
+        if constexpr (DOWN) {
+          {  // (columns behind the rank, and behind the last term, are zeros)
+            const int pad = terms.cols - terms.terms * terms.rp;
+            bf16* at = g.t + row * terms.cols;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+              if (j < n && feature < terms.rp) {
+                float x = in ? v[j] * bias : 0.f;
+                bf16 b = __float2bfloat16(x);
+                at[col0] = b;
+                x -= __bfloat162float(b);
+                b = __float2bfloat16(x);
+                at[col1] = b;
+                if (PARTS) at[col2] = __float2bfloat16(x - __bfloat162float(b));
+              }
+              if (j < n && feature < pad) at[terms.cols - pad + feature] = __float2bfloat16(0.f);
+              at += terms.cols;
+            }
+          }
+          return;
+        }
+        if (g.delta) {  // the low-rank part, formed by itself
+          const float* from = g.delta + row * g.n + feature;
+          float d[CH];
+#pragma unroll
+          for (int j = 0; j < CH; ++j) d[j] = j < n && in ? from[(size_t)j * g.n] : 0.f;
+#pragma unroll
+          for (int j = 0; j < CH; ++j) v[j] += d[j];
+        }
+        if constexpr (PARTS) {
           // straight to memory, 32 features of a token
-          add_delta(v, t0);
-          const size_t row = k.r0 + t0;
-          const bool in = feature < g.n;
           float rs[CH];
 #pragma unroll
           for (int j = 0; j < CH; ++j)
             rs[j] = g.resid && in && j < n ? g.resid[(row + j) * g.ldr + feature] : 0.f;
           const float gate = g.gate && in ? __ldg(g.gate + feature) : 1.f;
 #pragma unroll
-          for (int j = 0; j < CH; ++j) {
-            float x = v[j] + bias;
-            if (g.act == FB_ACT_GELU) x = gelu_f<true>(x);
-            if (!in || j >= n) continue;
-            if (g.out_type == FB_F32)
-              put(reinterpret_cast<float*>(g.out) + (row + j) * g.ldo + feature, fmaf(gate, x, rs[j]));
-            else
-              put(reinterpret_cast<bf16*>(g.out) + (row + j) * g.ldo + feature, x);
+          for (int j = 0; j < CH; ++j) v[j] += bias;
+          if (g.act == FB_ACT_GELU) {
+#pragma unroll
+            for (int j = 0; j < CH; ++j) v[j] = gelu_f<true>(v[j]);
+          }
+          if (g.out_type == FB_F32) {
+            float* at = reinterpret_cast<float*>(g.out) + row * g.ldo + feature;
+#pragma unroll
+            for (int j = 0; j < CH; ++j, at += g.ldo)
+              if (in && j < n) *at = fmaf(gate, v[j], rs[j]);
+          } else {
+            bf16* at = reinterpret_cast<bf16*>(g.out) + row * g.ldo + feature;
+#pragma unroll
+            for (int j = 0; j < CH; ++j, at += g.ldo)
+              if (in && j < n) *at = __float2bfloat16(v[j]);
           }
         } else {
-          add_delta(v, t0);
           uint8_t* tile = tiles + buf * EPI_TILE;
           buf ^= 1;
           if (elect_one()) bulk_wait_read<1>();  // the store from this tile two chunks ago
           __syncwarp();
+#pragma unroll
+          for (int j = 0; j < CH; ++j) v[j] += bias;
+          if (g.act == FB_ACT_GELU) {
+#pragma unroll
+            for (int j = 0; j < CH; j += 2) gelu_f2(v[j], v[j + 1]);
+          }
           // two tokens' values of each lane's feature as one 4-byte store per lane: lanes
           // exchange with their neighbour, even lanes then hold two features of token j, odd
           // lanes of token j + 1
           uint32_t* tw = reinterpret_cast<uint32_t*>(tile) + (lane & 1) * 16 + (lane >> 1);
 #pragma unroll
           for (int j = 0; j < CH; j += 2) {
-            float y0 = v[j] + bias, y1 = v[j + 1] + bias;
-            if (g.act == FB_ACT_GELU) gelu_f2(y0, y1);
-            const float got = __shfl_xor_sync(0xffffffffu, (lane & 1) ? y0 : y1, 1);
-            tw[j * 16] = (lane & 1) ? pack_bf16x2(got, y1) : pack_bf16x2(y0, got);
+            const float got = __shfl_xor_sync(0xffffffffu, (lane & 1) ? v[j] : v[j + 1], 1);
+            tw[j * 16] = (lane & 1) ? pack_bf16x2(got, v[j + 1]) : pack_bf16x2(v[j], got);
           }
           fence_proxy_async_smem();
           __syncwarp();
           if (elect_one()) {
 #pragma unroll
             for (int b = 0; b < CH; b += 16)
-              if (b + 16 <= n) tma_store_2d(&tmO, smem_u32(tile) + b * 64, f0, k.r0 + t0 + b);
+              if (b + 16 <= n) tma_store_2d(&maps.o, smem_u32(tile) + b * 64, f0, (int)row + b);
             bulk_commit();
           }
           if (n % 16) {  // 16 bytes at a time: n is a multiple of 8 features
             const int b = n / 16 * 16;
+#pragma unroll 1
             for (int i = lane; i < (n - b) * 4; i += 32) {
               const int tok = b + i / 4, q = i % 4;
               if (f0 + q * 8 < g.n)
-                *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(g.out) +
-                                          (size_t)(k.r0 + t0 + tok) * g.ldo + f0 + q * 8) =
-                    *reinterpret_cast<const uint4*>(tile + tok * 64 + q * 16);
+                *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(g.out) + (row + tok) * g.ldo + f0 +
+                                          q * 8) = *reinterpret_cast<const uint4*>(tile + tok * 64 + q * 16);
             }
             __syncwarp();
           }
         }
+      };
+      // The chunks one after the other, the code of one for all of them (unrolled it would not fit the
+      // instruction caches); sums in registers move up by a chunk each time.
+      constexpr int CHUNKS = (PARTS ? F32_T : MAX_T) / (GROUPS * CH);
+      if (partly) {
+#pragma unroll 1
+        for (int c = 0; adds && c < CHUNKS; ++c) {
+          const int t0 = (group + GROUPS * c) * CH;
+          if (t0 >= k.nv || f0 >= limit) break;
+          float v[CH] = {};
+#pragma unroll 2
+          for (int b = lo; b <= hi; ++b) {
+            const float* from = part_of(b) + c * CH * 32;
+            float w[CH];
+#pragma unroll
+            for (int j = 0; j < CH; ++j) w[j] = __ldcg(from + j * 32);
+#pragma unroll
+            for (int j = 0; j < CH; ++j) v[j] += w[j];
+          }
+          finish(v, t0);
+        }
+      } else {
+#pragma unroll 1
+        for (int c = 0; c < CHUNKS; ++c) {
+          const int t0 = (group + GROUPS * c) * CH;
+          if (t0 >= k.nv || f0 >= limit) break;
+          float v[CH];
+          if constexpr (PARTS) {
+#pragma unroll
+            for (int j = 0; j < CH; ++j) v[j] = sum[j];
+#pragma unroll
+            for (int j = 0; j + CH < F32_T / GROUPS; ++j) sum[j] = sum[j + CH];
+          } else {
+            uint32_t r[32];
+            tmem_ld32(taddr + acc * acc_cols + t0, r);
+            tmem_ld_wait();
+            reg_fence32(r);
+#pragma unroll
+            for (int j = 0; j < CH; ++j) v[j] = __uint_as_float(r[j]);
+          }
+          finish(v, t0);
+        }
       }
-      if constexpr (!PARTS) {
+      if (!PARTS && !partly) {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_relaxed_cluster(te_remote + acc * (uint32_t)sizeof(uint64_t));
         if (++acc == n_accs) { acc = 0; acc_phase ^= 1u; }
       }
       bias = bias_after;
-      half ^= 1;
+      group = group + 1 == GROUPS ? 0 : group + 1;
     }
     if (TILES && elect_one()) bulk_wait<0>();  // own TMA stores complete (one lane issued them all)
   }
@@ -532,33 +748,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   }
 }
 
-// t's terms from the sums of K's slices, in slice order.
-__global__ void __launch_bounds__(256) adapter_terms_kernel(const float* part, int slices, int rows,
-                                                            Terms terms, bf16* t) {
-  griddep_wait();
-  griddep_launch();
-  const size_t n = (size_t)rows * terms.rp;
-  for (size_t i = blockIdx.x * 256ull + threadIdx.x; i < n; i += gridDim.x * 256ull) {
-    float x = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < slices; ++s) x += part[s * n + i];
-    bf16* row = t + i / terms.rp * terms.cols;
-    for (int s = 0; s < terms.terms; ++s) {
-      const bf16 b = __float2bfloat16(x);
-      row[terms.column(s, (int)(i % terms.rp))] = b;
-      x -= __bfloat162float(b);
-    }
-  }
-}
-
 // ---- short segments ---------------------------------------------------------------------
 // The low-rank part of up to 16 rows of a segment, scale (x A_e^T) B_e^T in fp32, by a cluster of
 // eight CTAs: each forms its eighth of K's sums of t (mma.sync, A_e and x straight from memory into the
 // operand registers, A_e the M side), all of them add the eighths up in CTA order through distributed
 // shared memory, and each multiplies t with its eighth of B_e's rows (a feature per thread). What
 // counts is to have all of A_e and B_e on their way at once. Rows without an adapter get zeros.
-constexpr int D_CTAS = 8, D_WARPS = 8, D_THREADS = 32 * D_WARPS, D_ROWS = 16, D_RANKS = 64;
-constexpr int D_SMEM = (D_WARPS * D_RANKS * D_ROWS + 2 * FB_ADAPTER_MAX_RANK * D_ROWS) * 4;
+constexpr int D_CTAS = 8, D_WARPS = 8, D_THREADS = 32 * D_WARPS, D_ROWS = 16;
+// MT: 16 of the rank each, in one pass over K.
+template <int MT>
+size_t delta_smem(int rank) {
+  return (size_t)(D_WARPS * 16 * MT + 2 * rank) * D_ROWS * sizeof(float);
+}
 
 __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   float v;
@@ -566,14 +767,16 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   return v;
 }
 
-__global__ void __cluster_dims__(D_CTAS, 1, 1) __launch_bounds__(D_THREADS, 2)
+template <int MT>
+__global__ void __cluster_dims__(D_CTAS, 1, 1) __launch_bounds__(D_THREADS, MT == 1 ? 4 : MT == 2 ? 3 : 2)
     adapter_delta_kernel(const AdapterArgs g, float* delta, int* err) {
   griddep_wait();
   griddep_launch();
+  constexpr int D_RANKS = 16 * MT;
   extern __shared__ __align__(16) float sm[];
-  float* part = sm;                                     // [warp][64 of the rank][16 rows]
-  float* own = part + D_WARPS * D_RANKS * D_ROWS;       // [rank][16]: this CTA's sums
-  float* t = own + FB_ADAPTER_MAX_RANK * D_ROWS;        // [rank][16]: all of them
+  float* part = sm;                                // [warp][D_RANKS of the rank][16 rows]
+  float* own = part + D_WARPS * D_RANKS * D_ROWS;  // [rank][16]: this CTA's sums
+  float* t = own + g.rank * D_ROWS;                // [rank][16]: all of them
   __shared__ int found[4], scan[D_WARPS];
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   const uint32_t c = cluster_ctarank();
@@ -621,6 +824,12 @@ __global__ void __cluster_dims__(D_CTAS, 1, 1) __launch_bounds__(D_THREADS, 2)
   const int e = found[0], r0 = found[1];
   if (e == -2) return;  // (the whole cluster)
   const int rows = found[2] - r0 < D_ROWS ? found[2] - r0 : D_ROWS;
+  const int fa = (int)((int64_t)g.n * c / D_CTAS), fb = (int)((int64_t)g.n * (c + 1) / D_CTAS);
+  if (e >= 0 && tid < D_WARPS) {  // B_e's rows on their way into L2 meanwhile, an eighth a thread
+    const bf16* b = (const bf16*)g.b + ((size_t)e * g.n + fa) * g.rank;
+    const int64_t pieces = (int64_t)(fb - fa) * g.rank / 8, p0 = pieces * tid / D_WARPS, p1 = pieces * (tid + 1) / D_WARPS;
+    if (p1 > p0 && p1 - p0 < (1 << 20)) prefetch_l2_bulk(b + p0 * 8, (uint32_t)(p1 - p0) * 16);
+  }
   // ---- t: this CTA's part of K ----
   if (e >= 0) {
     const int gr = lane / 4, q = lane % 4;
@@ -692,10 +901,19 @@ __global__ void __cluster_dims__(D_CTAS, 1, 1) __launch_bounds__(D_THREADS, 2)
     cluster_sync();  // (no CTA leaves while its sums are read)
   }
   // ---- the product with this CTA's rows of B_e ----
-  const int fa = (int)((int64_t)g.n * c / D_CTAS), fb = (int)((int64_t)g.n * (c + 1) / D_CTAS);
+#pragma unroll 2
   for (int f = fa + tid; f < fb; f += D_THREADS) {
     float y[D_ROWS] = {};
-    if (e >= 0) {
+    if (e >= 0 && rows == 1) {
+      const bf16* b = (const bf16*)g.b + ((size_t)e * g.n + f) * g.rank;
+#pragma unroll 2
+      for (int r = 0; r < g.rank; r += 8) {
+        float w[8];
+        load_bf16x8(b + r, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[0] = fmaf(w[i], t[(r + i) * D_ROWS], y[0]);
+      }
+    } else if (e >= 0) {
       const bf16* b = (const bf16*)g.b + ((size_t)e * g.n + f) * g.rank;
 #pragma unroll 2
       for (int r = 0; r < g.rank; r += 8) {
@@ -835,7 +1053,7 @@ int resident_clusters(int num_sms) {
   cudaLaunchConfig_t cfg = {};
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) {
     cfg.gridDim = dim3(sms / 2 * 2, 1, 1);
-    cfg.blockDim = dim3(THREADS, 1, 1);
+    cfg.blockDim = dim3(Warps<PARTS>::THREADS, 1, 1);
     cfg.dynamicSmemBytes = SMEM_BYTES;
     if (cudaOccupancyMaxActiveClusters(&n, adapter_tc_kernel<DOWN, PARTS>, &cfg) == cudaSuccess && n > 0) {
       if (dev < DEVICES) known[dev].store(n, std::memory_order_relaxed);
@@ -847,10 +1065,11 @@ int resident_clusters(int num_sms) {
 }
 
 typedef cuuint64_t u64;
-// rows of x or t, in boxes of 64 and 8 rows
-bool row_maps(CUtensorMap* m64, CUtensorMap* m8, const void* p, u64 cols, u64 rows, u64 ld) {
-  return make_map<2>(m64, p, {cols, rows}, {ld}, {BK, 64}, true) &&
-         make_map<2>(m8, p, {cols, rows}, {ld}, {BK, 8}, true);
+// rows of x or t, in boxes of 64, 32, 16 and 8
+bool row_maps(CUtensorMap (&m)[4], const void* p, u64 cols, u64 rows, u64 ld) {
+  for (int i = 0; i < 4; ++i)
+    if (!make_map<2>(&m[i], p, {cols, rows}, {ld}, {BK, 64u >> i}, true)) return false;
+  return true;
 }
 
 template <bool DOWN, bool PARTS>
@@ -860,26 +1079,37 @@ cudaError_t launch_tc(const AdapterArgs& g, TcArgs a, const bf16* t, int* err, i
   if (e != cudaSuccess) return e;
   const u64 K = g.k, N = g.n, R = g.rank, E = g.adapters, rows = g.rows;
   const Terms terms(g.rank, PARTS);
-  CUtensorMap mw, mb{}, mx, mx8, mt{}, mt8{}, mo{};  // (zero: not used by this form)
-  bool ok = row_maps(&mx, &mx8, g.x, K, rows, g.ldx);
+  Maps m{};  // (zero: not used by this form)
+  bool ok = row_maps(m.x, g.x, K, rows, g.ldx);
   if (DOWN) {
-    ok = ok && make_map<3>(&mw, g.a, {K, R, E}, {K, R * K}, {BK, W_ROWS, 1}, true);
+    ok = ok && make_map<3>(&m.w, g.a, {K, R, E}, {K, R * K}, {BK, W_ROWS, 1}, true);
   } else {
-    ok = ok && make_map<3>(&mw, g.w, {K, N, 1}, {K, N * K}, {BK, W_ROWS, 1}, true);
+    ok = ok && make_map<3>(&m.w, g.w, {K, N, 1}, {K, N * K}, {BK, W_ROWS, 1}, true);
     if (a.adapter)
-      ok = ok && make_map<3>(&mb, g.b, {R, N, E}, {R, N * R}, {BK, W_ROWS, 1}, true) &&
-           row_maps(&mt, &mt8, t, terms.cols, rows, terms.cols);
-    if (!PARTS) ok = ok && make_map<2>(&mo, g.out, {N, rows}, {(u64)g.ldo}, {32, 16}, false);
+      ok = ok && make_map<3>(&m.b, g.b, {R, N, E}, {R, N * R}, {BK, W_ROWS, 1}, true) &&
+           row_maps(m.t, t, terms.cols, rows, terms.cols);
+    if (!PARTS) ok = ok && make_map<2>(&m.o, g.out, {N, rows}, {(u64)g.ldo}, {32, 16}, false);
   }
   if (!ok) return cudaErrorInvalidValue;
   const int occ = resident_clusters<DOWN, PARTS>(num_sms);
   const int mc = occ < num_sms / 2 ? occ : num_sms / 2;
   // no more clusters than there can be tiles: 16 rows at least each but a segment's last
-  const int n_ft = DOWN ? a.slices : (g.n + 2 * W_ROWS - 1) / (2 * W_ROWS);
+  const int n_ft = (a.n + 2 * W_ROWS - 1) / (2 * W_ROWS);
   const long long groups = a.groups < g.rows ? a.groups : g.rows;
-  const long long tiles = (g.rows / T_STEP + groups) * n_ft;
+  const long long tiles = (g.rows / T_STEP + groups) * n_ft * (a.ws ? 32 : 1);  // (cut ones in parts)
   const int clusters = tiles < mc ? (int)tiles : mc;
-  return launch_k(kern, dim3(2 * clusters), dim3(THREADS), SMEM_BYTES, st, mw, mb, mx, mx8, mt, mt8, mo, a, err);
+  return launch_k(kern, dim3(2 * clusters), dim3(Warps<PARTS>::THREADS), SMEM_BYTES, st, m, a, err);
+}
+
+template <int MT>
+cudaError_t launch_delta(const AdapterArgs& g, float* delta, int* err, cudaStream_t st) {
+  auto kern = adapter_delta_kernel<MT>;
+  const size_t smem = delta_smem<MT>(g.rank);
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)delta_smem<MT>(FB_ADAPTER_MAX_RANK));
+  if (e != cudaSuccess) return e;
+  const long long chunks = g.rows / D_ROWS + (g.segments < g.rows ? g.segments : g.rows);
+  return launch_k(kern, dim3((unsigned)(chunks * D_CTAS)), dim3(D_THREADS), smem, st, g, delta, err);
 }
 
 // How a call is computed.
@@ -887,35 +1117,36 @@ struct Plan {
   bool parts;   // sums in parts (fp32 results, very long K)
   bool by_row;  // the low-rank part formed by itself and added in the epilogue
   bool few;     // (then) the product by streamed weights
-  int slices;   // of K, for t
-  size_t t_bytes, part_bytes, delta_bytes;
+  bool cut, cut_t;  // the product's tiles, or t's, may be cut
+  size_t t_bytes, ws_bytes, delta_bytes;
 };
 size_t padded(size_t n) { return (n + 255) / 256 * 256; }
+// Whether the K blocks of all tiles, 16 units each at most, can be counted in 32 bits.
+bool fits(const AdapterArgs& g, int n_ft, const Plan& p) {
+  const double tiles = (double)(g.rows / T_STEP + g.segments) * n_ft;
+  return tiles * ((g.k + BK - 1) / BK + Terms(g.rank, p.parts).blocks()) * 16 < 4e9;
+}
 Plan plan_of(const AdapterArgs& g, int num_sms) {
   Plan p{};
   p.parts = in_parts(g);
   const int n_ft = (g.n + 2 * W_ROWS - 1) / (2 * W_ROWS);
   p.few = g.rows <= 32 && n_ft <= num_sms / 2 * (g.rows <= 8 ? 2 : 1);
   p.by_row = p.few || g.rows < 24 * g.segments;
-  p.slices = 1;
-  if (p.by_row) {
+  if (p.by_row)
     p.delta_bytes = padded((size_t)g.rows * g.n * sizeof(float));
-    return p;
-  }
-  const Terms terms(g.rank, p.parts);
-  // t has a tile of weight rows alone: K is cut so that every cluster has about two tiles, of at
-  // least eight K blocks
-  const long long tiles = g.rows / (p.parts ? 128 : 256) + g.segments, nk = (g.k + BK - 1) / BK;
-  long long s = (num_sms + tiles - 1) / tiles;
-  if (s > nk / 8) s = nk / 8;
-  p.slices = s < 1 ? 1 : s > 32 ? 32 : (int)s;
-  p.t_bytes = padded((size_t)g.rows * terms.cols * sizeof(bf16));
-  if (p.slices > 1) p.part_bytes = padded((size_t)p.slices * g.rows * terms.rp * sizeof(float));
+  else
+    p.t_bytes = padded((size_t)g.rows * Terms(g.rank, p.parts).cols * sizeof(bf16));
+  // parts of cut tiles: of t, and of the product where the tiles make few rounds
+  const long long tiles = (long long)(g.rows / MAX_T) * n_ft;
+  p.cut = !p.few && tiles < 4ll * num_sms && fits(g, n_ft, p);
+  p.cut_t = !p.by_row && fits(g, 1, p);
+  if (p.cut || p.cut_t) p.ws_bytes = num_sms / 2 * 2 * WS_SLOT * sizeof(float);
   return p;
 }
 
 template <bool PARTS>
-cudaError_t run(const AdapterArgs& g, const Plan& p, uint8_t* ws, int* err, int num_sms, cudaStream_t st) {
+cudaError_t run(const AdapterArgs& g, const Plan& p, uint8_t* ws, int* counters, int* err, int num_sms,
+                cudaStream_t st) {
   TcArgs a{};
   a.rows = g.rows;
   a.k = g.k;
@@ -930,14 +1161,15 @@ cudaError_t run(const AdapterArgs& g, const Plan& p, uint8_t* ws, int* err, int 
   a.out_type = g.out_type;
   a.ldo = g.ldo;
   a.n = g.n;
+  a.counters = counters;
+  float* parts = (float*)(ws + p.t_bytes + p.delta_bytes);
+  a.ws = p.cut ? parts : nullptr;
   cudaError_t e;
   if (p.by_row) {
     float* delta = (float*)ws;
-    e = cudaFuncSetAttribute(adapter_delta_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, D_SMEM);
-    if (e != cudaSuccess) return e;
-    const long long chunks = g.rows / D_ROWS + (g.segments < g.rows ? g.segments : g.rows);
-    e = launch_k(adapter_delta_kernel, dim3((unsigned)(chunks * D_CTAS)), dim3(D_THREADS), D_SMEM, st, g,
-                 delta, err);
+    e = g.rank <= 16   ? launch_delta<1>(g, delta, err, st)
+        : g.rank <= 32 ? launch_delta<2>(g, delta, err, st)
+                       : launch_delta<4>(g, delta, err, st);
     if (e != cudaSuccess) return e;
     if (p.few) {
       auto kern = g.rows > 8        ? adapter_few_kernel<PARTS, 2, 4, 2>
@@ -953,21 +1185,14 @@ cudaError_t run(const AdapterArgs& g, const Plan& p, uint8_t* ws, int* err, int 
   a.groups = g.segments;
   a.offsets = g.offsets;
   a.adapter = g.adapter;
-  a.slices = p.slices;
   a.t = (bf16*)ws;
-  a.part = (float*)(ws + p.t_bytes);
   a.scale = g.scale;
   a.n = g.rank;
+  a.ws = p.cut_t ? parts : nullptr;
   e = launch_tc<true, PARTS>(g, a, nullptr, err, num_sms, st);
   if (e != cudaSuccess) return e;
-  if (p.slices > 1) {
-    const Terms terms(g.rank, PARTS);
-    const long long need = ((long long)g.rows * terms.rp + 255) / 256, most = 8ll * num_sms;
-    e = launch_k(adapter_terms_kernel, dim3((unsigned)(need < most ? need : most)), dim3(256), 0, st,
-                 (const float*)a.part, p.slices, g.rows, terms, a.t);
-    if (e != cudaSuccess) return e;
-  }
   a.n = g.n;
+  a.ws = p.cut ? parts : nullptr;
   return launch_tc<false, PARTS>(g, a, a.t, err, num_sms, st);
 }
 
@@ -977,13 +1202,13 @@ cudaError_t adapter_set_wait_limit(unsigned long long ns) { return fb_set_wait_l
 
 size_t adapter_ws_bytes(const AdapterArgs& g, int num_sms) {
   const Plan p = plan_of(g, num_sms);
-  return p.t_bytes + p.part_bytes + p.delta_bytes;
+  return p.t_bytes + p.ws_bytes + p.delta_bytes;
 }
-int adapter_launches(const AdapterArgs& g, int num_sms) { return plan_of(g, num_sms).slices > 1 ? 3 : 2; }
 
-cudaError_t adapter_gemm(const AdapterArgs& g, void* ws, int* err, int num_sms, cudaStream_t st) {
+cudaError_t adapter_gemm(const AdapterArgs& g, void* ws, int* counters, int* err, int num_sms,
+                         cudaStream_t st) {
   if (num_sms < 2) return cudaErrorInvalidValue;
   const Plan p = plan_of(g, num_sms);
-  return p.parts ? run<true>(g, p, (uint8_t*)ws, err, num_sms, st)
-                 : run<false>(g, p, (uint8_t*)ws, err, num_sms, st);
+  return p.parts ? run<true>(g, p, (uint8_t*)ws, counters, err, num_sms, st)
+                 : run<false>(g, p, (uint8_t*)ws, counters, err, num_sms, st);
 }

@@ -206,6 +206,7 @@ struct fb_model {
   // launches; reset after a device error)
   float* attn_ws = nullptr;
   int* attn_flags = nullptr;
+  int* request_ctr = nullptr;  // of the calls for several requests (zero between launches, likewise)
   // scratch of the mixture-of-experts calls and of the ones for several requests, grown on demand
   uint8_t* moe_ws = nullptr;
   size_t moe_bytes = 0;
@@ -311,6 +312,7 @@ fb_status reset_errors(fb_model* m) {
                        m->st));
     CK(cudaMemsetAsync(m->attn_flags, 0, (size_t)m->dev_sms * ATTN_FLAGS_PER_CTA * sizeof(int),
                        m->st));
+    CK(cudaMemsetAsync(m->request_ctr, 0, (size_t)m->dev_sms * REQUEST_COUNTERS * sizeof(int), m->st));
     CK(cudaStreamSynchronize(m->st));
   }
   return FB_OK;
@@ -578,7 +580,7 @@ fb_status run_cross(fb_model* m, const CrossArgs& c, uint8_t* ws) {
   const double wq = (double)c.heads * c.head_dim, wk = (double)c.kv_heads * c.head_dim;
   const double keys = c.states ? (double)c.kv_rows / c.states : 0;
   KTimer t(m, FB_K_CROSS, 4.0 * wq * c.q_rows * keys, 4.0 * (wq * c.q_rows + wk * c.kv_rows));
-  CK(cross_attention(c, ws, m->attn_flags, m->derr, m->num_sms, m->st));
+  CK(cross_attention(c, ws, m->request_ctr, m->derr, m->num_sms, m->st));
   return FB_OK;
 }
 
@@ -614,8 +616,8 @@ fb_status run_adapters(fb_model* m, const AdapterArgs& g, uint8_t* ws) {
   KTimer t(m, FB_K_ADAPTER, 2.0 * r * (n * k + g.rank * (n + k)),
            2.0 * (r * k + n * k + (double)g.adapters * g.rank * (n + k)) +
                r * n * (type_bytes(g.out_type) + (g.resid ? 4 : 0)),
-           adapter_launches(g, m->num_sms));
-  CK(adapter_gemm(g, ws, m->derr, m->num_sms, m->st));
+           2);
+  CK(adapter_gemm(g, ws, m->request_ctr, m->derr, m->num_sms, m->st));
   return FB_OK;
 }
 
@@ -1520,12 +1522,14 @@ fb_status fb_init_model(const fb_cfg* cfg, const float* weights_host, fb_model**
   if ((s = dalloc_t(m, &m->sk_ws, (size_t)m->sk_clusters * SK_WS_FLOATS_PER_CLUSTER)) ||
       (s = dalloc_t(m, &m->sk_ctr, (size_t)m->sk_clusters * SK_CTR_PER_CLUSTER)) ||
       (s = dalloc_t(m, &m->attn_ws, (size_t)m->dev_sms * ATTN_WS_FLOATS_PER_CTA)) ||
-      (s = dalloc_t(m, &m->attn_flags, (size_t)m->dev_sms * ATTN_FLAGS_PER_CTA)))
+      (s = dalloc_t(m, &m->attn_flags, (size_t)m->dev_sms * ATTN_FLAGS_PER_CTA)) ||
+      (s = dalloc_t(m, &m->request_ctr, (size_t)m->dev_sms * REQUEST_COUNTERS)))
     return bail(s);
   if (cudaMemset(m->sk_ctr, 0, (size_t)m->sk_clusters * SK_CTR_PER_CLUSTER * sizeof(int)) !=
           cudaSuccess ||
       cudaMemset(m->attn_flags, 0, (size_t)m->dev_sms * ATTN_FLAGS_PER_CTA * sizeof(int)) !=
-          cudaSuccess)
+          cudaSuccess ||
+      cudaMemset(m->request_ctr, 0, (size_t)m->dev_sms * REQUEST_COUNTERS * sizeof(int)) != cudaSuccess)
     return bail(fail(FB_ECUDA, "cudaMemset failed"));
   if (m->PD % 64 == 0 && D % 128 == 0) {
     const size_t PDs = m->PD;

@@ -173,17 +173,19 @@ cudaError_t expert_gemm_set_wait_limit(unsigned long long ns);
 
 // ---- several requests in one batch (flashbon.h has the definitions) ---------------------
 struct CrossArgs : fb_cross {};  // scale filled in
-// ws: cross_ws_bytes of scratch; counters: [num_sms][8], zero between launches
+// counters of both, zero between launches: REQUEST_COUNTERS for each of the device's SMs
+constexpr int REQUEST_COUNTERS = 12;
+// ws: cross_ws_bytes of scratch
 size_t cross_ws_bytes(const CrossArgs& c, int num_sms);
 cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* err, int num_sms,
                             cudaStream_t st);
 // Sets the cross unit's device wait limit on the current device (ns).
 cudaError_t cross_set_wait_limit(unsigned long long ns);
 struct AdapterArgs : fb_adapters {};
-// ws: adapter_ws_bytes of scratch
+// ws: adapter_ws_bytes of scratch. Two launches.
 size_t adapter_ws_bytes(const AdapterArgs& g, int num_sms);
-int adapter_launches(const AdapterArgs& g, int num_sms);
-cudaError_t adapter_gemm(const AdapterArgs& g, void* ws, int* err, int num_sms, cudaStream_t st);
+cudaError_t adapter_gemm(const AdapterArgs& g, void* ws, int* counters, int* err, int num_sms,
+                         cudaStream_t st);
 // Sets the adapter unit's device wait limit on the current device (ns).
 cudaError_t adapter_set_wait_limit(unsigned long long ns);
 
