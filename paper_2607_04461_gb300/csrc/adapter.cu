@@ -24,6 +24,7 @@
 // Every wait is bounded (mbar_wait): a role that gives up records it and the kernel ends.
 #include <atomic>
 #include <climits>
+#include <type_traits>
 
 #include "grouped.cuh"
 #include "kernels.h"
@@ -580,29 +581,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<PARTS>::THREAD
           if (lane == 0) *counter = 0;
         }
       }
-      // the results of CH tokens from t0 on
-      auto finish = [&](float* v, int t0) {
-        const int n = k.nv - t0 < CH ? k.nv - t0 : CH;  // tokens of the chunk that exist
+      // The results of CH tokens from t0 on. ALL: every token and every lane's feature exists.
+      auto finish_as = [&](auto all, float* v, int t0) {
+        constexpr bool ALL = decltype(all)::value;
+        const int n = ALL || k.nv - t0 > CH ? CH : k.nv - t0;  // tokens of the chunk that exist
         const size_t row = k.r0 + t0;
-        const bool in = feature < g.n;
-        if constexpr (DOWN) {
-          {  // (columns behind the rank, and behind the last term, are zeros)
-            const int pad = terms.cols - terms.terms * terms.rp;
-            bf16* at = g.t + row * terms.cols;
+        const bool in = ALL || feature < g.n;
+        if constexpr (DOWN) {  // (columns behind the rank, and behind the last term, are zeros)
+          const int pad = terms.cols - terms.terms * terms.rp;
+          bf16* at = g.t + row * terms.cols;
 #pragma unroll
-            for (int j = 0; j < CH; ++j) {
-              if (j < n && feature < terms.rp) {
-                float x = in ? v[j] * bias : 0.f;
-                bf16 b = __float2bfloat16(x);
-                at[col0] = b;
-                x -= __bfloat162float(b);
-                b = __float2bfloat16(x);
-                at[col1] = b;
-                if (PARTS) at[col2] = __float2bfloat16(x - __bfloat162float(b));
-              }
-              if (j < n && feature < pad) at[terms.cols - pad + feature] = __float2bfloat16(0.f);
-              at += terms.cols;
+          for (int j = 0; j < CH; ++j, at += terms.cols) {
+            if (!ALL && j >= n) break;
+            if (feature < terms.rp) {
+              float x = in ? v[j] * bias : 0.f;
+              bf16 b = __float2bfloat16(x);
+              at[col0] = b;
+              x -= __bfloat162float(b);
+              b = __float2bfloat16(x);
+              at[col1] = b;
+              if (PARTS) at[col2] = __float2bfloat16(x - __bfloat162float(b));
             }
+            if (feature < pad) at[terms.cols - pad + feature] = __float2bfloat16(0.f);
           }
           return;
         }
@@ -610,33 +610,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<PARTS>::THREAD
           const float* from = g.delta + row * g.n + feature;
           float d[CH];
 #pragma unroll
-          for (int j = 0; j < CH; ++j) d[j] = j < n && in ? from[(size_t)j * g.n] : 0.f;
+          for (int j = 0; j < CH; ++j, from += g.n) d[j] = ALL || (in && j < n) ? *from : 0.f;
 #pragma unroll
           for (int j = 0; j < CH; ++j) v[j] += d[j];
         }
         if constexpr (PARTS) {
           // straight to memory, 32 features of a token
           float rs[CH];
+          if (g.resid) {
+            const float* from = g.resid + row * g.ldr + feature;
 #pragma unroll
-          for (int j = 0; j < CH; ++j)
-            rs[j] = g.resid && in && j < n ? g.resid[(row + j) * g.ldr + feature] : 0.f;
-          const float gate = g.gate && in ? __ldg(g.gate + feature) : 1.f;
+            for (int j = 0; j < CH; ++j, from += g.ldr) rs[j] = ALL || (in && j < n) ? *from : 0.f;
+          }
 #pragma unroll
           for (int j = 0; j < CH; ++j) v[j] += bias;
           if (g.act == FB_ACT_GELU) {
 #pragma unroll
             for (int j = 0; j < CH; ++j) v[j] = gelu_f<true>(v[j]);
           }
+          if (g.gate) {
+            const float gate = in ? __ldg(g.gate + feature) : 0.f;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) v[j] *= gate;
+          }
+          if (g.resid) {
+#pragma unroll
+            for (int j = 0; j < CH; ++j) v[j] += rs[j];
+          }
           if (g.out_type == FB_F32) {
             float* at = reinterpret_cast<float*>(g.out) + row * g.ldo + feature;
 #pragma unroll
             for (int j = 0; j < CH; ++j, at += g.ldo)
-              if (in && j < n) *at = fmaf(gate, v[j], rs[j]);
+              if (ALL || (in && j < n)) *at = v[j];
           } else {
             bf16* at = reinterpret_cast<bf16*>(g.out) + row * g.ldo + feature;
 #pragma unroll
             for (int j = 0; j < CH; ++j, at += g.ldo)
-              if (in && j < n) *at = __float2bfloat16(v[j]);
+              if (ALL || (in && j < n)) *at = __float2bfloat16(v[j]);
           }
         } else {
           uint8_t* tile = tiles + buf * EPI_TILE;
@@ -663,10 +673,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<PARTS>::THREAD
           if (elect_one()) {
 #pragma unroll
             for (int b = 0; b < CH; b += 16)
-              if (b + 16 <= n) tma_store_2d(&maps.o, smem_u32(tile) + b * 64, f0, (int)row + b);
+              if (ALL || b + 16 <= n) tma_store_2d(&maps.o, smem_u32(tile) + b * 64, f0, (int)row + b);
             bulk_commit();
           }
-          if (n % 16) {  // 16 bytes at a time: n is a multiple of 8 features
+          if (!ALL && n % 16) {  // 16 bytes at a time: n is a multiple of 8 features
             const int b = n / 16 * 16;
 #pragma unroll 1
             for (int i = lane; i < (n - b) * 4; i += 32) {
@@ -678,6 +688,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<PARTS>::THREAD
             __syncwarp();
           }
         }
+      };
+      auto finish = [&](float* v, int t0) {
+        if (t0 + CH <= k.nv && f0 + 32 <= g.n)
+          finish_as(std::true_type{}, v, t0);
+        else
+          finish_as(std::false_type{}, v, t0);
       };
       // The chunks one after the other, the code of one for all of them (unrolled it would not fit the
       // instruction caches); sums in registers move up by a chunk each time.
@@ -1121,6 +1137,21 @@ struct Plan {
   size_t t_bytes, ws_bytes, delta_bytes;
 };
 size_t padded(size_t n) { return (n + 255) / 256 * 256; }
+// Whether forming the low-rank part by itself is faster. In us, fitted to the figures below: it costs
+// reading A_e and B_e for every 16 rows, multiplying them by CUDA cores, and writing and reading the
+// part, and something to begin with; the K blocks of t cost every segment tiles of its own, which
+// take 313 clocks a K block however few rows they have. us by itself / as K blocks (segments x
+// rows, n x k, rank): 1536 x 1536, 16: 64 x 1 20.1 / 50.0, 64 x 32 37.1 / 50.6, 64 x 64 60.3 / 51.4,
+// 16 x 32 23.6 / 24.2, 16 x 128 36.0 / 31.1, 4 x 256 25.1 / 26.2, 1 x 1560 33.1 / 26.9; rank 64: 64 x 16
+// 44.6 / 53.3, 64 x 32 72.0 / 48.4, 1 x 64 18.7 / 15.1; 1536 x 4096, 16: 64 x 64 85.9 / 109, 16 x 128
+// 45.8 / 47.2, 1 x 1560 42.6 / 40.9; 8960 x 1536, 16: 64 x 64 172 / 208, 16 x 128 94.6 / 69.5, 1 x 64
+// 27.1 / 16.8; 1536 x 8960, 32, fp32: 16 x 128 107 / 116, 4 x 1024 198 / 145.
+bool short_segments(const AdapterArgs& g, int n_ft) {
+  const double n = g.n, k = g.k, r = g.rank, blocks = (k + BK - 1) / BK;
+  const double row = 1.1e-7 * r * n + 4e-8 * r * k + 0.003, first = n / 850 * (r / 32 + 0.5);
+  const double segment = 1.45 * n_ft * blocks * 313 / 144400;
+  return g.rows * row + first < g.segments * segment + 3.5 && g.rows * n < 1 << 28;  // (1 GB of scratch)
+}
 // Whether the K blocks of all tiles, 16 units each at most, can be counted in 32 bits.
 bool fits(const AdapterArgs& g, int n_ft, const Plan& p) {
   const double tiles = (double)(g.rows / T_STEP + g.segments) * n_ft;
@@ -1131,7 +1162,7 @@ Plan plan_of(const AdapterArgs& g, int num_sms) {
   p.parts = in_parts(g);
   const int n_ft = (g.n + 2 * W_ROWS - 1) / (2 * W_ROWS);
   p.few = g.rows <= 32 && n_ft <= num_sms / 2 * (g.rows <= 8 ? 2 : 1);
-  p.by_row = p.few || g.rows < 24 * g.segments;
+  p.by_row = p.few || short_segments(g, n_ft);
   if (p.by_row)
     p.delta_bytes = padded((size_t)g.rows * g.n * sizeof(float));
   else

@@ -320,32 +320,36 @@ class Adapters:
             assert whole_rows[:, self.out.shape[1]:].isnan().all()
 
 
+LONG = [1400, 33, 700, 5, 900], [0, 1, -1, 0, 1]  # (long enough for t as K blocks of the product)
+
+
 @pytest.mark.parametrize("out_t", [BF, F32])
 @pytest.mark.parametrize("segments,of", [
     ([1], [0]), ([1], [-1]), ([2, 1], [1, 0]), ([1] * 9, [0, 1, 2, -1, 2, 2, 0, -1, 1]), ([33], [0]),
     ([16, 17], [0, 1]), ([0, 5, 0, 0, 11, 0], [0, 1, 2, -1, 0, 1]), ([300], [0]), ([129, 1, 257], [1, -1, 0]),
     ([40] * 6, [0, 1, 2, 3, 4, 5]), ([1] * 70, list(range(70))), ([3] * 50, [i % 7 - 1 for i in range(50)]),
     ([600, 2, 2, 2], [0, 1, 0, -1]), ([2000], [0]), ([700, 900, 31], [1, 0, -1]),
+    ([1, 1500, 0, 15, 2049, 17], [0, 2, 1, 0, -1, 1]),
 ])
 def test_adapter_segments(model, out_t, segments, of):
     Adapters(segments, of, out_t=out_t, seed=len(segments)).check(model)
 
 
 @pytest.mark.parametrize("out_t", [BF, F32])
-@pytest.mark.parametrize("segments,of", [([5], [0]), ([1] * 40, [i % 3 for i in range(40)]), ([200, 150], [0, 1])])
+@pytest.mark.parametrize("segments,of", [([5], [0]), ([1] * 40, [i % 3 for i in range(40)]), ([200, 150], [0, 1]), LONG])
 @pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 64, 72, 128, 200, 256])
 def test_adapter_ranks(model, out_t, segments, of, rank):
     Adapters(segments, of, out_t=out_t, rank=rank, seed=rank).check(model)
 
 
 @pytest.mark.parametrize("out_t", [BF, F32])
-@pytest.mark.parametrize("segments,of", [([1], [0]), ([20], [0]), ([1] * 40, [i % 3 for i in range(40)]), ([260, 90], [0, 1])])
+@pytest.mark.parametrize("segments,of", [([1], [0]), ([20], [0]), ([1] * 40, [i % 3 for i in range(40)]), ([260, 90], [0, 1]), LONG])
 @pytest.mark.parametrize("N,K", [(8, 8), (8, 520), (264, 8), (1000, 1032), (136, 64), (520, 72), (2048, 4104)])
 def test_adapter_odd_sizes(model, out_t, segments, of, N, K):
     Adapters(segments, of, N=N, K=K, out_t=out_t, seed=N + K).check(model)
 
 
-@pytest.mark.parametrize("segments,of", [([1], [0]), ([7, 9], [0, -1]), ([1] * 40, [i % 4 - 1 for i in range(40)]), ([300, 140], [1, 0])])
+@pytest.mark.parametrize("segments,of", [([1], [0]), ([7, 9], [0, -1]), ([1] * 40, [i % 4 - 1 for i in range(40)]), ([300, 140], [1, 0]), LONG])
 @pytest.mark.parametrize("kw", [
     dict(act="gelu"), dict(act="gelu", out_t=F32), dict(out_t=F32, resid=True, gate=True),
     dict(out_t=F32, resid=True, gate=True, in_place=True), dict(out_t=F32, resid=True),
@@ -356,9 +360,17 @@ def test_adapter_epilogues(model, segments, of, kw):
     Adapters(segments, of, N=328, K=448, rank=16, seed=21, **kw).check(model)
 
 
+@pytest.mark.parametrize("out_t", [BF, F32])
+@pytest.mark.parametrize("N,K", [(264, 1032), (264, 4160), (1536, 2056)])
+@pytest.mark.parametrize("segments,of", [LONG, ([1300], [0]), ([80, 90, 70], [0, -1, 1]), ([3000, 1, 400], [0, 1, -1])])
+def test_adapter_cut_tiles(model, out_t, N, K, segments, of):
+    """Few tiles of a long sum, which several SM pairs share."""
+    Adapters(segments, of, N=N, K=K, rank=40, out_t=out_t, seed=26).check(model)
+
+
 def test_adapter_same_result_every_time_and_on_few_sms(model):
-    for segments, of in (([1] * 50, [i % 5 for i in range(50)]), ([400, 300, 9], [0, -1, 1]), ([6], [0])):
-        c = Adapters(segments, of, N=1536, K=1536, rank=16, seed=22)
+    for segments, of in (([1] * 50, [i % 5 for i in range(50)]), ([400, 300, 9], [0, -1, 1]), ([6], [0]), LONG):
+        c = Adapters(segments, of, N=1536, K=1544, rank=16, seed=22)
         c.check(model)
         first = c.out.clone()
         fb.fb_set_op_repeat(model.handle, 3)
@@ -385,9 +397,9 @@ def test_adapter_on_another_stream(model):
         model.set_stream(None)
 
 
-@pytest.mark.parametrize("rows", [4, 40, 400])
+@pytest.mark.parametrize("rows", [4, 40, 400, 4000])
 @pytest.mark.parametrize("at,of", [
-    ([0, 3, 2], [0, 0]), ([1, 2, 3], [0, 0]), ([0, 3, 5000], [0, 0]), ([0, 2, 4], [0, 2]), ([0, 2, 4], [-2, 0]),
+    ([0, 3, 2], [0, 0]), ([1, 2, 3], [0, 0]), ([0, 3, 50000], [0, 0]), ([0, 2, 4], [0, 2]), ([0, 2, 4], [-2, 0]),
     ([0, -1, 4], [0, 0]), ([0, 2, -4], [0, 0]),
 ])
 def test_adapter_bad_segments(model, rows, at, of):
