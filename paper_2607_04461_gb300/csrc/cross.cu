@@ -5,9 +5,12 @@
 // One persistent kernel on tcgen05, one CTA per SM. A tile is 128 rows of (query, head): with
 // G = heads / kv_heads, RQ = 128 / G consecutive queries (rounded down) by the G heads that share
 // a kv head (one TMA box of three dimensions), so K and V are read once for all of them, for one
-// token as for many. An item is a pair of query tiles of one sequence and kv head (the last one
-// may be single); its two tiles share each 128-key tile of K and V. Both lengths come from device
-// memory: every CTA adds up the items' costs and takes an equal share of them (see Plan).
+// token as for many. An item is a pair of query tiles of one sequence and kv head, which share each
+// 128-key tile of K and V (the last one may be single), or, where a sequence has one query tile and
+// there are more such than SMs, a pair of kv heads side by side (dual), which keeps twice as much of
+// K and V on its way. Both lengths come from device memory: the CTAs draw whole items from a counter,
+// or take an equal stretch each of all items' key tiles where whole ones would leave SMs idle (see
+// Plan).
 //  * warp 0: TMA. Lane 0 loads Q and a ring of K tiles, lane 1 a ring of V tiles.
 //  * warp 1: MMA issuer. S_g = Q_g K^T (both K-major in shared memory), then O_g += P_g V (P from
 //    TMEM, V MN-major); the order PV_A(j), S_A(j+1), PV_B(j), S_B(j+1) lets each group's softmax run
@@ -23,6 +26,15 @@
 //  * warp 11: fetches the CTA's segments (whole items, parts of cut ones), one ahead.
 // The last key tile's MMAs cover ceil16 of its keys. Every wait is bounded (mbar_wait): a role
 // that gives up records it and the kernel ends.
+//
+// Bounds: with many queries for each key the tensor pipe and the exponentials, 2 x 128 x 128 of both
+// in about 2600 clocks (32 candidates of 1560 rows, 12 heads of 128: 161 us, 0.98 PFLOP/s, for 512 shared
+// keys, 419 us, 1.14 PFLOP/s, for 1560 own ones; 4096 rows on 8191 keys in cut items: 151 us, 1.37), with
+// tokens on long states the bytes of K and V (64 requests, 4 kv heads of 128, 32 to 4096 keys, 92 MB:
+// 32.5 us, of which 22 stream K and V at the rate of a copy; 38 us with one kv head at a time). What
+// is left beside them: 4 to 5 us from launch to the first scores, 3000 to 4000 clocks of an item's end in
+// which the next one's scores wait for the rows' stores (which take as long in 128-byte pieces, and
+// through shared memory and TMA with a ring of two K tiles), and the joining of cut items.
 #include <cudaTypedefs.h>
 
 #include <cfloat>
@@ -37,7 +49,7 @@ constexpr int THREADS = 384;
 constexpr uint32_t TMEM_COLS = 512;  // S|P of A [0,128), of B [128,256), O of A [256, ..), of B [384, ..)
 constexpr uint32_t O_COL = 256;
 constexpr int SEGS = 2;             // ring of segments: the current one and one ahead
-constexpr int MASKS = 8;             // ring of key tiles' masks (> V slots + 1: see the mask warp)
+constexpr int MASKS = 8;             // ring of key tiles' masks (> V slots + 2: see the mask warp)
 
 template <int D>
 struct Shape {
@@ -45,14 +57,17 @@ struct Shape {
   static constexpr int KS = D == 128 ? 3 : 6, VS = D == 128 ? 2 : 5;  // ring slots (KS >= VS)
   static constexpr int RING = (2 + KS + VS) * TILE;
   static constexpr int SMEM = RING + 512;                 // + barriers and masks
-  static constexpr int WS_WARP = 32 * D + 64;             // floats of a warp's part: rows, (m, l)
-  static_assert(KS >= VS && MASKS > VS + 1, "rings");
+  static_assert(KS >= VS && MASKS > VS + 2, "rings");
 };
+
+// floats of a warp's part: rows, (m, l)
+__host__ __device__ constexpr int part_floats(int D) { return 32 * D + 64; }
 
 struct Params {
   const int32_t *q_off, *kv_off, *kv_of;
   const uint8_t* valid;
   int seqs, states, q_rows, kv_rows, kv_heads, group, rq;
+  bool dual;       // two kv heads side by side where a sequence has one query tile
   bool flat;       // every item costs 1 (sizes whose costs would pass 32 bits)
   bf16* O;
   int64_t ldo;
@@ -154,19 +169,31 @@ __device__ __forceinline__ void load_seq(const Params& p, int s, Seq& q) {
     q = Seq{0, 0, 0, 0};
   }
 }
-// Costs in quarters of what a key tile takes for two query tiles (1.2 us): 3 for one query tile, 4
-// for an item's start and end. Items stand in a row: per sequence, per kv head, the pairs of query
-// tiles; a position u in the row is a sum of costs.
+// The items of a sequence: `heads` times `tiles` in pairs (the last one may be single). With several
+// query tiles: its kv heads, and the query tiles, a pair of which shares each tile of K and V. With one
+// (`dual`): once, and the kv heads, two of which run side by side on their own tiles of K and V.
+// Costs are in quarters of what a key tile takes for two query tiles (1.2 us): 3 for one query tile, 5
+// for two kv heads, 4 for an item's start and end. Items stand in a row, sequence by sequence; a
+// position u in the row is a sum of costs.
 struct Cost {
-  int tiles, n_kv;         // query tiles and key tiles of the sequence
-  u32 pair, single, head;  // an item of two tiles, of one, all of a kv head
+  int heads, tiles, n_kv;
+  bool dual;
+  u32 w, pair, single, head;  // a key tile of a pair; an item of a pair, of one, all of a head
   __device__ __forceinline__ Cost(const Params& p, const Seq& q) {
     tiles = (q.nq + p.rq - 1) / p.rq;
+    dual = p.dual && tiles == 1 && p.kv_heads > 1;
+    heads = dual ? 1 : p.kv_heads;
+    if (dual) tiles = p.kv_heads;
     n_kv = (q.nk + TB - 1) / TB;
-    pair = p.flat ? 1 : 4u * n_kv + 4;
+    w = dual ? 5 : 4;
+    pair = p.flat ? 1 : w * n_kv + 4;
     single = p.flat ? 1 : 3u * n_kv + 4;
     head = (u32)(tiles / 2) * pair + (tiles & 1 ? single : 0);
   }
+  __device__ __forceinline__ u32 all() const { return head * heads; }
+  __device__ __forceinline__ u32 items() const { return (u32)((tiles + 1) / 2) * heads; }
+  __device__ __forceinline__ bool two(int t) const { return 2 * t + 1 < tiles; }
+  __device__ __forceinline__ u32 weight(int t) const { return two(t) ? w : 3; }
 };
 // Whole items are handed out as CTAs become free (a counter; what an item gives does not depend on
 // who works on it), in the row's order, so that the CTAs work on neighbours, which share K and V
@@ -175,20 +202,30 @@ struct Cost {
 // and the one that comes last adds them up in CTA order.
 struct Plan {
   bool cut;
-  u64 units, ctas;  // all costs, the CTAs that work on cut items
-  // cut: where this CTA's stretch begins (an item's sequence, kv head (kv_heads: go on to the next
+  u32 units, ctas;  // all costs, the CTAs that work on cut items
+  // cut: where this CTA's stretch begins (an item's sequence, head (behind the last: go on to the next
   // sequence), pair, position and the key tile in it) and ends
   int s, h, t, j;
   u32 u, end;
   Seq q;
 };
+// Where CTA c's stretch begins: floor(c units / ctas).
+__device__ __forceinline__ u32 stretch_at(u32 c, u32 units, u32 ctas) {
+  const u32 q = units / ctas;
+  return q * c + (units - q * ctas) * c / ctas;
+}
 // The CTAs lo .. hi that hold parts of a cut item of n_kv key tiles at u0, each costing w: a CTA's
 // beginning is moved to the item's where it lies before its third key tile, to its end where it
-// lies in the last one (see begin_at); CTA c begins at floor(c units / ctas).
+// lies in the last one (see begin_at).
 __device__ __forceinline__ void holders(const Plan& pl, u32 u0, int n_kv, u32 w, int& lo, int& hi) {
-  auto from = [&](u64 y) { return (int)((y * pl.ctas + pl.units - 1) / pl.units); };  // first c at y or behind
+  const u32 most = pl.units / pl.ctas + 1;
+  auto from = [&](u32 y) {  // the first CTA that begins at y or behind
+    u32 c = y / most;
+    while (stretch_at(c, pl.units, pl.ctas) < y) ++c;
+    return (int)c;
+  };
   lo = from(u0 + 4 + 2 * w) - 1;
-  hi = from(u0 + 4 + (u64)(n_kv - 1) * w) - 1;
+  hi = from(u0 + 4 + (u32)(n_kv - 1) * w) - 1;
 }
 // Position x within a sequence, which begins at u_s, moved to where a stretch may begin: key tile j
 // of the item that x lies in, or the next item. Returns the position of that.
@@ -199,13 +236,12 @@ __device__ __forceinline__ u32 begin_at(const Cost& c, u32 u_s, u32 x, int& h, i
   t = (int)(v / c.pair);
   if (t > c.tiles / 2) t = c.tiles / 2;
   v -= t * c.pair;  // within the item
-  const bool two = 2 * t + 1 < c.tiles;
-  const u32 w = two ? 4 : 3;
+  const u32 w = c.weight(t);
   u = x - v;
   j = v < 4 ? 0 : (int)((v - 4) / w);
   if (c.n_kv - j < 2 && v >= 4) {
     j = 0;
-    u += two ? c.pair : c.single;
+    u += c.two(t) ? c.pair : c.single;
     if (2 * ++t >= c.tiles) {
       t = 0;
       ++h;
@@ -227,8 +263,8 @@ __device__ __forceinline__ Seq make_plan(const Params& p, Plan* plan, uint3* sca
   for (int s = s0; s < s1; ++s) {
     load_seq(p, s, q);
     const Cost c(p, q);
-    sum += c.head * p.kv_heads;
-    n += (u32)((c.tiles + 1) / 2) * p.kv_heads;
+    sum += c.all();
+    n += c.items();
     const u32 most = c.tiles > 1 ? c.pair : c.tiles ? c.single : 0;
     big = most > big ? most : big;
   }
@@ -274,14 +310,14 @@ __device__ __forceinline__ Seq make_plan(const Params& p, Plan* plan, uint3* sca
     if (!work) plan->u = 0;
   }
   for (u32 e = 0; work && cut && e < 2; ++e) {  // this CTA's stretch, and the next one's
-    const u32 x = (u32)((u64)(c + e) * total / ctas);
+    const u32 x = stretch_at(c + e, total, ctas);
     if (x < at || x - at >= sum) continue;
     int s = s0, h, t, j;
     u32 u_s = at, u;
     if (per > 1) {
       for (;; ++s) {
         load_seq(p, s, q);
-        const u32 all = Cost(p, q).head * p.kv_heads;
+        const u32 all = Cost(p, q).all();
         if (x - u_s < all) break;
         u_s += all;
       }
@@ -309,23 +345,26 @@ struct __align__(16) Seg {
   int key, keys;     // first key, keys from there to the states' end
   int h, last;       // kv head; whether the states end with this segment
   int whole, lo, hi; // a whole item, or a part of one that CTAs lo .. hi share
-  int pad;
+  int dual;          // two kv heads, h and h + 1, of one query tile
 };
-__device__ __forceinline__ void fill(const Params& p, const Plan& pl, const Seq& q, int n_kv, int h, int t,
-                                     bool two, int j0, int j1, u32 u, Seg& g) {
+// Key tiles j0 .. j1 - 1 of item (h, t) at u
+__device__ __forceinline__ void fill(const Params& p, const Plan& pl, const Seq& q, const Cost& c, int h, int t,
+                                     int j0, int j1, u32 u, Seg& g) {
+  const int first = c.dual ? 0 : 2 * t * p.rq;  // query
   g.steps = j1 - j0;
-  g.ng = two ? 2 : 1;
-  g.row = q.q0 + 2 * t * p.rq;
-  g.left = q.nq - 2 * t * p.rq;
+  g.ng = c.two(t) ? 2 : 1;
+  g.dual = c.dual && c.two(t);
+  g.h = c.dual ? 2 * t : h;
+  g.row = q.q0 + first;
+  g.left = q.nq - first;
   g.key = q.k0 + j0 * TB;
   g.keys = q.nk - j0 * TB;
-  g.h = h;
-  g.last = j1 == n_kv;
+  g.last = j1 == c.n_kv;
   g.whole = j0 == 0 && g.last;
   g.lo = g.hi = 0;
-  if (!g.whole) holders(pl, u, n_kv, two ? 4 : 3, g.lo, g.hi);
+  if (!g.whole) holders(pl, u, c.n_kv, c.weight(t), g.lo, g.hi);
 }
-// The segments of a CTA's stretch (one thread).
+// The segments of a CTA's stretch.
 struct Stretch {
   int s, h, t, j;
   u32 u, end;
@@ -334,15 +373,15 @@ struct Stretch {
       : s(pl.s), h(pl.h), t(pl.t), j(pl.j), u(pl.u), end(pl.end), q(pl.q) {}
   __device__ __forceinline__ bool next(const Params& p, const Plan& pl, Seg& g) {
     if (u >= end) return false;
-    if (h >= p.kv_heads) {  // the next sequence with queries (there is one: u < end)
+    Cost c(p, q);
+    if (h >= c.heads) {  // the next sequence with queries (there is one: u < end)
       h = 0;
       do load_seq(p, ++s, q);
       while (q.nq == 0);
+      c = Cost(p, q);
     }
-    const Cost c(p, q);
-    const bool two = 2 * t + 1 < c.tiles;
-    const u32 cost = two ? c.pair : c.single;
-    fill(p, pl, q, c.n_kv, h, t, two, j, end - u < cost ? (int)((end - u - 4) / (two ? 4 : 3)) : c.n_kv, u, g);
+    const u32 cost = c.two(t) ? c.pair : c.single;
+    fill(p, pl, q, c, h, t, j, end - u < cost ? (int)((end - u - 4) / c.weight(t)) : c.n_kv, u, g);
     j = 0;
     u += cost;
     if (2 * ++t >= c.tiles) {
@@ -356,10 +395,9 @@ struct Stretch {
 struct Items {
   int s0 = -32;       // the sequences at hand
   u32 end = 0;        // first item behind them
-  Seq q;              // this lane's sequence, its first item, pairs of query tiles, query tiles
+  Seq q;              // this lane's sequence, and its first item
   bool have;          // (q is that of the first 32 already)
   u32 first = 0;
-  int pairs = 1, tiles = 0;
   __device__ __forceinline__ Items(bool have_, const Seq& q_) : q(q_), have(have_) {}
   __device__ __forceinline__ bool find(const Params& p, const Plan& pl, u32 i, int lane, Seg& g) {
     while (i >= end) {
@@ -369,9 +407,7 @@ struct Items {
       u32 n = 0;
       if (s < p.seqs) {
         if (!have) load_seq(p, s, q);
-        tiles = (q.nq + p.rq - 1) / p.rq;
-        pairs = (tiles + 1) / 2;
-        n = (u32)pairs * p.kv_heads;
+        n = Cost(p, q).items();
       }
       u32 upto = n;
 #pragma unroll
@@ -389,10 +425,10 @@ struct Items {
     o.nq = __shfl_sync(0xffffffffu, q.nq, of);
     o.k0 = __shfl_sync(0xffffffffu, q.k0, of);
     o.nk = __shfl_sync(0xffffffffu, q.nk, of);
-    const u32 k = i - __shfl_sync(0xffffffffu, first, of);
-    const u32 per = __shfl_sync(0xffffffffu, pairs, of);
-    const int h = (int)(k / per), t = (int)(k - h * per), n_kv = (o.nk + TB - 1) / TB;
-    fill(p, pl, o, n_kv, h, t, 2 * t + 1 < __shfl_sync(0xffffffffu, tiles, of), 0, n_kv, 0, g);
+    const Cost c(p, o);
+    const u32 k = i - __shfl_sync(0xffffffffu, first, of), per = (u32)(c.tiles + 1) / 2;
+    const int h = (int)(k / per), t = (int)(k - h * per);
+    fill(p, pl, o, c, h, t, 0, c.n_kv, 0, g);
     return true;
   }
 };
@@ -426,19 +462,28 @@ __device__ __forceinline__ void store32(bf16* to, bool st32, const uint32_t* u, 
 // that begins with it one that is not its stretch's first.
 template <int D>
 __device__ __forceinline__ float* part_of(const Params& p, int lo, int c, int ww) {
-  return p.ws + ((size_t)(c == lo ? 2 * c + 1 : 2 * c) * 8 + ww) * Shape<D>::WS_WARP;
+  return p.ws + ((size_t)(c == lo ? 2 * c + 1 : 2 * c) * 8 + ww) * part_floats(D);
 }
 // Adds up the parts of CTAs lo .. hi for a warp's `live` rows, in CTA order, and stores them. out:
 // this lane's row.
 template <int D>
 __device__ __forceinline__ void join(const Params& p, int lo, int hi, int ww, int lane, int live, bf16* out) {
-  float m = -FLT_MAX, l = 0.f;
-#pragma unroll 4
-  for (int c = lo; c <= hi; ++c) m = fmaxf(m, __ldcg(part_of<D>(p, lo, c, ww) + 32 * D + 2 * lane));
-#pragma unroll 4
-  for (int c = lo; c <= hi; ++c) {
-    const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_of<D>(p, lo, c, ww) + 32 * D) + lane);
-    l += ml.y * ex2(ml.x - m);
+  float m = -FLT_MAX, l = 0.f;  // of this lane's row, eight parts at a time
+#pragma unroll 1
+  for (int c0 = lo; c0 <= hi; c0 += 8) {
+    float2 ml[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      ml[i] = c0 + i <= hi
+                  ? __ldcg(reinterpret_cast<const float2*>(part_of<D>(p, lo, c0 + i, ww) + 32 * D) + lane)
+                  : make_float2(-FLT_MAX, 0.f);
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
+    l *= ex2(m - top);
+    m = top;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) l += ml[i].y * ex2(ml[i].x - m);
   }
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
   if (live > 8) {  // a lane its row, 32 columns at a time
@@ -468,31 +513,55 @@ __device__ __forceinline__ void join(const Params& p, int lo, int hi, int ww, in
     }
     return;
   }
-  // few rows: a lane four columns, four parts of a row (D 64: of two) at a time
+  // few rows: a lane four columns (D 64: of every other row); four parts of up to four (eight) rows
+  // on their way
   constexpr int GROUPS = D / 4, AT = 32 / GROUPS;
-  const int cg = lane % GROUPS;
-  for (int r0 = 0; r0 < live; r0 += AT) {
-    const int row = r0 + lane / GROUPS;
-    const float mr = __shfl_sync(0xffffffffu, m, row), ir = __shfl_sync(0xffffffffu, inv, row);
-    bf16* to = reinterpret_cast<bf16*>(__shfl_sync(0xffffffffu, reinterpret_cast<u64>(out), row));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int c = lo; c <= hi; ++c) {
-      const float* from = part_of<D>(p, lo, c, ww);
-      const float f = ex2(__ldcg(from + 32 * D + 2 * row) - mr);
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(from) + cg * 32 + row);
-      acc.x += f * v.x;
-      acc.y += f * v.y;
-      acc.z += f * v.z;
-      acc.w += f * v.w;
+  const int cg = lane % GROUPS, sub = lane / GROUPS;
+#pragma unroll 1
+  for (int r0 = 0; r0 < live; r0 += 4 * AT) {
+    float4 acc[4] = {};
+#pragma unroll 1
+    for (int c0 = lo; c0 <= hi; c0 += 4) {
+      float f[4];
+      float4 v[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = c0 + i <= hi;
+        const float* from = part_of<D>(p, lo, in ? c0 + i : hi, ww);
+        f[i] = in ? __ldcg(from + 32 * D + 2 * lane) : -INFINITY;  // (of this lane's row)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          v[i][r] = __ldcg(reinterpret_cast<const float4*>(from) + cg * 32 + ((r0 + r * AT + sub) & 31));
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[i] = ex2(f[i] - m);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float fr = __shfl_sync(0xffffffffu, f[i], (r0 + r * AT + sub) & 31);
+          if (fr != 0.f) {  // (rows behind the live ones may hold anything)
+            acc[r].x += fr * v[i][r].x;
+            acc[r].y += fr * v[i][r].y;
+            acc[r].z += fr * v[i][r].z;
+            acc[r].w += fr * v[i][r].w;
+          }
+        }
+      }
     }
-    if (row < live)
-      *reinterpret_cast<uint2*>(to + cg * 4) =
-          make_uint2(pack_bf16x2(acc.x * ir, acc.y * ir), pack_bf16x2(acc.z * ir, acc.w * ir));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = (r0 + r * AT + sub) & 31;
+      const float ir = __shfl_sync(0xffffffffu, inv, row);
+      bf16* to = reinterpret_cast<bf16*>(__shfl_sync(0xffffffffu, reinterpret_cast<u64>(out), row));
+      if (r0 + r * AT + sub < live)
+        *reinterpret_cast<uint2*>(to + cg * 4) = make_uint2(pack_bf16x2(acc[r].x * ir, acc[r].y * ir),
+                                                            pack_bf16x2(acc[r].z * ir, acc[r].w * ir));
+    }
   }
 }
 
-template <int D, bool MASKED>
+// DUAL: p.dual
+template <int D, bool MASKED, bool DUAL>
 __global__ void __launch_bounds__(THREADS, 1)
     cross_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const Params p) {
@@ -505,7 +574,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint8_t* Qs = smem;
   uint8_t* Ks = smem + 2 * TILE;
   uint8_t* Vs = Ks + KS * TILE;
-  uint64_t* q_full = reinterpret_cast<uint64_t*>(Vs + VS * TILE);
+  uint64_t* q_full = reinterpret_cast<uint64_t*>(smem + Shape<D>::RING);
   uint64_t* q_empty = q_full + 2;   // [2 query tiles], as q_full
   uint64_t* k_full = q_empty + 2;   // [KS]
   uint64_t* k_empty = k_full + KS;  // [KS]
@@ -518,7 +587,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* p_full = s_full + 2;
   uint64_t* o_done = p_full + 2;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(o_done + 2);
-  uint4* masks = reinterpret_cast<uint4*>(Vs + VS * TILE + 512 - 16 * MASKS);  // [MASKS]
+  uint4* masks = reinterpret_cast<uint4*>(smem + Shape<D>::RING + 512 - 16 * MASKS);  // [MASKS]
   static_assert(8 * (4 + 2 * KS + 2 * VS + MASKS + 2 * SEGS + 6) + 8 <= 512 - 16 * MASKS, "barriers");
   __shared__ Plan plan;
   __shared__ uint3 scan[THREADS / 32];
@@ -567,52 +636,59 @@ __global__ void __launch_bounds__(THREADS, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
 
+  auto is_dual = [](const Seg& sg) { return DUAL && sg.dual; };
   uint32_t seg = 0;  // segments that this role has come to
   if (warp == 0) {
     // ---------------- TMA: lane 0 Q and K, lane 1 V ----------------
     if (lane < 2) {
       const uint32_t q_bytes = (uint32_t)(SUBS * 128 * p.group * p.rq);
-      uint32_t t = 0, qph = 0;  // key tiles; phases of the query tiles (bits)
+      // key tiles; phases of the query tiles; which of the last key tiles were of two heads (bits)
+      uint32_t t = 0, qph = 0, was_dual = 0;
       for (;; ++seg) {
         if (!mbar_wait(&g_full[seg % SEGS], (seg / SEGS) & 1, err)) { failed = true; break; }
         const Seg sg = segs[seg % SEGS];
         mbar_arrive(&g_empty[seg % SEGS]);
         if (sg.steps < 0) break;
+        // (dual: tiles of the two kv heads by turns)
+        const int tiles = is_dual(sg) ? 2 * sg.steps : sg.steps;
         if (lane == 0) {
-          for (int i = 0; i < sg.steps; ++i, ++t) {
-            const int s = t % KS;
+          for (int i = 0; i < tiles; ++i, ++t) {
+            const int s = t % KS, h = is_dual(sg) ? sg.h + (i & 1) : sg.h, j = is_dual(sg) ? i >> 1 : i;
             if (!mbar_wait(&k_empty[s], ((t / KS) & 1) ^ 1u, err)) { failed = true; break; }
             mbar_expect_tx(&k_full[s], TILE);
             for (int c = 0; c < SUBS; ++c)
-              tma_load_2d(Ks + s * TILE + c * SUB, &tmK, &k_full[s], sg.h * D + c * 64, sg.key + i * TB);
+              tma_load_2d(Ks + s * TILE + c * SUB, &tmK, &k_full[s], h * D + c * 64, sg.key + j * TB);
             if (i == 0) {
               for (int g = 0; g < sg.ng; ++g) {
                 if (!mbar_wait(&q_empty[g], ((qph >> g) & 1) ^ 1u, err)) { failed = true; break; }
                 qph ^= 1u << g;
                 mbar_expect_tx(&q_full[g], q_bytes);
                 for (int c = 0; c < SUBS; ++c)
-                  tma_load_3d(Qs + g * TILE + c * SUB, &tmQ, &q_full[g], c * 64, sg.h * p.group,
-                              sg.row + g * p.rq);
+                  tma_load_3d(Qs + g * TILE + c * SUB, &tmQ, &q_full[g], c * 64,
+                              (is_dual(sg) ? sg.h + g : sg.h) * p.group,
+                              is_dual(sg) ? sg.row : sg.row + g * p.rq);
               }
               if (failed) break;
             }
           }
         } else {
-          for (int i = 0; i < sg.steps; ++i, ++t) {
-            const int s = t % VS;
-            // slot s last held tile t - VS; its PV MMAs are done once the S MMAs of the tile after
-            // it are (the issuer issues those after them), which is when that tile's K slot is
-            // released (K and V tiles are counted alike)
+          for (int i = 0; i < tiles; ++i, ++t) {
+            const int s = t % VS, h = is_dual(sg) ? sg.h + (i & 1) : sg.h, j = is_dual(sg) ? i >> 1 : i;
+            // Slot s last held tile t - VS; its PV MMAs are done once S MMAs that the issuer issued
+            // behind them are, which is when that tile's K slot is released (K and V tiles are counted
+            // alike): those of the tile after it, or of the second one after it where either is one
+            // head's of two.
             if (t >= VS) {
-              const uint32_t a = t - VS + 1;
+              const uint32_t a = t - VS + (DUAL && ((was_dual >> (VS - 2)) & 3) ? 2 : 1);
               if (!mbar_wait(&k_empty[a % KS], (a / KS) & 1, err)) { failed = true; break; }
             } else if (t == 0) {  // the first K and Q come before everything else
               if (!mbar_wait(&k_full[0], 0, err)) { failed = true; break; }
             }
-            uint64_t* bar = MASKED || (sg.keys - i * TB < TB && sg.keys % 16) ? &v_land[s] : &v_full[s];
+            was_dual = was_dual << 1 | (uint32_t)is_dual(sg);
+            uint64_t* bar = MASKED || (sg.keys - j * TB < TB && sg.keys % 16) ? &v_land[s] : &v_full[s];
             mbar_expect_tx(bar, TILE);
             for (int c = 0; c < SUBS; ++c)
-              tma_load_2d(Vs + s * TILE + c * SUB, &tmV, bar, sg.h * D + c * 64, sg.key + i * TB);
+              tma_load_2d(Vs + s * TILE + c * SUB, &tmV, bar, h * D + c * 64, sg.key + j * TB);
           }
         }
         if (failed) break;
@@ -626,7 +702,15 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t idesc_pv = idesc_s | (1u << 16) | ((uint32_t)(D >> 3) << 17);
     const uint32_t q_lo[2] = {desc_lo_k(smem_u32(Qs)), desc_lo_k(smem_u32(Qs + TILE))};
     const uint32_t k_lo = desc_lo_k(smem_u32(Ks)), v_lo = desc_lo_mn(smem_u32(Vs), SUB);
-    uint32_t ks = 0, kph = 0, vs = 0, vph = 0;  // K and V slots and phases
+    uint32_t ks = 0, kph = 0, vs = 0, vph = 0;  // the next K and V tiles: slots and phases
+    auto next_k = [&] {
+      kph ^= ks + 1 == KS;
+      ks = ks + 1 == KS ? 0 : ks + 1;
+    };
+    auto next_v = [&] {
+      vph ^= vs + 1 == VS;
+      vs = vs + 1 == VS ? 0 : vs + 1;
+    };
     uint32_t pph[2] = {0u, 0u}, qph[2] = {0u, 0u};
     bool ok = true;
     // short_: the states' last key tile, of n16 < 8 sixteens of keys
@@ -665,13 +749,14 @@ __global__ void __launch_bounds__(THREADS, 1)
     // the next segment's steps, sixteens of its last tile, tiles
     int steps = 0;
     uint32_t n16 = 8;
-    bool some = false, two = false, ends_short = false;
+    bool some = false, two = false, dual = false, ends_short = false;
     auto fetch = [&] {
       if (!mbar_wait_warp(&g_full[seg % SEGS], (seg / SEGS) & 1, err)) return false;
       const Seg& sg = segs[seg % SEGS];
       steps = sg.steps;
       n16 = sg.last ? (uint32_t)(sg.keys - (steps - 1) * TB + 15) / 16 : 8u;
       two = __all_sync(0xffffffffu, sg.ng == 2);
+      dual = DUAL && __all_sync(0xffffffffu, sg.dual != 0);
       some = __all_sync(0xffffffffu, steps > 0);
       ends_short = __all_sync(0xffffffffu, n16 < 8);
       __syncwarp();
@@ -679,26 +764,30 @@ __global__ void __launch_bounds__(THREADS, 1)
       ++seg;
       return true;
     };
+    // S of group g in the next K slot; a group's first of a segment waits for its Q
+    auto next_s = [&](int g, bool first, bool short_, uint32_t sixteens) {
+      if (!mbar_wait_warp(&k_full[ks], kph, err)) return false;
+      if (first) {
+        if (!mbar_wait_warp(&q_full[g], qph[g], err)) return false;
+        qph[g] ^= 1u;
+      }
+      tc_fence_after();
+      if (elect_one()) issue_s(g, ks, short_, sixteens);
+      return true;
+    };
     ok = fetch();
     if (ok && some) {
-      const bool only = __all_sync(0xffffffffu, steps == 1);
-      ok = mbar_wait_warp(&k_full[0], 0, err) && mbar_wait_warp(&q_full[0], 0, err);
-      if (ok && two) ok = mbar_wait_warp(&q_full[1], 0, err);
-      if (ok) {
-        tc_fence_after();
-        if (elect_one()) {
-          issue_s(0, 0, only && ends_short, n16);
-          if (two) issue_s(1, 0, only && ends_short, n16);
-        }
-        qph[0] = 1u;
-        qph[1] = two ? 1u : 0u;
-      }
+      const bool s_short = __all_sync(0xffffffffu, steps == 1) && ends_short;
+      ok = next_s(0, true, s_short, n16);
+      if (ok && dual) next_k();
+      if (ok && two) ok = next_s(1, true, s_short, n16);
+      next_k();
     }
-    // A key tile at a time: its PV, and S of the one after it, which may be the next segment's first
-    // (its Q has been on its way since this segment's last S).
+    // A key tile (dual: a tile of either head) at a time: its PV, and S of the one after it, which may
+    // be the next segment's first (its Q has been on its way since this segment's last S).
     int left = steps;
     uint32_t x16 = n16;
-    bool more = some, x_two = two, x_ends_short = ends_short, x_first = true;
+    bool more = some, x_two = two, x_dual = dual, x_ends_short = ends_short, x_first = true;
     while (ok && more) {
       const bool end = __all_sync(0xffffffffu, left == 1);
       const bool x_short = end && x_ends_short;
@@ -708,20 +797,19 @@ __global__ void __launch_bounds__(THREADS, 1)
         more = some;
         y_short = __all_sync(0xffffffffu, steps == 1) && ends_short;
       }
-      const bool y_two = more && (end ? two : x_two);
+      const bool y_two = more && (end ? two : x_two), y_dual = DUAL && more && (end ? dual : x_dual);
       const uint32_t y16 = end ? n16 : x16;
-      const uint32_t ks1 = ks + 1 == KS ? 0 : ks + 1, kph1 = ks + 1 == KS ? kph ^ 1u : kph;
       // this step's V and the next one's K first: they are normally there already, and these
       // waits overlap the tensor pipe's last instructions
       if (!(ok = mbar_wait_warp(&v_full[vs], vph, err))) break;
-      if (more && !(ok = mbar_wait_warp(&k_full[ks1], kph1, err))) break;
+      if (more && !(ok = mbar_wait_warp(&k_full[ks], kph, err))) break;
       if (!(ok = mbar_wait_warp(&p_full[0], pph[0], err))) break;
       pph[0] ^= 1u;
       tc_fence_after();
-      if (!end) {
+      if (!end && !(DUAL && x_dual)) {
         if (elect_one()) {
           issue_pv(0, x_first ? 0u : 1u, false, 8u);
-          issue_s(0, ks1, y_short, y16);
+          issue_s(0, ks, y_short, y16);
         }
         if (x_two) {
           if (!(ok = mbar_wait_warp(&p_full[1], pph[1], err))) break;
@@ -729,8 +817,26 @@ __global__ void __launch_bounds__(THREADS, 1)
           tc_fence_after();
           if (elect_one()) {
             issue_pv(1, x_first ? 0u : 1u, false, 8u);
-            issue_s(1, ks1, y_short, y16);
+            issue_s(1, ks, y_short, y16);
           }
+        }
+        --left;
+        x_first = false;
+      } else if (!end) {
+        if (elect_one()) {
+          issue_pv(0, x_first ? 0u : 1u, false, 8u);
+          issue_s(0, ks, y_short, y16);
+        }
+        next_v();
+        next_k();
+        if (!(ok = mbar_wait_warp(&v_full[vs], vph, err))) break;
+        if (!(ok = mbar_wait_warp(&k_full[ks], kph, err))) break;
+        if (!(ok = mbar_wait_warp(&p_full[1], pph[1], err))) break;
+        pph[1] ^= 1u;
+        tc_fence_after();
+        if (elect_one()) {
+          issue_pv(1, x_first ? 0u : 1u, false, 8u);
+          issue_s(1, ks, y_short, y16);
         }
         --left;
         x_first = false;
@@ -740,17 +846,14 @@ __global__ void __launch_bounds__(THREADS, 1)
           tc_commit(&o_done[0]);
         }
         // S of a segment with one query tile goes behind both PVs of a pair: the K slot's release
-        // stands for the V slot of the tile before (see the V loads)
+        // stands for the V slots of the tiles before (see the V loads)
         const bool late = x_two && !y_two;
-        auto next_a = [&] {
-          if (!mbar_wait_warp(&q_full[0], qph[0], err)) return false;
-          qph[0] ^= 1u;
-          tc_fence_after();
-          if (elect_one()) issue_s(0, ks1, y_short, y16);
-          return true;
-        };
-        if (more && !late && !(ok = next_a())) break;
+        if (more && !late && !(ok = next_s(0, true, y_short, y16))) break;
         if (x_two) {
+          if (DUAL && x_dual) {
+            next_v();
+            if (!(ok = mbar_wait_warp(&v_full[vs], vph, err))) break;
+          }
           if (!(ok = mbar_wait_warp(&p_full[1], pph[1], err))) break;
           pph[1] ^= 1u;
           tc_fence_after();
@@ -758,31 +861,26 @@ __global__ void __launch_bounds__(THREADS, 1)
             issue_pv(1, x_first ? 0u : 1u, x_short, x16);
             tc_commit(&o_done[1]);
           }
-          if (more && late && !(ok = next_a())) break;
+          if (more && late && !(ok = next_s(0, true, y_short, y16))) break;
         }
-        if (y_two) {
-          if (!(ok = mbar_wait_warp(&q_full[1], qph[1], err))) break;
-          qph[1] ^= 1u;
-          tc_fence_after();
-          if (elect_one()) issue_s(1, ks1, y_short, y16);
-        }
+        if (y_dual) next_k();
+        if (y_two && !(ok = next_s(1, true, y_short, y16))) break;
         left = steps;
         x16 = n16;
         x_two = two;
+        x_dual = dual;
         x_ends_short = ends_short;
         x_first = true;
       }
-      ks = ks1;
-      kph = kph1;
-      vph ^= vs + 1 == VS;
-      vs = vs + 1 == VS ? 0 : vs + 1;
+      next_k();
+      next_v();
     }
     failed = !ok;
   } else if (warp == 10) {
     // ---------------- masks ----------------
     // The mask of tile T goes into slot T % MASKS once tile T - 1 of V has landed. That tile was
-    // loaded after the K slot of tile T - VS had been released, i.e. after both groups had announced
-    // P of tile T - VS - 1: its mask, and those before it, have been read.
+    // loaded after the K slot of tile T - VS had been released, i.e. after the groups had announced
+    // P of tile T - VS - 2: its mask, and those before it, have been read.
     uint32_t t = 0;                 // key tiles so far
     uint32_t land = 0;              // bit s: phase of v_land[s]
     if (blockIdx.x == 0) {  // states that no sequence asks for are checked here, the others by load_seq
@@ -794,12 +892,16 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (bad) fb_report(err, FB_DEVERR_BAD_INDEX);
     }
     for (; !failed; ++seg) {
-      if (!__all_sync(0xffffffffu, mbar_wait_idle(&g_full[seg % SEGS], (seg / SEGS) & 1, err))) { failed = true; break; }
+      if (!__all_sync(0xffffffffu, mbar_wait_idle(&g_full[seg % SEGS], (seg / SEGS) & 1, err))) {
+        failed = true;
+        break;
+      }
       const Seg sg = segs[seg % SEGS];
       __syncwarp();
       if (lane == 0) mbar_arrive(&g_empty[seg % SEGS]);
       if (sg.steps < 0) break;
-      for (int i = 0; i < sg.steps; ++i, ++t) {
+      for (int e = 0; e < (is_dual(sg) ? 2 * sg.steps : sg.steps); ++e, ++t) {
+        const int i = is_dual(sg) ? e >> 1 : e;
         const int n = sg.keys - i * TB < TB ? sg.keys - i * TB : TB, slot = t % VS;
         if (!MASKED && (n == TB || n % 16 == 0)) continue;
         uint32_t w[4];
@@ -857,7 +959,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if (!more) g.steps = -1;
       if (g.steps == 0) {  // no keys: zeros, written here, and the other roles never hear of it
-        const int n = (g.left < g.ng * p.rq ? g.left : g.ng * p.rq), row = p.group * D / 8;  // pieces of a query
+        const int most = g.dual ? p.rq : g.ng * p.rq, n = g.left < most ? g.left : most;
+        const int row = (g.dual ? 2 : 1) * p.group * D / 8;  // 16-byte pieces of a query
         for (int q = 0; q < n; ++q) {
           bf16* out = p.O + (size_t)(g.row + q) * p.ldo + (size_t)g.h * p.group * D;
           for (int i = lane; i < row; i += 32) reinterpret_cast<uint4*>(out)[i] = make_uint4(0, 0, 0, 0);
@@ -890,11 +993,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     uint32_t cnt = 0, sc = 0, kt = 0;  // segments and S tiles of this group, K tiles of the CTA
     bool due = false;  // this warp has stored its part of `parts`, and not yet said so
     auto out_row = [&](const Seg& sg) {
-      return p.O + (size_t)(sg.row + g * p.rq + qi) * p.ldo + (size_t)(sg.h * p.group + hi) * D;
+      return p.O + (size_t)(sg.row + (is_dual(sg) ? 0 : g * p.rq) + qi) * p.ldo +
+             (size_t)((is_dual(sg) ? sg.h + g : sg.h) * p.group + hi) * D;
     };
     // rows of this warp that exist in a segment: the tile's queries by the group's heads
     auto live_rows = [&](const Seg& sg) {
-      const int tile_q = sg.left - g * p.rq < p.rq ? sg.left - g * p.rq : p.rq;
+      const int left = is_dual(sg) ? sg.left : sg.left - g * p.rq, tile_q = left < p.rq ? left : p.rq;
       const int n = tile_q * p.group - quarter * 32;
       return n < 0 ? 0 : n > 32 ? 32 : n;
     };
@@ -937,8 +1041,10 @@ __global__ void __launch_bounds__(THREADS, 1)
         done_with();
         continue;
       }
-      const bool last_group = g == sg.ng - 1;
+      const bool last_group = is_dual(sg) || g == sg.ng - 1;  // (this group's S comes last for a key tile)
       const int live = live_rows(sg), keys = sg.keys;
+      const uint32_t kt_step = is_dual(sg) ? 2 : 1;
+      if (is_dual(sg)) kt += g;
       // S of this group's next key tile is there; the tile's K slot (and at the last one its Q) is free
       auto scores_ready = [&](bool last) {
         const bool ok = __all_sync(0xffffffffu, mbar_wait(&s_full[g], sc & 1, err));
@@ -948,111 +1054,112 @@ __global__ void __launch_bounds__(THREADS, 1)
       };
       float m_used = -INFINITY, l = 0.f;
       if (live == 0) {  // nothing of this warp's exists: P of its rows may be anything
-        for (int i = 0; i < steps; ++i, ++sc, ++kt) {
+        for (int i = 0; i < steps; ++i, ++sc, kt += kt_step) {
           if (!scores_ready(i == steps - 1)) { failed = true; break; }
           if (lane == 0) mbar_arrive(&p_full[g]);
         }
-      } else
-      for (int i = 0; i < steps; ++i, ++sc, ++kt) {
+      }
+      for (int i = live > 0 ? 0 : steps; i < steps; ++i, ++sc, kt += kt_step) {
         if (!scores_ready(i == steps - 1)) { failed = true; break; }
-          tc_fence_after();
-          const int valid = keys - i * TB;
-          uint32_t mk[4] = {~0u, ~0u, ~0u, ~0u};
-          if (MASKED) {
-            const bool seen = mbar_wait(&m_full[kt % MASKS], (kt / MASKS) & 1, err);
-            if (!__all_sync(0xffffffffu, seen)) { failed = true; break; }
-            const uint4 w = masks[kt % MASKS];
-            mk[0] = w.x;
-            mk[1] = w.y;
-            mk[2] = w.z;
-            mk[3] = w.w;
-          }
-          const bool all = MASKED ? (mk[0] & mk[1] & mk[2] & mk[3]) == ~0u : valid >= TB;
-          float s[128];
-          {
-            uint32_t u[128];
+        tc_fence_after();
+        const int valid = keys - i * TB;
+        uint32_t mk[4] = {~0u, ~0u, ~0u, ~0u};
+        if (MASKED) {
+          const bool seen = mbar_wait(&m_full[kt % MASKS], (kt / MASKS) & 1, err);
+          if (!__all_sync(0xffffffffu, seen)) { failed = true; break; }
+          const uint4 w = masks[kt % MASKS];
+          mk[0] = w.x;
+          mk[1] = w.y;
+          mk[2] = w.z;
+          mk[3] = w.w;
+        }
+        const bool all = MASKED ? (mk[0] & mk[1] & mk[2] & mk[3]) == ~0u : valid >= TB;
+        float s[128];
+        {
+          uint32_t u[128];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(lane_base + s_col + c * 32, u + c * 32);
-            tmem_ld_wait();
+          for (int c = 0; c < 4; ++c) tmem_ld32(lane_base + s_col + c * 32, u + c * 32);
+          tmem_ld_wait();
 #pragma unroll
-            for (int c = 0; c < 4; ++c) reg_fence32(u + c * 32);
+          for (int c = 0; c < 4; ++c) reg_fence32(u + c * 32);
 #pragma unroll
-            for (int e = 0; e < 128; ++e) s[e] = __uint_as_float(u[e]);
-          }
-          if (!all) {
+          for (int e = 0; e < 128; ++e) s[e] = __uint_as_float(u[e]);
+        }
+        if (!all) {
 #pragma unroll
-            for (int e = 0; e < 128; ++e)
-              if (MASKED ? !((mk[e / 32] >> (e % 32)) & 1) : e >= valid) s[e] = -INFINITY;
-          }
-          // (at least the lowest finite value: a row without a key so far has exponentials of
-          // exp2(-inf) = 0 and joins others with a factor of 0)
-          const float mx = fmaxf(rowmax128(s) * p.scale_log2, -FLT_MAX);
-          if (__all_sync(0xffffffffu, m_used == -INFINITY)) {  // the segment's first tile
-            m_used = mx;
-          } else if (__any_sync(0xffffffffu, mx > m_used + 8.f)) {
-            const float m_new = fmaxf(m_used, mx);
-            const float alpha = ex2(m_used - m_new);
-            m_used = m_new;
-            l *= alpha;
+          for (int e = 0; e < 128; ++e)
+            if (MASKED ? !((mk[e / 32] >> (e % 32)) & 1) : e >= valid) s[e] = -INFINITY;
+        }
+        // (at least the lowest finite value: a row without a key so far has exponentials of
+        // exp2(-inf) = 0 and joins others with a factor of 0)
+        const float mx = fmaxf(rowmax128(s) * p.scale_log2, -FLT_MAX);
+        if (__all_sync(0xffffffffu, m_used == -INFINITY)) {  // the segment's first tile
+          m_used = mx;
+        } else if (__any_sync(0xffffffffu, mx > m_used + 8.f)) {
+          const float m_new = fmaxf(m_used, mx);
+          const float alpha = ex2(m_used - m_new);
+          m_used = m_new;
+          l *= alpha;
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-              uint32_t u[32];
-              tmem_ld32(lane_base + o_col + c * 32, u);
-              tmem_ld_wait();
-              reg_fence32(u);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) * alpha);
-              tmem_st32(lane_base + o_col + c * 32, u);
-            }
-          }
-          const uint64_t sc2 = f2_join(p.scale_log2, p.scale_log2);
-          const uint64_t nm2 = f2_join(-m_used, -m_used);
-          uint64_t ls2[2] = {0ull, 0ull};
-          // keys 0-63 from the registers, keys 64-127 read again (P of keys 0-63 only overwrites
-          // columns 0-31): the first half need not keep them
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float h[64];
-            if (c == 0) {
-#pragma unroll
-              for (int e = 0; e < 64; ++e) h[e] = s[e];
-            } else {
-              uint32_t u2[64];
-              tmem_ld32(lane_base + s_col + 64, u2);
-              tmem_ld32(lane_base + s_col + 96, u2 + 32);
-              tmem_ld_wait();
-              reg_fence32(u2);
-              reg_fence32(u2 + 32);
-#pragma unroll
-              for (int e = 0; e < 64; ++e) h[e] = __uint_as_float(u2[e]);
-              if (!all) {
-#pragma unroll
-                for (int e = 0; e < 64; ++e)
-                  if (MASKED ? !((mk[2 + e / 32] >> (e % 32)) & 1) : 64 + e >= valid) h[e] = -INFINITY;
-              }
-            }
+          for (int c = 0; c < D / 32; ++c) {
             uint32_t u[32];
+            tmem_ld32(lane_base + o_col + c * 32, u);
+            tmem_ld_wait();
+            reg_fence32(u);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              float t0, t1;
-              f2_split(f2_fma(f2_join(h[2 * e], h[2 * e + 1]), sc2, nm2), t0, t1);
-              const float e0 = ex2(t0), e1 = ex2(t1);
-              ls2[e & 1] = f2_add(ls2[e & 1], f2_join(e0, e1));
-              u[e] = pack_bf16x2(e0, e1);
+            for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) * alpha);
+            tmem_st32(lane_base + o_col + c * 32, u);
+          }
+        }
+        const uint64_t sc2 = f2_join(p.scale_log2, p.scale_log2);
+        const uint64_t nm2 = f2_join(-m_used, -m_used);
+        uint64_t ls2[2] = {0ull, 0ull};
+        // keys 0-63 from the registers, keys 64-127 read again (P of keys 0-63 only overwrites
+        // columns 0-31): the first half need not keep them
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float h[64];
+          if (c == 0) {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) h[e] = s[e];
+          } else {
+            uint32_t u2[64];
+            tmem_ld32(lane_base + s_col + 64, u2);
+            tmem_ld32(lane_base + s_col + 96, u2 + 32);
+            tmem_ld_wait();
+            reg_fence32(u2);
+            reg_fence32(u2 + 32);
+#pragma unroll
+            for (int e = 0; e < 64; ++e) h[e] = __uint_as_float(u2[e]);
+            if (!all) {
+#pragma unroll
+              for (int e = 0; e < 64; ++e)
+                if (MASKED ? !((mk[2 + e / 32] >> (e % 32)) & 1) : 64 + e >= valid) h[e] = -INFINITY;
             }
-            tmem_st32(lane_base + s_col + c * 32, u);
           }
-          {
-            float a0, a1;
-            f2_split(f2_add(ls2[0], ls2[1]), a0, a1);
-            l += a0 + a1;
+          uint32_t u[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            float t0, t1;
+            f2_split(f2_fma(f2_join(h[2 * e], h[2 * e + 1]), sc2, nm2), t0, t1);
+            const float e0 = ex2(t0), e1 = ex2(t1);
+            ls2[e & 1] = f2_add(ls2[e & 1], f2_join(e0, e1));
+            u[e] = pack_bf16x2(e0, e1);
           }
-          tmem_st_wait();
-          tc_fence_before();
+          tmem_st32(lane_base + s_col + c * 32, u);
+        }
+        {
+          float a0, a1;
+          f2_split(f2_add(ls2[0], ls2[1]), a0, a1);
+          l += a0 + a1;
+        }
+        tmem_st_wait();
+        tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_full[g]);
       }
       if (failed) break;
+      if (is_dual(sg)) kt -= g;
       say_due();
       // the segment's rows: PV of its last key tile done
       if (!mbar_wait_warp(&o_done[g], cnt & 1, err)) { failed = true; break; }
@@ -1160,7 +1267,7 @@ bool may_cut(const CrossArgs& c, int num_sms) {
   return fewest < 8ll * num_sms && (c.kv_rows > 7 * TB || most_items(c) > num_sms);
 }
 
-template <int D, bool MASKED>
+template <int D, bool MASKED, bool DUAL>
 cudaError_t launch(const CrossArgs& c, const Params& p, int grid, cudaStream_t st) {
   CUtensorMap mq, mk, mv;
   const bool no_keys = c.kv_rows == 0;  // (any map: nothing is loaded then)
@@ -1169,11 +1276,16 @@ cudaError_t launch(const CrossArgs& c, const Params& p, int grid, cudaStream_t s
     mk = mv = mq;
   else if (!map_kv(&mk, c, c.k, c.ldk) || !map_kv(&mv, c, c.v, c.ldv))
     return cudaErrorInvalidValue;
-  auto kern = cross_kernel<D, MASKED>;
+  auto kern = cross_kernel<D, MASKED, DUAL>;
   const cudaError_t e =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::SMEM);
   if (e != cudaSuccess) return e;
   return launch_k(kern, dim3(grid), dim3(THREADS), Shape<D>::SMEM, st, mq, mk, mv, p);
+}
+
+template <int D, bool MASKED>
+cudaError_t choose(const CrossArgs& c, const Params& p, int grid, cudaStream_t st) {
+  return p.dual ? launch<D, MASKED, true>(c, p, grid, st) : launch<D, MASKED, false>(c, p, grid, st);
 }
 
 }  // namespace
@@ -1182,8 +1294,7 @@ cudaError_t cross_set_wait_limit(unsigned long long ns) { return fb_set_wait_lim
 
 size_t cross_ws_bytes(const CrossArgs& c, int num_sms) {
   if (!may_cut(c, num_sms)) return 0;
-  const size_t warp = c.head_dim == 128 ? Shape<128>::WS_WARP : Shape<64>::WS_WARP;
-  return 2 * (size_t)num_sms * 8 * warp * sizeof(float);
+  return 2 * (size_t)num_sms * 8 * part_floats(c.head_dim) * sizeof(float);
 }
 
 cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* err, int num_sms,
@@ -1203,6 +1314,12 @@ cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* er
   p.O = (bf16*)c.out;
   p.ldo = c.ldo;
   p.scale_log2 = c.scale * 1.4426950408889634f;
+  // Two kv heads side by side keep twice as much of K and V on its way (64 tokens of 4 kv heads on 32 to
+  // 4096 keys: 32.5 us for 38), but a step of both takes 3500 clocks for one's 2600: only where every CTA
+  // has more than one to do. With longer sequences the items have two query tiles for the most part, and
+  // the kernel without that takes 161 us for 171 (32 of 1560 rows on 512 keys).
+  const long long seqs = c.seqs < c.q_rows ? c.seqs : c.q_rows;
+  p.dual = seqs * c.kv_heads > num_sms && c.q_rows <= seqs * p.rq;
   const long long tiles = (c.kv_rows + TB - 1) / TB;
   p.flat = most_items(c) * (4.0 * tiles + 4) >= 4e9;
   const bool cut = may_cut(c, num_sms) && !p.flat;
@@ -1213,6 +1330,6 @@ cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* er
   if (cut) units *= tiles;
   const int grid = (int)(units < num_sms ? units : num_sms);
   if (c.head_dim == 128)
-    return c.valid ? launch<128, true>(c, p, grid, st) : launch<128, false>(c, p, grid, st);
-  return c.valid ? launch<64, true>(c, p, grid, st) : launch<64, false>(c, p, grid, st);
+    return c.valid ? choose<128, true>(c, p, grid, st) : choose<128, false>(c, p, grid, st);
+  return c.valid ? choose<64, true>(c, p, grid, st) : choose<64, false>(c, p, grid, st);
 }

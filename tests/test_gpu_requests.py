@@ -190,6 +190,34 @@ def test_cross_many_sequences(model):
     Cross(queries, keys, heads=2, kv_heads=1, D=64, seed=12).check(model)
 
 
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("heads,kv_heads", [(4, 2), (3, 3), (20, 5)])
+@pytest.mark.parametrize("valid", [None, 0.3])
+@pytest.mark.parametrize("long", [False, True])
+def test_cross_kv_heads_side_by_side(model, D, heads, kv_heads, valid, long):
+    """More sequences of one query tile than SMs, among them some of several tiles, of no query and of
+    no key; with one long prompt, whose keys several SMs share."""
+    rng = torch.Generator().manual_seed(kv_heads)
+    queries = torch.randint(0, 5, (160,), generator=rng).tolist()
+    keys = torch.randint(0, 400, (160,), generator=rng).tolist()
+    queries[7], queries[90], queries[91], queries[159] = 300, 130, 700, 129
+    if long:
+        keys[3], keys[100], queries[3] = 9000, 2500, 1
+    keys[20] = 0
+    Cross(queries, keys, heads=heads, kv_heads=kv_heads, D=D, valid=valid, seed=17).check(model)
+
+
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("queries,keys", [([1] * 9, [700] * 9), ([2, 300, 1, 1, 40], [1, 130, 2000, 16, 513])])
+def test_cross_on_few_sms(model, D, queries, keys):
+    model.set_sm_budget(4)
+    try:
+        Cross(queries, keys, heads=6, kv_heads=3, D=D, valid=0.1, seed=18).check(model)
+        Cross(queries, keys, heads=6, kv_heads=2, D=D, seed=19).check(model)
+    finally:
+        model.set_sm_budget(0)
+
+
 def test_cross_same_result_every_time_and_on_few_sms(model):
     """The same bits on every call, with a repeat count, and on a budget of few SMs within the
     tolerance."""
