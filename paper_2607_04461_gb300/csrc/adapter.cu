@@ -41,7 +41,7 @@ struct Warps {
   static constexpr int EPI = PARTS ? 12 : 8, GROUPS = EPI / 4, LOAD = 2 + EPI, THREADS = 32 * (4 + EPI);
 };
 constexpr int MAX_S = FB_ADAPTER_MAX_SEGMENTS;
-constexpr int SMEM_BYTES = 229888;  // (room for a block of the low-rank part beside it)
+constexpr int SMEM_BYTES = 229888;  // of 232448 that a block may have
 constexpr int EPI_TILE = 2048;      // an epilogue warp's tile: 32 tokens x 32 rows, bf16
 constexpr int EPI_BYTES = 8 * 2 * EPI_TILE;
 constexpr int TABLE_BYTES = (3 * (MAX_S + 8) * 4 + 127) / 128 * 128;

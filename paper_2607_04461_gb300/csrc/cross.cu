@@ -253,15 +253,14 @@ __device__ __forceinline__ u32 begin_at(const Cost& c, u32 u_s, u32 x, int& h, i
 
 // Adds up the sequences' costs and decides how the items are handed out; the thread whose sequence
 // a stretch begins in writes where. TEAM: the threads that work on it, one warp (at most 32
-// sequences; returns the lane's own) or the whole block (which has to synchronise after it).
+// sequences, whose own each lane has at hand) or the whole block (which has to synchronise after it).
 template <int TEAM>
-__device__ __forceinline__ Seq make_plan(const Params& p, Plan* plan, uint3* scan, int tid) {
+__device__ __forceinline__ void make_plan(const Params& p, Seq q, Plan* plan, uint3* scan, int tid) {
   const int lane = tid % 32;
   const int per = (p.seqs + TEAM - 1) / TEAM, s0 = tid * per, s1 = s0 + per < p.seqs ? s0 + per : p.seqs;
   u32 sum = 0, big = 0, n = 0;
-  Seq q{0, 0, 0, 0};
   for (int s = s0; s < s1; ++s) {
-    load_seq(p, s, q);
+    if (TEAM > 32) load_seq(p, s, q);
     const Cost c(p, q);
     sum += c.all();
     n += c.items();
@@ -334,7 +333,6 @@ __device__ __forceinline__ Seq make_plan(const Params& p, Plan* plan, uint3* sca
       plan->q = q;
     }
   }
-  return q;
 }
 
 // A CTA's segments, one after the other: what the roles read of each, through a ring in shared
@@ -395,10 +393,9 @@ struct Stretch {
 struct Items {
   int s0 = -32;       // the sequences at hand
   u32 end = 0;        // first item behind them
-  Seq q;              // this lane's sequence, and its first item
-  bool have;          // (q is that of the first 32 already)
+  Seq q;              // this lane's sequence (at first, one of the first 32), and its first item
   u32 first = 0;
-  __device__ __forceinline__ Items(bool have_, const Seq& q_) : q(q_), have(have_) {}
+  __device__ __forceinline__ explicit Items(const Seq& q_) : q(q_) {}
   __device__ __forceinline__ bool find(const Params& p, const Plan& pl, u32 i, int lane, Seg& g) {
     while (i >= end) {
       if (s0 + 32 >= p.seqs) return false;
@@ -406,7 +403,7 @@ struct Items {
       const int s = s0 + lane;
       u32 n = 0;
       if (s < p.seqs) {
-        if (!have) load_seq(p, s, q);
+        if (s0 > 0) load_seq(p, s, q);
         n = Cost(p, q).items();
       }
       u32 upto = n;
@@ -630,7 +627,9 @@ __global__ void __launch_bounds__(THREADS, 1)
   // Where no item can be cut there is nothing to plan; few sequences warp 11 adds up by itself, while
   // the others come to their roles.
   const bool few = p.seqs <= 32;
-  if (p.ws && !few) make_plan<THREADS>(p, &plan, scan, threadIdx.x);
+  Seq own{0, 0, 0, 0};  // of the first 32 sequences, a lane of warp 11 one each
+  if (warp == 11 && lane < p.seqs) load_seq(p, lane, own);
+  if (p.ws && !few) make_plan<THREADS>(p, Seq{}, &plan, scan, threadIdx.x);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -939,10 +938,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
   } else if (warp == 11) {
     // ---------------- segments ----------------
-    Seq own{0, 0, 0, 0};
-    if (p.ws && few) own = make_plan<32>(p, &plan, scan, lane);
+    if (p.ws && few) make_plan<32>(p, own, &plan, scan, lane);
     __syncwarp();
-    Items items(p.ws && few, own);
+    Items items(own);
     const bool cut = p.ws && plan.cut;
     Stretch stretch(plan);
     u32 item = blockIdx.x;  // the CTA's first one; the others' numbers come from the counter

@@ -455,6 +455,116 @@ def test_scratch_failure_leaves_the_model_usable():
         c.check(m)
 
 
+def test_cross_scratch_failure_leaves_the_model_usable():
+    with fb.Model(synth.TINY, synth.make_weights(synth.TINY)) as m:
+        c = Cross([3], [4000], seed=26)  # (its keys shared by SMs, the parts in the scratch)
+        fb.fb_test_fail_alloc(0)
+        try:
+            with pytest.raises(fb.FlashBonError) as e:
+                m.op_cross_attention(c.args)
+            assert e.value.status == fb.FB_ENOMEM
+        finally:
+            fb.fb_test_fail_alloc(-1)
+        assert (c.out == 7.0).all()
+        c.check(m)
+
+
+def test_cross_wait_runs_out_then_recovers(model):
+    """Four items or so for each SM, of 32 key tiles: an item's place in the ring of two comes free after
+    some 40 us, past a limit of a microsecond on that wait. The call reports it, and the next ones are as
+    before, with whole items and with cut ones."""
+    whole_items = Cross([200] * 160, [4096], heads=4, kv_of=[0] * 160, seed=27)
+    cut_items = Cross([3, 40], [4000, 9000], seed=28)
+    model.op_cross_attention(whole_items.args)
+    ref = whole_items.out.clone()
+    torch.cuda.synchronize()
+    fb.fb_set_device_wait_limit(1000)
+    try:
+        with pytest.raises(fb.FlashBonError) as e:
+            model.op_cross_attention(whole_items.args)
+    finally:
+        fb.fb_set_device_wait_limit(0)
+    assert e.value.status == fb.FB_ECUDA and "device wait timed out" in str(e.value)
+    for _ in range(2):
+        whole_items.out.fill_(7.0)
+        model.op_cross_attention(whole_items.args)
+        torch.cuda.synchronize()
+        assert torch.equal(whole_items.out, ref)
+        cut_items.check(model)
+
+
+def test_adapter_wait_runs_out_then_recovers(model):
+    """Tiles of 2048 K blocks, all at once, take their mainloop 0.6 ms, past a limit of a microsecond on
+    the epilogue's wait for it (whose clock is looked at every 64 polls, 0.3 ms): the call reports it,
+    and the next ones are as before."""
+    rows, n, k = 1024, 4864, 1 << 17
+    g = gen(29)
+    x = torch.randn(rows, k, generator=g, device="cuda").to(BF)
+    w = torch.empty(n, k, dtype=BF, device="cuda").normal_(generator=g)
+    a, b = (torch.randn(*size, generator=g, device="cuda").to(BF) for size in ((1, 8, k), (1, n, 8)))
+    out = torch.zeros(rows, n, dtype=BF, device="cuda")
+    args = fb.make_adapters(x, w, a, b, whole([0, rows]), whole([0]), out)
+    model.op_adapter_gemm(args)
+    ref = out.clone()
+    torch.cuda.synchronize()
+    fb.fb_set_device_wait_limit(1000)
+    try:
+        with pytest.raises(fb.FlashBonError) as e:
+            model.op_adapter_gemm(args)
+    finally:
+        fb.fb_set_device_wait_limit(0)
+    assert e.value.status == fb.FB_ECUDA and "device wait timed out" in str(e.value)
+    for _ in range(2):
+        out.zero_()
+        model.op_adapter_gemm(args)
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref)
+    Adapters(*LONG, N=1536, K=1544, rank=16, seed=30).check(model)
+
+
+def test_statistics_of_both(model):
+    """Launches, operations and bytes under the operators' own kinds."""
+    c, a = Cross([70, 3], [200, 90], seed=32), Adapters([300, 20], [0, 1], rank=16, seed=33)
+    model.reset_stats()
+    c.check(model)
+    a.check(model)
+    stats = model.stats()
+    assert {kind: x["launches"] for kind, x in stats.items() if x["launches"]} == \
+        {"cross_attention": 1, "adapter_gemm": 2}
+    assert stats["cross_attention"]["flops"] > 0 and stats["adapter_gemm"]["bytes"] > 0
+
+
+def test_two_models_at_once():
+    """Calls of two models on streams of their own, from two threads: each has its scratch and counters."""
+    import threading
+    with fb.Model(synth.TINY, synth.make_weights(synth.TINY)) as one, \
+            fb.Model(synth.TINY, synth.make_weights(synth.TINY)) as two:
+        work = [(m, torch.cuda.Stream(), Cross([3, 300], [6000, 700], seed=34 + i),
+                 Adapters(*LONG, N=1536, K=1544, rank=16, seed=36 + i)) for i, m in enumerate((one, two))]
+        torch.cuda.synchronize()
+        failures = []
+
+        def run(m, stream, c, a):
+            try:
+                m.set_stream(stream.cuda_stream)
+                for _ in range(20):
+                    m.op_cross_attention(c.args)
+                    m.op_adapter_gemm(a.args)
+            except Exception as e:  # noqa: BLE001
+                failures.append(e)
+
+        threads = [threading.Thread(target=run, args=w) for w in work]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert not failures
+        for m, _, c, a in work:
+            c.check(m)
+            a.check(m)
+            m.set_stream(None)
+
+
 # ---- together -------------------------------------------------------------------------
 
 def test_cross_sublayer_of_several_requests(model):
