@@ -396,6 +396,19 @@ def test_adapter_cut_tiles(model, out_t, N, K, segments, of):
     Adapters(segments, of, N=N, K=K, rank=40, out_t=out_t, seed=26).check(model)
 
 
+@pytest.mark.parametrize("segments,of,K", [([1300], [0], 4160), ([3000, 1, 400], [0, 1, -1], 1032), LONG + (8200,)])
+def test_adapter_cut_tiles_of_t_and_the_product(model, segments, of, K):
+    """Both kernels' cut tiles share their scratch: every call gives the same bits."""
+    c = Adapters(segments, of, N=1536, K=K, rank=16, seed=38)
+    c.check(model)
+    first = c.out.clone()
+    for _ in range(20):
+        c.out.copy_(c.before)
+        model.op_adapter_gemm(c.args)
+        torch.cuda.synchronize()
+        assert torch.equal(first, c.out)
+
+
 def test_adapter_same_result_every_time_and_on_few_sms(model):
     for segments, of in (([1] * 50, [i % 5 for i in range(50)]), ([400, 300, 9], [0, -1, 1]), ([6], [0]), LONG):
         c = Adapters(segments, of, N=1536, K=1544, rank=16, seed=22)
