@@ -770,19 +770,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<PARTS>::THREAD
 // The low-rank part of up to 16 rows of a segment, scale (x A_e^T) B_e^T in fp32, by a cluster of
 // eight CTAs: each forms its eighth of K's sums of t (mma.sync, A_e and x straight from memory into the
 // operand registers, A_e the M side), all of them add the eighths up in CTA order through distributed
-// shared memory, and each multiplies t with its eighth of B_e's rows (a feature per thread). What
-// counts is to have all of A_e and B_e on their way at once. Rows without an adapter get zeros.
+// shared memory, and each multiplies t with its eighth of B_e's rows (a feature per thread). Rows without
+// an adapter get zeros. Latency bounds it: 64 segments of a row, 9216 x 1536, rank 16 (22 MB) take 7 us of
+// the call's 22.5, of which 1.5 find the segment, 1.5 form the sums, 2 join them and 2 multiply. So B_e's rows
+// come by one bulk copy meanwhile (read when t is there, or by copies of single threads, which wait behind
+// A_e's in the load units: 25 to 27 us a call), and a row's features share the reads of t.
 constexpr int D_CTAS = 8, D_WARPS = 8, D_THREADS = 32 * D_WARPS, D_ROWS = 16;
+constexpr int D_STAGE = 40 << 10;  // of B_e's rows in shared memory (four blocks of rank 16 on an SM)
+// Features of a block whose rows of B_e wait in shared memory, the others come from L2. (Ranks above 32
+// have their rows on too few banks.)
+__host__ __device__ inline int delta_staged(int features, int rank) {
+  const int fit = rank > 32 ? 0 : D_STAGE / (rank * 2);
+  return features < fit ? features : fit;
+}
 // MT: 16 of the rank each, in one pass over K.
 template <int MT>
-size_t delta_smem(int rank) {
-  return (size_t)(D_WARPS * 16 * MT + 2 * rank) * D_ROWS * sizeof(float);
+size_t delta_smem(int n, int rank) {
+  return (size_t)(D_WARPS * 16 * MT + 2 * rank) * D_ROWS * sizeof(float) +
+         (size_t)delta_staged(n / D_CTAS + 1, rank) * rank * sizeof(bf16);
 }
 
 __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
   return v;
+}
+// bytes (a multiple of 16) into this CTA's shared memory
+__device__ __forceinline__ void bulk_load(void* to, const void* from, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                   smem_u32(to)),
+               "l"(from), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
 }
 
 template <int MT>
@@ -795,24 +813,33 @@ __global__ void __cluster_dims__(D_CTAS, 1, 1) __launch_bounds__(D_THREADS, MT =
   float* part = sm;                                // [warp][D_RANKS of the rank][16 rows]
   float* own = part + D_WARPS * D_RANKS * D_ROWS;  // [rank][16]: this CTA's sums
   float* t = own + g.rank * D_ROWS;                // [rank][16]: all of them
+  bf16* stage = reinterpret_cast<bf16*>(t + g.rank * D_ROWS);  // rows of B_e
   __shared__ int found[4], scan[D_WARPS];
+  __shared__ uint64_t landed;
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   const uint32_t c = cluster_ctarank();
   const int want = blockIdx.x / D_CTAS;
   // ---- the want-th chunk of 16 rows: each thread up to four segments ----
-  if (tid == 0) found[0] = -2;
-  int chunks[4], sum = 0;
+  if (tid == 0) {
+    found[0] = -2;
+    mbar_init(&landed, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  int a[4], b[4], of[4], sum = 0;
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int s = 4 * tid + i;
-    chunks[i] = 0;
-    if (s < g.segments) {
-      const int a = g.offsets[s], b = g.offsets[s + 1], e = g.adapter[s];
-      bad = bad || a < 0 || b < a || b > g.rows || (s == 0 && a != 0) || e < -1 || e >= g.adapters;
-      chunks[i] = (b - a + D_ROWS - 1) / D_ROWS;
-      sum += chunks[i];
-    }
+    const bool in = s < g.segments;
+    a[i] = in ? g.offsets[s] : 0;
+    b[i] = in ? g.offsets[s + 1] : 0;
+    of[i] = in ? g.adapter[s] : -1;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    bad = bad || a[i] < 0 || b[i] < a[i] || b[i] > g.rows || (tid == 0 && i == 0 && a[i] != 0) || of[i] < -1 ||
+          of[i] >= g.adapters;
+    sum += (b[i] - a[i] + D_ROWS - 1) / D_ROWS;
   }
   static_assert(FB_ADAPTER_MAX_SEGMENTS <= 4 * D_THREADS, "segments of a thread");
   int upto = sum;
@@ -830,22 +857,31 @@ __global__ void __cluster_dims__(D_CTAS, 1, 1) __launch_bounds__(D_THREADS, MT =
   for (int w = 0; w < warp; ++w) at += scan[w];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (want >= at && want < at + chunks[i]) {
-      const int s = 4 * tid + i;
-      found[0] = g.adapter[s];
-      found[1] = g.offsets[s] + (want - at) * D_ROWS;
-      found[2] = g.offsets[s + 1];
+    const int chunks = (b[i] - a[i] + D_ROWS - 1) / D_ROWS;
+    if (want >= at && want < at + chunks) {
+      found[0] = of[i];
+      found[1] = a[i] + (want - at) * D_ROWS;
+      found[2] = b[i];
     }
-    at += chunks[i];
+    at += chunks;
   }
   __syncthreads();
   const int e = found[0], r0 = found[1];
   if (e == -2) return;  // (the whole cluster)
   const int rows = found[2] - r0 < D_ROWS ? found[2] - r0 : D_ROWS;
   const int fa = (int)((int64_t)g.n * c / D_CTAS), fb = (int)((int64_t)g.n * (c + 1) / D_CTAS);
-  if (e >= 0 && tid < D_WARPS) {  // B_e's rows on their way into L2 meanwhile, an eighth a thread
+  // B_e's rows on their way meanwhile: as many as fit into shared memory, the others into L2, an eighth of
+  // them a thread
+  const int staged = delta_staged(fb - fa, g.rank);
+  if (e >= 0 && tid < D_WARPS) {
     const bf16* b = (const bf16*)g.b + ((size_t)e * g.n + fa) * g.rank;
-    const int64_t pieces = (int64_t)(fb - fa) * g.rank / 8, p0 = pieces * tid / D_WARPS, p1 = pieces * (tid + 1) / D_WARPS;
+    if (tid == 0 && staged > 0) {
+      const uint32_t bytes = (uint32_t)(staged * g.rank * sizeof(bf16));
+      mbar_expect_tx(&landed, bytes);
+      bulk_load(stage, b, bytes, &landed);
+    }
+    const int64_t first = (int64_t)staged * g.rank / 8, pieces = (int64_t)(fb - fa) * g.rank / 8 - first;
+    const int64_t p0 = first + pieces * tid / D_WARPS, p1 = first + pieces * (tid + 1) / D_WARPS;
     if (p1 > p0 && p1 - p0 < (1 << 20)) prefetch_l2_bulk(b + p0 * 8, (uint32_t)(p1 - p0) * 16);
   }
   // ---- t: this CTA's part of K ----
@@ -908,53 +944,79 @@ __global__ void __cluster_dims__(D_CTAS, 1, 1) __launch_bounds__(D_THREADS, MT =
       }
       __syncthreads();
     }
-    cluster_sync();
     const float scale = g.scale ? g.scale[e] : 1.f;
+    cluster_sync();
     for (int i = tid; i < g.rank * D_ROWS; i += D_THREADS) {
-      float v = 0.f;
+      float v = 0.f, w[D_CTAS];
+      if (i % D_ROWS < rows) {
 #pragma unroll
-      for (uint32_t p = 0; p < D_CTAS; ++p) v += ld_cluster(mapa_shared(smem_u32(own + i), p));
+        for (uint32_t p = 0; p < D_CTAS; ++p) w[p] = ld_cluster(mapa_shared(smem_u32(own + i), p));
+#pragma unroll
+        for (int p = 0; p < D_CTAS; ++p) v += w[p];
+      }
       t[i] = v * scale;
     }
-    cluster_sync();  // (no CTA leaves while its sums are read)
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   }
   // ---- the product with this CTA's rows of B_e ----
-#pragma unroll 2
-  for (int f = fa + tid; f < fb; f += D_THREADS) {
-    float y[D_ROWS] = {};
-    if (e >= 0 && rows == 1) {
-      const bf16* b = (const bf16*)g.b + ((size_t)e * g.n + f) * g.rank;
-#pragma unroll 2
-      for (int r = 0; r < g.rank; r += 8) {
-        float w[8];
-        load_bf16x8(b + r, w);
+  if (e >= 0 && staged > 0 && !mbar_wait(&landed, 0, err)) {  // (reported; the copy lands before the block ends)
+    const uint64_t t0 = fb_globaltimer();
+    while (fb_globaltimer() - t0 < 100000ull) __nanosleep(1000);
+  }
+  // F of a thread's features at a time, so that each reads t only once for all of them
+  auto product = [&](auto features, auto of_rows) {
+    constexpr int F = decltype(features)::value, R = decltype(of_rows)::value;
+#pragma unroll 1
+    for (int f = fa + tid; f < fb; f += F * D_THREADS) {
+      float y[F][R] = {};
+#pragma unroll 1
+      for (int r = 0; e >= 0 && r < g.rank; r += 8) {
+        float w[F][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[0] = fmaf(w[i], t[(r + i) * D_ROWS], y[0]);
-      }
-    } else if (e >= 0) {
-      const bf16* b = (const bf16*)g.b + ((size_t)e * g.n + f) * g.rank;
-#pragma unroll 2
-      for (int r = 0; r < g.rank; r += 8) {
-        float w[8];
-        load_bf16x8(b + r, w);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (4 * j >= rows) break;
+        for (int j = 0; j < F; ++j) {
+          const int at = min(f + j * D_THREADS, fb - 1) - fa;
+          const bf16* from = stage + at * g.rank + r;
+          if (at >= staged) from = (const bf16*)g.b + ((size_t)e * g.n + fa + at) * g.rank + r;
+          load_bf16x8(from, w[j]);
+        }
+        if constexpr (R == 1) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float4 v = *reinterpret_cast<const float4*>(t + (r + i) * D_ROWS + 4 * j);
-            y[4 * j] = fmaf(w[i], v.x, y[4 * j]);
-            y[4 * j + 1] = fmaf(w[i], v.y, y[4 * j + 1]);
-            y[4 * j + 2] = fmaf(w[i], v.z, y[4 * j + 2]);
-            y[4 * j + 3] = fmaf(w[i], v.w, y[4 * j + 3]);
+            const float v = t[(r + i) * D_ROWS];
+#pragma unroll
+            for (int j = 0; j < F; ++j) y[j][0] = fmaf(w[j][i], v, y[j][0]);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < R; k += 4) {
+            if (k >= rows) break;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float4 v = *reinterpret_cast<const float4*>(t + (r + i) * D_ROWS + k);
+#pragma unroll
+              for (int j = 0; j < F; ++j) {
+                y[j][k] = fmaf(w[j][i], v.x, y[j][k]);
+                y[j][k + 1] = fmaf(w[j][i], v.y, y[j][k + 1]);
+                y[j][k + 2] = fmaf(w[j][i], v.z, y[j][k + 2]);
+                y[j][k + 3] = fmaf(w[j][i], v.w, y[j][k + 3]);
+              }
+            }
           }
         }
       }
-    }
 #pragma unroll
-    for (int j = 0; j < D_ROWS; ++j)
-      if (j < rows) delta[(size_t)(r0 + j) * g.n + f] = y[j];
-  }
+      for (int j = 0; j < F; ++j)
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+          if (k < rows && f + j * D_THREADS < fb) delta[(size_t)(r0 + k) * g.n + f + j * D_THREADS] = y[j][k];
+    }
+  };
+  if (rows == 1)
+    product(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+  else
+    product(std::integral_constant<int, 1>{}, std::integral_constant<int, D_ROWS>{});
+  if (e >= 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");  // (no CTA leaves while its sums are read)
 }
 
 // ---- few rows ---------------------------------------------------------------------------
@@ -1123,9 +1185,9 @@ cudaError_t launch_tc(const AdapterArgs& g, TcArgs a, const bf16* t, int most, i
 template <int MT>
 cudaError_t launch_delta(const AdapterArgs& g, float* delta, int* err, cudaStream_t st) {
   auto kern = adapter_delta_kernel<MT>;
-  const size_t smem = delta_smem<MT>(g.rank);
+  const size_t smem = delta_smem<MT>(g.n, g.rank);
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)delta_smem<MT>(FB_ADAPTER_MAX_RANK));
+                                             (int)(delta_smem<MT>(0, FB_ADAPTER_MAX_RANK) + D_STAGE));
   if (e != cudaSuccess) return e;
   const long long chunks = g.rows / D_ROWS + (g.segments < g.rows ? g.segments : g.rows);
   return launch_k(kern, dim3((unsigned)(chunks * D_CTAS)), dim3(D_THREADS), smem, st, g, delta, err);
@@ -1145,11 +1207,12 @@ size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 // reading A_e and B_e for every 16 rows, multiplying them by CUDA cores, and writing and reading the
 // part, and something to begin with; the K blocks of t cost every segment tiles of its own, which
 // take 313 clocks a K block however few rows they have. us by itself / as K blocks (segments x
-// rows, n x k, rank): 1536 x 1536, 16: 64 x 1 20.1 / 50.0, 64 x 32 37.1 / 50.6, 64 x 64 60.3 / 51.4,
-// 16 x 32 23.6 / 24.2, 16 x 128 36.0 / 31.1, 4 x 256 25.1 / 26.2, 1 x 1560 33.1 / 26.9; rank 64: 64 x 16
-// 44.6 / 53.3, 64 x 32 72.0 / 48.4, 1 x 64 18.7 / 15.1; 1536 x 4096, 16: 64 x 64 85.9 / 109, 16 x 128
-// 45.8 / 47.2, 1 x 1560 42.6 / 40.9; 8960 x 1536, 16: 64 x 64 172 / 208, 16 x 128 94.6 / 69.5, 1 x 64
-// 27.1 / 16.8; 1536 x 8960, 32, fp32: 16 x 128 107 / 116, 4 x 1024 198 / 145.
+// rows, n x k, rank): 1536 x 1536, 16: 64 x 1 18.5 / 48.3, 64 x 32 32.5 / 50.4, 64 x 64 53.3 / 51.2,
+// 16 x 32 20.8 / 23.6, 16 x 128 31.3 / 31.5, 4 x 256 23.7 / 19.4, 1 x 1560 29.4 / 22.3; rank 64: 64 x 16
+// 42.4 / 52.2, 64 x 32 69.5 / 46.8, 1 x 64 17.9 / 14.4; 1536 x 4096, 16: 64 x 64 78.4 / 110, 16 x 128
+// 42.0 / 46.6, 1 x 256 27.0 / 22.6 (taken by itself all the same), 1 x 1560 39.0 / 29.5; 8960 x 1536, 16:
+// 64 x 64 159 / 208, 16 x 128 88.7 / 70.2, 1 x 64 26.3 / 14.8; 1536 x 8960, 32, fp32: 16 x 128 107 / 120,
+// 4 x 1024 198 / 150.
 bool short_segments(const AdapterArgs& g, int n_ft) {
   const double n = g.n, k = g.k, r = g.rank, blocks = (k + BK - 1) / BK;
   const double row = 1.1e-7 * r * n + 4e-8 * r * k + 0.003, first = n / 850 * (r / 32 + 0.5);
