@@ -472,7 +472,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<PARTS>::THREAD
     uint8_t* tiles = epi_smem + we * 2 * EPI_TILE;
     int acc = 0, buf = 0;
     uint32_t acc_phase = 0;
-    bool waited = DOWN;
     auto first_feature = [&](const Tile& q) {
       return ((DOWN ? 0 : 2 * q.f) + (int)rank) * W_ROWS + quarter * 32;
     };
@@ -499,10 +498,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Warps<PARTS>::THREAD
       const bool partly = split && ((t == cut.t0 && cut.k0 > 0) || (t == cut.t1 && cut.k1 > 0));
       // (the kernel before forms the low-rank part, or t, whose cut tiles' parts and counters lie in
       // the same place)
-      if (!waited && (g.delta || partly)) {
-        griddep_wait();
-        waited = true;
-      }
+      if (!DOWN && (g.delta || partly)) griddep_wait();
       if (partly) group = we >> 2;  // (every cluster's warps take the same chunks)
       // sums in parts: added up here as they are done, a part's accumulator going back at once
       float sum[PARTS ? F32_T / GROUPS : 1];
