@@ -18,23 +18,27 @@
 //  * warps 2-9: softmax, one row per thread, warps 2-5 tile A, 6-9 tile B: running maximum and
 //    sum in fp32 registers, P = exp2(scale log2(e) s - m) as bf16 over S in TMEM (its rounding is
 //    random from key to key and averages out in O, at most 2^-8 of a term), O rescaled in TMEM
-//    only when the maximum grew by more than 2^8. The sum is of the unrounded values.
+//    only when the maximum grew by more than 2^8. The sum is of the unrounded values. Its code is kept
+//    short, since an item's end and the next one's start run as fast as their instructions arrive: masked
+//    scores become -inf in TMEM by a loop over 32 at a time, and exponentials are taken 64 at a time from a
+//    second read (both unrolled over the 128 registers of the first read: 128 us for those 110).
 //  * warp 10: masks. A weight of zero does not stop a NaN in V, so the V rows of masked keys, and
 //    of what follows the last key up to a multiple of 16, are overwritten by zeros in shared
 //    memory once they have landed; with a mask it also lays out each key tile's 128 bits for the
 //    softmax, which takes masked scores as -inf by selection.
-//  * warp 11: fetches the CTA's segments (whole items, parts of cut ones), one ahead.
+//  * warp 11: fetches the CTA's segments (whole items, parts of cut ones), up to three ahead (with one
+//    ahead 115 us where three take 110: 32 sequences of 1560 rows on 20 to 512 keys).
 // The last key tile's MMAs cover ceil16 of its keys. Every wait is bounded (mbar_wait): a role
 // that gives up records it and the kernel ends.
 //
 // Bounds: with many queries for each key the tensor pipe and the exponentials, 2 x 128 x 128 of both
-// in about 2600 clocks (32 candidates of 1560 rows, 12 heads of 128: 161 us, 0.98 PFLOP/s, for 512 shared
-// keys, 419 us, 1.14 PFLOP/s, for 1560 own ones; 4096 rows on 8191 keys in cut items: 151 us, 1.37), with
+// in about 2600 clocks (32 candidates of 1560 rows, 12 heads of 128: 149 us, 1.05 PFLOP/s, for 512 shared
+// keys, 388 us, 1.23 PFLOP/s, for 1560 own ones; 4096 rows on 8191 keys in cut items: 147 us, 1.40), with
 // tokens on long states the bytes of K and V (64 requests, 4 kv heads of 128, 32 to 4096 keys, 92 MB:
-// 32.5 us, of which 22 stream K and V at the rate of a copy; 38 us with one kv head at a time). What
-// is left beside them: 4 to 5 us from launch to the first scores, 3000 to 4000 clocks of an item's end in
-// which the next one's scores wait for the rows' stores (which take as long in 128-byte pieces, and
-// through shared memory and TMA with a ring of two K tiles), and the joining of cut items.
+// 28.5 us, half of it at the rate of a copy). What is left beside them: 4 to 5 us from launch to the first
+// scores, some 3000 clocks at an item's end until the next one's scores are looked at (tried without gain:
+// rows stored in 128-byte pieces, or through shared memory and TMA with a ring of two K tiles; slower, as
+// longer code: rows that leave TMEM only before the next item's P), and the joining of cut items.
 #include <cudaTypedefs.h>
 
 #include <cfloat>
@@ -48,7 +52,8 @@ constexpr int SUB = TB * 64 * 2;     // 128 rows x 64 bf16: one swizzle width
 constexpr int THREADS = 384;
 constexpr uint32_t TMEM_COLS = 512;  // S|P of A [0,128), of B [128,256), O of A [256, ..), of B [384, ..)
 constexpr uint32_t O_COL = 256;
-constexpr int SEGS = 2;             // ring of segments: the current one and one ahead
+constexpr int SEGS = 4;              // ring of segments: the current one and those ahead
+constexpr int TAIL = 768;            // bytes of barriers and masks
 constexpr int MASKS = 8;             // ring of key tiles' masks (> V slots + 2: see the mask warp)
 
 template <int D>
@@ -56,7 +61,7 @@ struct Shape {
   static constexpr int SUBS = D / 64, TILE = SUBS * SUB;  // bytes of a Q, K or V tile
   static constexpr int KS = D == 128 ? 3 : 6, VS = D == 128 ? 2 : 5;  // ring slots (KS >= VS)
   static constexpr int RING = (2 + KS + VS) * TILE;
-  static constexpr int SMEM = RING + 512;                 // + barriers and masks
+  static constexpr int SMEM = RING + TAIL;
   static_assert(KS >= VS && MASKS > VS + 2, "rings");
 };
 
@@ -81,20 +86,6 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}
-// maximum of a row's 128 scores, in eight chains of three-input maxima
-__device__ __forceinline__ float rowmax128(const float* s) {
-  float m[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) m[k] = fmax3(s[k], s[k + 8], s[k + 16]);
-#pragma unroll
-  for (int i = 24; i + 16 <= 120; i += 16) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) m[k] = fmax3(m[k], s[i + k], s[i + 8 + k]);
-  }
-#pragma unroll
-  for (int k = 0; k < 8; ++k) m[k] = fmaxf(m[k], s[120 + k]);
-  return fmax3(fmax3(m[0], m[1], m[2]), fmax3(m[3], m[4], m[5]), fmaxf(m[6], m[7]));
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -433,24 +424,17 @@ struct Items {
 // ---- one row's results ------------------------------------------------------------------
 // 32 columns of a row, scaled and rounded, in 32-byte stores where the rows allow it.
 __device__ __forceinline__ void store32(bf16* to, bool st32, const uint32_t* u, float inv) {
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    w[i] = pack_bf16x2(__uint_as_float(u[2 * i]) * inv, __uint_as_float(u[2 * i + 1]) * inv);
   if (st32) {
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      uint32_t w[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        w[i] = pack_bf16x2(__uint_as_float(u[q * 16 + 2 * i]) * inv,
-                           __uint_as_float(u[q * 16 + 2 * i + 1]) * inv);
-      store_b32x8(to + q * 16, w);
-    }
+    for (int q = 0; q < 2; ++q) store_b32x8(to + q * 16, w + q * 8);
   } else {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      float v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[q * 8 + i]) * inv;
-      store_bf16x8(to + q * 8, v);
-    }
+    for (int q = 0; q < 4; ++q)
+      reinterpret_cast<uint4*>(to)[q] = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
   }
 }
 
@@ -584,8 +568,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* p_full = s_full + 2;
   uint64_t* o_done = p_full + 2;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(o_done + 2);
-  uint4* masks = reinterpret_cast<uint4*>(smem + Shape<D>::RING + 512 - 16 * MASKS);  // [MASKS]
-  static_assert(8 * (4 + 2 * KS + 2 * VS + MASKS + 2 * SEGS + 6) + 8 <= 512 - 16 * MASKS, "barriers");
+  uint4* masks = reinterpret_cast<uint4*>(smem + Shape<D>::RING + TAIL - 16 * MASKS);  // [MASKS]
+  static_assert(8 * (4 + 2 * KS + 2 * VS + MASKS + 2 * SEGS + 6) + 8 <= TAIL - 16 * MASKS, "barriers");
   __shared__ Plan plan;
   __shared__ uint3 scan[THREADS / 32];
   __shared__ Seg segs[SEGS], parts[8];
@@ -1061,36 +1045,51 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!scores_ready(i == steps - 1)) { failed = true; break; }
         tc_fence_after();
         const int valid = keys - i * TB;
-        uint32_t mk[4] = {~0u, ~0u, ~0u, ~0u};
+        // the keys that there are, 32 to a word; the other scores become -inf where they are
+        const uint32_t* mask = reinterpret_cast<const uint32_t*>(masks + kt % MASKS);
+        bool all = valid >= TB;
         if (MASKED) {
           const bool seen = mbar_wait(&m_full[kt % MASKS], (kt / MASKS) & 1, err);
           if (!__all_sync(0xffffffffu, seen)) { failed = true; break; }
-          const uint4 w = masks[kt % MASKS];
-          mk[0] = w.x;
-          mk[1] = w.y;
-          mk[2] = w.z;
-          mk[3] = w.w;
-        }
-        const bool all = MASKED ? (mk[0] & mk[1] & mk[2] & mk[3]) == ~0u : valid >= TB;
-        float s[128];
-        {
-          uint32_t u[128];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(lane_base + s_col + c * 32, u + c * 32);
-          tmem_ld_wait();
-#pragma unroll
-          for (int c = 0; c < 4; ++c) reg_fence32(u + c * 32);
-#pragma unroll
-          for (int e = 0; e < 128; ++e) s[e] = __uint_as_float(u[e]);
+          all = (mask[0] & mask[1] & mask[2] & mask[3]) == ~0u;
         }
         if (!all) {
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            const int n = valid - c * 32;
+            const uint32_t on = MASKED ? mask[c] : n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+            if (on == ~0u) continue;
+            uint32_t u[32];
+            tmem_ld32(lane_base + s_col + c * 32, u);
+            tmem_ld_wait();
+            reg_fence32(u);
 #pragma unroll
-          for (int e = 0; e < 128; ++e)
-            if (MASKED ? !((mk[e / 32] >> (e % 32)) & 1) : e >= valid) s[e] = -INFINITY;
+            for (int e = 0; e < 32; ++e)
+              if (!((on >> e) & 1)) u[e] = 0xff800000u;
+            tmem_st32(lane_base + s_col + c * 32, u);
+          }
+          tmem_st_wait();
+        }
+        float top[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top[k] = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t u[64];
+          tmem_ld32(lane_base + s_col + c * 64, u);
+          tmem_ld32(lane_base + s_col + c * 64 + 32, u + 32);
+          tmem_ld_wait();
+          reg_fence32(u);
+          reg_fence32(u + 32);
+#pragma unroll
+          for (int e = 0; e < 64; e += 16)
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              top[k] = fmax3(top[k], __uint_as_float(u[e + k]), __uint_as_float(u[e + 8 + k]));
         }
         // (at least the lowest finite value: a row without a key so far has exponentials of
         // exp2(-inf) = 0 and joins others with a factor of 0)
-        const float mx = fmaxf(rowmax128(s) * p.scale_log2, -FLT_MAX);
+        const float mx = fmaxf(fmax3(fmax3(top[0], top[1], top[2]), fmax3(top[3], top[4], top[5]), fmaxf(top[6], top[7])) * p.scale_log2, -FLT_MAX);
         if (__all_sync(0xffffffffu, m_used == -INFINITY)) {  // the segment's first tile
           m_used = mx;
         } else if (__any_sync(0xffffffffu, mx > m_used + 8.f)) {
@@ -1112,28 +1111,20 @@ __global__ void __launch_bounds__(THREADS, 1)
         const uint64_t sc2 = f2_join(p.scale_log2, p.scale_log2);
         const uint64_t nm2 = f2_join(-m_used, -m_used);
         uint64_t ls2[2] = {0ull, 0ull};
-        // keys 0-63 from the registers, keys 64-127 read again (P of keys 0-63 only overwrites
-        // columns 0-31): the first half need not keep them
-#pragma unroll
+        // read again, half by half (P of keys 0-63 only overwrites columns 0-31): code for one half, and the
+        // first read's registers need not be kept
+#pragma unroll 1
         for (int c = 0; c < 2; ++c) {
           float h[64];
-          if (c == 0) {
-#pragma unroll
-            for (int e = 0; e < 64; ++e) h[e] = s[e];
-          } else {
+          {
             uint32_t u2[64];
-            tmem_ld32(lane_base + s_col + 64, u2);
-            tmem_ld32(lane_base + s_col + 96, u2 + 32);
+            tmem_ld32(lane_base + s_col + c * 64, u2);
+            tmem_ld32(lane_base + s_col + c * 64 + 32, u2 + 32);
             tmem_ld_wait();
             reg_fence32(u2);
             reg_fence32(u2 + 32);
 #pragma unroll
             for (int e = 0; e < 64; ++e) h[e] = __uint_as_float(u2[e]);
-            if (!all) {
-#pragma unroll
-              for (int e = 0; e < 64; ++e)
-                if (MASKED ? !((mk[2 + e / 32] >> (e % 32)) & 1) : 64 + e >= valid) h[e] = -INFINITY;
-            }
           }
           uint32_t u[32];
 #pragma unroll
@@ -1313,9 +1304,9 @@ cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* er
   p.ldo = c.ldo;
   p.scale_log2 = c.scale * 1.4426950408889634f;
   // Two kv heads side by side keep twice as much of K and V on its way (64 tokens of 4 kv heads on 32 to
-  // 4096 keys: 32.5 us for 38), but a step of both takes 3500 clocks for one's 2600: only where every CTA
+  // 4096 keys: 28.5 us for 30.9), but a step of both takes 3500 clocks for one's 2600: only where every CTA
   // has more than one to do. With longer sequences the items have two query tiles for the most part, and
-  // the kernel without that takes 161 us for 171 (32 of 1560 rows on 512 keys).
+  // the kernel without that takes 149 us for 161 (32 of 1560 rows on 512 keys).
   const long long seqs = c.seqs < c.q_rows ? c.seqs : c.q_rows;
   p.dual = seqs * c.kv_heads > num_sms && c.q_rows <= seqs * p.rq;
   const long long tiles = (c.kv_rows + TB - 1) / TB;

@@ -483,10 +483,10 @@ def test_cross_scratch_failure_leaves_the_model_usable():
 
 
 def test_cross_wait_runs_out_then_recovers(model):
-    """Four items or so for each SM, of 32 key tiles: an item's place in the ring of two comes free after
-    some 40 us, past a limit of a microsecond on that wait. The call reports it, and the next ones are as
+    """More than four items for each SM, of 32 key tiles: an item's place in the ring of four comes free
+    after some 40 us, past a limit of a microsecond on that wait. The call reports it, and the next ones are as
     before, with whole items and with cut ones."""
-    whole_items = Cross([200] * 160, [4096], heads=4, kv_of=[0] * 160, seed=27)
+    whole_items = Cross([200] * 300, [4096], heads=4, kv_of=[0] * 300, seed=27)
     cut_items = Cross([3, 40], [4000, 9000], seed=28)
     model.op_cross_attention(whole_items.args)
     ref = whole_items.out.clone()
