@@ -1225,7 +1225,7 @@ void side_by_side(const AdapterArgs& g, int n_ft, Plan* p) {
   const int all = p->clusters;
   for (int T = 128; T <= (p->parts ? F32_T : MAX_T); T += T_STEP) {
     const long long tiles = (long long)(g.rows / T + g.segments) * n_ft;
-    if (tiles > all - all / 8) continue;
+    if (tiles > all - (all < 8 ? 1 : all / 8)) continue;  // (at least one is left for t)
     p->clusters = (int)tiles;
     p->down_clusters = all - (int)tiles;
     return;

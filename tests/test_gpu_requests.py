@@ -409,6 +409,17 @@ def test_adapter_cut_tiles_of_t_and_the_product(model, segments, of, K):
         assert torch.equal(first, c.out)
 
 
+@pytest.mark.parametrize("sms", [2, 4, 6, 16])
+@pytest.mark.parametrize("segments,of,N", [([100], [0], 264), ([100], [0], 8), ([90, 100, 3], [1, -1, 0], 520)])
+def test_adapter_as_many_tiles_as_clusters(model, sms, segments, of, N):
+    """Every cluster of the few has a tile of the product, or nearly: t's kernel still has one."""
+    model.set_sm_budget(sms)
+    try:
+        Adapters(segments, of, N=N, K=64, rank=256, seed=39).check(model)
+    finally:
+        model.set_sm_budget(0)
+
+
 def test_adapter_same_result_every_time_and_on_few_sms(model):
     for segments, of in (([1] * 50, [i % 5 for i in range(50)]), ([400, 300, 9], [0, -1, 1]), ([6], [0]), LONG):
         c = Adapters(segments, of, N=1536, K=1544, rank=16, seed=22)
