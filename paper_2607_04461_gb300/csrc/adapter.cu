@@ -21,6 +21,10 @@
 // fp32 results take K in parts of 4 blocks, each in an accumulator of its own, which the epilogue
 // adds up (the tensor core's sums lose about 6e-8 of the result per K block of 64). So do results of
 // a K past 2^17.
+// Bounds: with many rows the tensor pipe under the power cap (24960 rows, 8960 x 1536, rank 64: 430 us, 1.6
+// PFLOP/s, t's 26 among them); with one round of tiles the SM's operand rate, some 45 bytes a clock (1560
+// rows, 1536 x 8960, rank 32, fp32: 58 us, K blocks of 256 x 192 590 clocks); with few rows latency (see
+// adapter_delta_kernel).
 // Every wait is bounded (mbar_wait): a role that gives up records it and the kernel ends.
 #include <atomic>
 #include <climits>
@@ -1016,10 +1020,13 @@ __global__ void __cluster_dims__(D_CTAS, 1, 1) __launch_bounds__(D_THREADS, MT =
 }
 
 // ---- few rows ---------------------------------------------------------------------------
-// Up to 32 rows read every weight once: a block takes 16 weight rows, its warps split K, and the
-// weights go straight from memory into the operand registers of mma.sync (the weights are the M
+// Up to 32 rows read every weight once, up to 64 twice: a block takes 16 weight rows, its warps split K,
+// and the weights go straight from memory into the operand registers of mma.sync (the weights are the M
 // side, eight rows of x the N side), as in the products grouped by expert. The weights do not wait
-// for the low-rank part; the epilogue does.
+// for the low-rank part; the epilogue does. One row, 1536 x 1536, rank 16: 6.0 us with the low-rank part's
+// kernel (in tiles 12), whose latency and its own are all there is. 32 rows at a time with two steps of K
+// on their way, two blocks an SM, against 16 with four: 5120 x 5120 21.0 us for 26.1; 16 rows with three
+// steps, three blocks, 11.5 for 15.6.
 constexpr int FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32, FEW_LONG_K = 2048;
 
 template <bool EXACT, int NT, int UN, int BLOCKS>
@@ -1203,7 +1210,7 @@ size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 // reading A_e and B_e for every 16 rows, multiplying them by CUDA cores, and writing and reading the
 // part, and something to begin with; the K blocks of t cost every segment tiles of its own, which
 // take 313 clocks a K block however few rows they have. us by itself / as K blocks (segments x
-// rows, n x k, rank): 1536 x 1536, 16: 64 x 1 18.5 / 48.3, 64 x 32 32.5 / 50.4, 64 x 64 53.3 / 51.2,
+// rows, n x k, rank): 1536 x 1536, 16: 64 x 4 19.2 / 48.6, 64 x 32 32.5 / 50.4, 64 x 64 53.3 / 51.2,
 // 16 x 32 20.8 / 23.6, 16 x 128 31.3 / 31.5, 4 x 256 23.7 / 19.4, 1 x 1560 29.4 / 22.3; rank 64: 64 x 16
 // 42.4 / 52.2, 64 x 32 69.5 / 46.8, 1 x 64 17.9 / 14.4; 1536 x 4096, 16: 64 x 64 78.4 / 110, 16 x 128
 // 42.0 / 46.6, 1 x 256 27.0 / 22.6 (taken by itself all the same), 1 x 1560 39.0 / 29.5; 8960 x 1536, 16:
@@ -1240,7 +1247,13 @@ Plan plan_of(const AdapterArgs& g, int num_sms) {
   Plan p{};
   p.parts = in_parts(g);
   const int n_ft = (g.n + 2 * W_ROWS - 1) / (2 * W_ROWS);
-  p.few = g.rows <= 32 && n_ft <= num_sms / 2 * (g.rows <= 8 ? 2 : 1);
+  // Streamed weights: up to 8 rows at any rate, up to 32 unless there are tiles for all clusters, and up to
+  // 64 (the weights twice, the second time from L2) where the tiles leave most SMs without work and K is
+  // not long. us streamed / in tiles: 32 rows 9216 x 1536 17.7 / 20.7, 1536 x 8960 18.1 / 29.2; 64 rows
+  // 1536 x 1536 13.8 / 18.4, 4608 x 1536 16.8 / 21.4, 4096 x 4096 25.5 / 28.2, 5120 x 5120 37.8 / 31.6,
+  // 1536 x 8960 43.4 / 39.6, 9216 x 1536 26.7 / 22.4.
+  p.few = (g.rows <= 32 && n_ft <= num_sms / 2 * (g.rows <= 8 ? 2 : 1)) ||
+          (g.rows <= 64 && n_ft <= num_sms / 8 && g.k <= 4096);
   p.by_row = p.few || short_segments(g, n_ft);
   if (p.by_row)
     p.delta_bytes = padded((size_t)g.rows * g.n * sizeof(float));
@@ -1284,7 +1297,8 @@ cudaError_t run(const AdapterArgs& g, const Plan& p, uint8_t* ws, int* counters,
                        : launch_delta<4>(g, delta, err, st);
     if (e != cudaSuccess) return e;
     if (p.few) {
-      auto kern = g.rows > 8        ? adapter_few_kernel<PARTS, 2, 4, 2>
+      auto kern = g.rows > 16        ? adapter_few_kernel<PARTS, 4, 2, 2>
+                  : g.rows > 8       ? adapter_few_kernel<PARTS, 2, 3, 3>
                   : g.k > FEW_LONG_K ? adapter_few_kernel<PARTS, 1, 6, 2>
                                      : adapter_few_kernel<PARTS, 1, 4, 3>;
       return launch_k(kern, dim3((g.n + 15) / 16), dim3(FEW_THREADS), 0, st, g, (const float*)delta);
