@@ -1020,7 +1020,7 @@ __global__ void __cluster_dims__(D_CTAS, 1, 1) __launch_bounds__(D_THREADS, MT =
 }
 
 // ---- few rows ---------------------------------------------------------------------------
-// Up to 32 rows read every weight once, up to 64 twice: a block takes 16 weight rows, its warps split K,
+// Up to 32 rows read every weight once, up to 64 in two halves: a block takes 16 weight rows, its warps split K,
 // and the weights go straight from memory into the operand registers of mma.sync (the weights are the M
 // side, eight rows of x the N side), as in the products grouped by expert. The weights do not wait
 // for the low-rank part; the epilogue does. One row, 1536 x 1536, rank 16: 6.0 us with the low-rank part's
@@ -1043,7 +1043,7 @@ __global__ void __launch_bounds__(FEW_THREADS, BLOCKS)
   const int steps = (g.k + 31) / 32;
   const int s0 = steps * warp / FEW_WARPS, s1 = steps * (warp + 1) / FEW_WARPS;
   bool waited = false;
-  for (int p0 = 0; p0 < rows; p0 += 8 * NT) {
+  for (int p0 = 8 * NT * blockIdx.y; p0 < rows; p0 += 8 * NT * gridDim.y) {
     const bf16* x[NT];
     bool have[NT];
 #pragma unroll
@@ -1248,12 +1248,12 @@ Plan plan_of(const AdapterArgs& g, int num_sms) {
   p.parts = in_parts(g);
   const int n_ft = (g.n + 2 * W_ROWS - 1) / (2 * W_ROWS);
   // Streamed weights: up to 8 rows at any rate, up to 32 unless there are tiles for all clusters, and up to
-  // 64 (the weights twice, the second time from L2) where the tiles leave most SMs without work and K is
-  // not long. us streamed / in tiles: 32 rows 9216 x 1536 17.7 / 20.7, 1536 x 8960 18.1 / 29.2; 64 rows
-  // 1536 x 1536 13.8 / 18.4, 4608 x 1536 16.8 / 21.4, 4096 x 4096 25.5 / 28.2, 5120 x 5120 37.8 / 31.6,
-  // 1536 x 8960 43.4 / 39.6, 9216 x 1536 26.7 / 22.4.
+  // 64 (by two blocks a weight row, which both read it) where the tiles leave most SMs without work and the
+  // weights are not many. us streamed / in tiles: 32 rows 9216 x 1536 17.7 / 20.7, 1536 x 8960 18.1 / 29.2;
+  // 64 rows 1536 x 1536 12.1 / 18.4, 4608 x 1536 17.3 / 21.4, 4096 x 4096 25.5 / 28.2, 1536 x 8960 31.8 / 39.9,
+  // 4864 x 8960 52.2 / 41.9, 9216 x 1536 27.5 / 22.4; 40 rows 2048 x 16384 37.8 / 35.5.
   p.few = (g.rows <= 32 && n_ft <= num_sms / 2 * (g.rows <= 8 ? 2 : 1)) ||
-          (g.rows <= 64 && n_ft <= num_sms / 8 && g.k <= 4096);
+          (g.rows <= 64 && n_ft <= num_sms / 8 && (long long)g.n * g.k <= 20 << 20);
   p.by_row = p.few || short_segments(g, n_ft);
   if (p.by_row)
     p.delta_bytes = padded((size_t)g.rows * g.n * sizeof(float));
@@ -1301,7 +1301,7 @@ cudaError_t run(const AdapterArgs& g, const Plan& p, uint8_t* ws, int* counters,
                   : g.rows > 8       ? adapter_few_kernel<PARTS, 2, 3, 3>
                   : g.k > FEW_LONG_K ? adapter_few_kernel<PARTS, 1, 6, 2>
                                      : adapter_few_kernel<PARTS, 1, 4, 3>;
-      return launch_k(kern, dim3((g.n + 15) / 16), dim3(FEW_THREADS), 0, st, g, (const float*)delta);
+      return launch_k(kern, dim3((g.n + 15) / 16, g.rows > 32 ? 2 : 1), dim3(FEW_THREADS), 0, st, g, (const float*)delta);
     }
     a.groups = 1;
     a.end = g.offsets + g.segments;
