@@ -591,6 +591,50 @@ def test_two_models_at_once():
             m.set_stream(None)
 
 
+def test_cross_cache_past_32_bits(model):
+    """Keys, values, masks and rows behind 2^32 elements: as in buffers of their own."""
+    far, D, keys = 34_000_000, 64, 700
+    g = gen(40)
+    kv = torch.zeros(far + keys, 2 * D, dtype=BF, device="cuda")
+    kv[far:] = torch.randn(keys, 2 * D, generator=g, device="cuda").to(BF)
+    valid = torch.ones(far + keys, dtype=torch.uint8, device="cuda")
+    valid[far + 5::3] = 0
+    wide = 1 << 16  # row stride of q and out
+    rows = 66_000
+    q = torch.zeros(rows, wide, dtype=BF, device="cuda")[:, :2 * D]
+    out = torch.full((rows, wide), 7.0, dtype=BF, device="cuda")[:, :2 * D]
+    q[rows - 150:] = torch.randn(150, 2 * D, generator=g, device="cuda").to(BF)
+    assert (rows - 150) * wide > 1 << 32 and far * 2 * D > 1 << 32
+    model.op_cross_attention(fb.make_cross(q, kv[:, :D], kv[:, D:], out, whole([0, rows - 150, rows]),
+                                           whole([0, 0, far, far + keys]), head_dim=D, kv_of=whole([0, 2]), valid=valid))
+    near = torch.empty(150, 2 * D, dtype=BF, device="cuda")
+    model.op_cross_attention(fb.make_cross(q[rows - 150:].contiguous(), kv[far:, :D].contiguous(),
+                                           kv[far:, D:].contiguous(), near, whole([0, 150]), whole([0, keys]),
+                                           head_dim=D, valid=valid[far:].contiguous()))
+    assert (out[:rows - 150] == 0).all() and near.abs().sum() > 0
+    assert torch.allclose(out[rows - 150:].double(), near.double(), rtol=2 ** -7, atol=2 ** -7)
+
+
+@pytest.mark.parametrize("out_t", [BF, F32])
+def test_adapter_results_past_32_bits(model, out_t):
+    """More results than 2^32: the last rows as in a call of few."""
+    rows, N, K, rank = (1 << 21) + 77, 2056, 16, 8
+    g = gen(41)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    x, w, a, b = randn(rows, K).to(BF), randn(N, K).to(BF), randn(2, rank, K).to(BF), randn(2, N, rank).to(BF)
+    out = torch.zeros(rows, N, dtype=out_t, device="cuda")
+    assert rows * N > 1 << 32
+    model.op_adapter_gemm(fb.make_adapters(x, w, a, b, whole([0, 1000, rows]), whole([0, 1]), out))
+    for r, e in ((slice(0, 1000), 0), (slice(rows - 3000, rows), 1)):
+        part = torch.zeros(r.stop - r.start, N, dtype=out_t, device="cuda")
+        n = r.stop - r.start
+        model.op_adapter_gemm(fb.make_adapters(x[r].contiguous(), w, a, b, whole([0, n]), whole([e]), part))
+        size = x[r].double().abs() @ w.double().abs().T + \
+            (x[r].double().abs() @ a[e].double().abs().T) @ b[e].double().abs().T
+        unit = 2.0 ** -7 if out_t == BF else 1e-6
+        assert ((out[r].double() - part.double()).abs() <= unit * part.double().abs() + 2.0 ** -15 * size).all()
+
+
 # ---- together -------------------------------------------------------------------------
 
 def test_cross_sublayer_of_several_requests(model):
