@@ -1045,6 +1045,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!scores_ready(i == steps - 1)) { failed = true; break; }
         tc_fence_after();
         const int valid = keys - i * TB;
+        const int halves = valid > 64 ? 2 : 1;  // (without a key in the second half its P is not read)
         // the keys that there are, 32 to a word; the other scores become -inf where they are
         const uint32_t* mask = reinterpret_cast<const uint32_t*>(masks + kt % MASKS);
         bool all = valid >= TB;
@@ -1114,7 +1115,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         // read again, half by half (P of keys 0-63 only overwrites columns 0-31): code for one half, and the
         // first read's registers need not be kept
 #pragma unroll 1
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < halves; ++c) {
           float h[64];
           {
             uint32_t u2[64];
