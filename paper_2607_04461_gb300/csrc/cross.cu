@@ -35,7 +35,7 @@
 // in about 2600 clocks (32 candidates of 1560 rows, 12 heads of 128: 149 us, 1.05 PFLOP/s, for 512 shared
 // keys, 388 us, 1.23 PFLOP/s, for 1560 own ones; 4096 rows on 8191 keys in cut items: 147 us, 1.40), with
 // tokens on long states the bytes of K and V (64 requests, 4 kv heads of 128, 32 to 4096 keys, 92 MB:
-// 28.5 us, half of it at the rate of a copy). What is left beside them: 4 to 5 us from launch to the first
+// 28.3 us, half of it at the rate of a copy). What is left beside them: 4 to 5 us from launch to the first
 // scores, some 3000 clocks at an item's end until the next one's scores are looked at (tried without gain:
 // rows stored in 128-byte pieces, or through shared memory and TMA with a ring of two K tiles; slower, as
 // longer code: rows that leave TMEM only before the next item's P), and the joining of cut items.
@@ -1305,7 +1305,7 @@ cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* er
   p.ldo = c.ldo;
   p.scale_log2 = c.scale * 1.4426950408889634f;
   // Two kv heads side by side keep twice as much of K and V on its way (64 tokens of 4 kv heads on 32 to
-  // 4096 keys: 28.5 us for 30.9), but a step of both takes 3500 clocks for one's 2600: only where every CTA
+  // 4096 keys: 28.3 us for 30.9), but a step of both takes 3500 clocks for one's 2600: only where every CTA
   // has more than one to do. With longer sequences the items have two query tiles for the most part, and
   // the kernel without that takes 149 us for 161 (32 of 1560 rows on 512 keys).
   const long long seqs = c.seqs < c.q_rows ? c.seqs : c.q_rows;
