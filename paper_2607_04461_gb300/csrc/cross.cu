@@ -567,9 +567,10 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* s_full = g_empty + SEGS;  // [2 groups]
   uint64_t* p_full = s_full + 2;
   uint64_t* o_done = p_full + 2;
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(o_done + 2);
+  uint64_t* begun = o_done + 2;  // the first K tile and its Q are on their way: one phase, never begun again
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(begun + 1);
   uint4* masks = reinterpret_cast<uint4*>(smem + Shape<D>::RING + TAIL - 16 * MASKS);  // [MASKS]
-  static_assert(8 * (4 + 2 * KS + 2 * VS + MASKS + 2 * SEGS + 6) + 8 <= TAIL - 16 * MASKS, "barriers");
+  static_assert(8 * (4 + 2 * KS + 2 * VS + MASKS + 2 * SEGS + 7) + 8 <= TAIL - 16 * MASKS, "barriers");
   __shared__ Plan plan;
   __shared__ uint3 scan[THREADS / 32];
   __shared__ Seg segs[SEGS], parts[8];
@@ -599,6 +600,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&p_full[s], 4);
       mbar_init(&o_done[s], 1);
     }
+    mbar_init(begun, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma_prefetch_desc(&tmQ);
     tma_prefetch_desc(&tmK);
@@ -652,6 +654,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                               is_dual(sg) ? sg.row : sg.row + g * p.rq);
               }
               if (failed) break;
+              if (t == 0) mbar_arrive(begun);
             }
           }
         } else {
@@ -664,8 +667,10 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (t >= VS) {
               const uint32_t a = t - VS + (DUAL && ((was_dual >> (VS - 2)) & 3) ? 2 : 1);
               if (!mbar_wait(&k_empty[a % KS], (a / KS) & 1, err)) { failed = true; break; }
-            } else if (t == 0) {  // the first K and Q come before everything else
-              if (!mbar_wait(&k_full[0], 0, err)) { failed = true; break; }
+            } else if (t == 0) {
+              // The first K and Q come before everything else. (Not by their own barriers: S needs no V,
+              // so that their slots may be on the next phase, and the one after it, before this lane looks.)
+              if (!mbar_wait(begun, 0, err)) { failed = true; break; }
             }
             was_dual = was_dual << 1 | (uint32_t)is_dual(sg);
             uint64_t* bar = MASKED || (sg.keys - j * TB < TB && sg.keys % 16) ? &v_land[s] : &v_full[s];

@@ -681,3 +681,21 @@ def test_cross_sublayer_of_several_requests(model):
         err = (out[rows].double() - h[rows].double() - step).norm() / step.norm()
         # four roundings to bf16 on the way (k, v, q, weights, o), 2^-8 each at most
         assert err < 5 * 2.0 ** -8, (i, err)
+
+
+@pytest.mark.parametrize("D,queries,keys", [(128, [1] * 3, [4000, 1300, 900]), (128, [300], [5000]), (64, [2, 200], [6000, 2100])])
+def test_cross_first_tiles_of_every_cta(model, D, queries, keys):
+    """More key tiles for a CTA than its rings hold, from the first one on, over many launches: K's ring
+    may be ahead of V's first load by as much as it holds."""
+    c = Cross(queries, keys, heads=4, kv_heads=4, D=D, valid=0.1, seed=50)
+    c.check(model)
+    first = c.out.clone()
+    fb.fb_set_op_repeat(model.handle, 50)
+    try:
+        for _ in range(4):
+            c.out.fill_(7.0)
+            model.op_cross_attention(c.args)
+            torch.cuda.synchronize()
+            assert torch.equal(first, c.out)
+    finally:
+        fb.fb_set_op_repeat(model.handle, 1)

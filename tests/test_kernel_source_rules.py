@@ -64,3 +64,16 @@ def test_noalloc_entry_point_allocates_nothing():
         assert bad not in body, bad
     assert body.count("cudaGetSymbolAddress") == 3
     assert re.search(r"static __device__ __align__\(256\) float g_na_ws\[", src)
+
+
+def test_loaders_of_cross_attention_wait_for_no_phase_that_can_pass_them():
+    """A wait for a phase's parity is only safe where the barrier cannot complete the phase behind it
+    before the waiter has looked. The loaders' own full barriers can: scores need K and Q alone, so K
+    slots go round while the lane that loads V stands still (it then never loads V, and the kernel
+    ends at its time limit). The loading warp waits for free slots and for a barrier of one phase."""
+    src = open(os.path.join(CSRC, "cross.cu")).read()
+    at = src.index("TMA: lane 0")
+    waited = set(re.findall(r"mbar_wait\w*\(&?(\w+)", src[at:src.index("MMA issuer", at)]))
+    assert waited == {"g_full", "k_empty", "q_empty", "begun"}, waited
+    # begun: arrived at once, by the first key tile's load
+    assert re.findall(r"[^;\n]*mbar_arrive\(begun\)", src) == ["              if (t == 0) mbar_arrive(begun)"]
