@@ -699,3 +699,27 @@ def test_cross_first_tiles_of_every_cta(model, D, queries, keys):
             assert torch.equal(first, c.out)
     finally:
         fb.fb_set_op_repeat(model.handle, 1)
+
+
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("heads,kv_heads", [(2, 2), (4, 2), (3, 1), (5, 1), (6, 2)])
+@pytest.mark.parametrize("valid", [None, 0.2])
+def test_cross_row_does_not_depend_on_its_neighbours(model, D, heads, kv_heads, valid):
+    """A few rows of a tile, with other sequences' behind them, or none: the same bits. The neighbours'
+    scores grow from key tile to key tile by far more than the rows' own."""
+    c = Cross([5, 60, 1], [700, 300], heads=heads, kv_heads=kv_heads, D=D, kv_of=[0, 0, 1], valid=valid, seed=51)
+    own = c.q[:5].clone()
+    results = []
+    for spread, signs in ((0.0, 1.0), (1.0, 1.0), (30.0, 1.0), (30.0, -1.0)):
+        c.q[5:] = (spread * signs * torch.randn(c.q[5:].shape, generator=gen(52), device="cuda")).to(BF)
+        assert torch.equal(c.q[:5], own)
+        c.out.fill_(7.0)
+        c.check(model)
+        results.append(c.out[:5].clone())
+    alone = Cross([5], [700, 300], heads=heads, kv_heads=kv_heads, D=D, kv_of=[0], seed=51, extra_rows=0)
+    alone.args = fb.make_cross(own, c.k, c.v, alone.out, whole([0, 5]), whole([0, 700, 1000]), head_dim=D,
+                               kv_of=whole([0]), valid=c.valid)
+    model.op_cross_attention(alone.args)
+    results.append(alone.out)
+    for r in results[1:]:
+        assert torch.equal(results[0], r)
