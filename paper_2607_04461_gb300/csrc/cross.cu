@@ -1257,8 +1257,9 @@ long long most_items(const CrossArgs& c) {
 }
 // Whether items may be worth cutting. With eight rounds of them for each CTA they are not, and
 // neither are ones that all run side by side and have at most seven key tiles: the least that a cut
-// costs is then more than the item (see make_plan).
+// costs is then more than the item (see make_plan). Without a key there is nothing to cut.
 bool may_cut(const CrossArgs& c, int num_sms) {
+  if (c.kv_rows == 0) return false;
   const long long fewest = (long long)c.q_rows / (2 * rows_of_tile(c)) * c.kv_heads;
   return fewest < 8ll * num_sms && (c.kv_rows > 7 * TB || most_items(c) > num_sms);
 }

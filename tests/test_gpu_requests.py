@@ -723,3 +723,23 @@ def test_cross_row_does_not_depend_on_its_neighbours(model, D, heads, kv_heads, 
     results.append(alone.out)
     for r in results[1:]:
         assert torch.equal(results[0], r)
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("queries,heads,kv_heads,D,sms", [
+    ([4096], 12, 12, 128, 0), ([5], 6, 6, 64, 4), ([1] * 200, 4, 2, 64, 0), ([3, 0, 300], 3, 1, 128, 2), ([1], 1, 1, 64, 0),
+])
+def test_cross_no_key_at_all(model, queries, heads, kv_heads, D, sms, masked):
+    """Key buffers of no row, with more items than SMs and fewer: zeros."""
+    rows = sum(queries) + 2
+    q = torch.randn(rows, heads * D, generator=gen(53), device="cuda").to(BF)
+    k = torch.empty(0, kv_heads * D, dtype=BF, device="cuda")
+    out = torch.full_like(q, 7.0)
+    valid = torch.empty(0, dtype=torch.uint8, device="cuda") if masked else None
+    args = fb.make_cross(q, k, k, out, whole(offsets(queries)), whole([0] * (len(queries) + 1)), head_dim=D, valid=valid)
+    model.set_sm_budget(sms)
+    try:
+        model.op_cross_attention(args)
+    finally:
+        model.set_sm_budget(0)
+    assert (out[:-2] == 0).all() and (out[-2:] == 7.0).all()
