@@ -85,6 +85,9 @@ fb_status fb_init_model(const fb_cfg* cfg, const float* weights_host, fb_model**
  * model owns (device memory, its own streams, events, the pinned error word). NULL is
  * allowed. A stream given with fb_set_stream stays the caller's. */
 void fb_free(fb_model* m);
+/* fb_model_device: the device that was current when the model was made, on which it lives and whose
+ * memory its calls take (-1 for NULL). */
+int fb_model_device(const fb_model* m);
 /* stream: a cudaStream_t (NULL = the model's own stream). */
 fb_status fb_set_stream(fb_model* m, void* stream);
 /* fb_set_sm_budget: the number of SMs the model's launches may occupy (0 = all of the

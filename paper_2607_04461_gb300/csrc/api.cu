@@ -1574,6 +1574,8 @@ fb_status fb_init_model(const fb_cfg* cfg, const float* weights_host, fb_model**
   return FB_OK;
 }
 
+int fb_model_device(const fb_model* m) { return m ? m->dev : -1; }
+
 fb_status fb_set_stream(fb_model* m, void* stream) {
   if (!m) return fail(FB_EINVAL, "model is NULL");
   CK(cudaStreamSynchronize(m->st));

@@ -124,7 +124,7 @@ EXPORTS = ["fb_weights_count", "fb_weights_entry", "fb_init_model", "fb_free", "
            "fb_test_request_handover", "fb_test_attention_split", "fb_test_plan_traffic",
            "fb_probe_mma_rate", "fb_probe_mma_gap", "fb_probe_mufu", "fb_probe_tmem_load",
            "fb_probe_mma_mix", "fb_op_sandwich_norm", "fb_op_route", "fb_op_expert_gemm",
-           "fb_moe_forward", "fb_op_cross_attention", "fb_op_adapter_gemm"]
+           "fb_moe_forward", "fb_op_cross_attention", "fb_op_adapter_gemm", "fb_model_device"]
 
 PAIR_VERIFIER = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
                                  ctypes.POINTER(ctypes.c_int))
@@ -171,6 +171,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "fb_state_offload": (I, [P, I, I, ctypes.POINTER(P)]),
         "fb_state_wait": (I, [P]),
         "fb_set_sm_budget": (I, [P, I]),
+        "fb_model_device": (I, [P]),
         "fb_sm_split_create": (I, [I, ctypes.POINTER(P)]),
         "fb_sm_split_info": (I, [P, I, ctypes.POINTER(P), ctypes.POINTER(I)]),
         "fb_sm_split_free": (None, [P]),
@@ -288,6 +289,11 @@ def fb_set_stream(model: int, stream) -> None:
     """stream: a torch.cuda.Stream, a raw cudaStream_t int, or None (model's own)."""
     s = getattr(stream, "cuda_stream", stream)
     _check(load_library().fb_set_stream(model, s))
+
+
+def fb_model_device(model: int) -> int:
+    """The device that the model lives on."""
+    return load_library().fb_model_device(model)
 
 
 def fb_set_sm_budget(model: int, n_sms: int) -> None:
@@ -739,10 +745,21 @@ def fb_moe_forward(model: int, moe: fb_moe, a, sandwich: fb_sandwich, valid=None
 # ---- several requests in one batch --------------------------------------------------------
 
 def _one_device(**tensors):
-    """All tensors lie on one device (the library reads them on the model's)."""
+    """The one device that all tensors lie on (the library reads them on the model's, see
+    _on_model)."""
     found = {name: x.device.index for name, x in tensors.items() if x is not None}
     if len(set(found.values())) > 1:
         raise ValueError(f"tensors on several devices: {found}")
+    return next(iter(found.values()))
+
+
+def _on_model(model, args):
+    """Refuses tensors of another device than the model's, whose addresses mean nothing there.
+    (Structures filled in by hand say nothing about their device.)"""
+    device = getattr(args, "_device", None)
+    if device is not None and device != load_library().fb_model_device(model):
+        raise ValueError(f"tensors on device {device}, the model on device "
+                         f"{load_library().fb_model_device(model)}")
 
 
 def make_cross(q, k, v, out, q_offsets, kv_offsets, head_dim=128, kv_of=None, valid=None, scale=0.0):
@@ -765,8 +782,8 @@ def make_cross(q, k, v, out, q_offsets, kv_offsets, head_dim=128, kv_of=None, va
     c.kv_offsets = _tensor("kv_offsets", kv_offsets, ("int32",), (None,))
     c.kv_of = _tensor("kv_of", kv_of, ("int32",), (c.seqs,))
     c.valid = _tensor("valid", valid, ("uint8",), (k.shape[0],))
-    _one_device(q=q, k=k, v=v, out=out, q_offsets=q_offsets, kv_offsets=kv_offsets, kv_of=kv_of,
-                valid=valid)
+    c._device = _one_device(q=q, k=k, v=v, out=out, q_offsets=q_offsets, kv_offsets=kv_offsets,
+                            kv_of=kv_of, valid=valid)
     c._keep = (q, k, v, out, q_offsets, kv_offsets, kv_of, valid)
     return c
 
@@ -794,17 +811,19 @@ def make_adapters(x, w, a, b, offsets, adapter, out, scale=None, bias=None, act=
         g.resid, g.ldr = _tensor("resid", resid, f32, (rows, n), True), _row_stride(resid)
     g.out, g.out_type = _tensor("out", out, _FLOATS, (rows, n), True), _type(out)
     g.ldo = _row_stride(out)
-    _one_device(x=x, w=w, a=a, b=b, scale=scale, bias=bias, gate=gate, offsets=offsets,
-                adapter=adapter, resid=resid, out=out)
+    g._device = _one_device(x=x, w=w, a=a, b=b, scale=scale, bias=bias, gate=gate, offsets=offsets,
+                            adapter=adapter, resid=resid, out=out)
     g._keep = (x, w, a, b, offsets, adapter, out, scale, bias, resid, gate)
     return g
 
 
 def fb_op_cross_attention(model: int, args: fb_cross) -> None:
+    _on_model(model, args)
     _check(load_library().fb_op_cross_attention(model, ctypes.byref(args)))
 
 
 def fb_op_adapter_gemm(model: int, args: fb_adapters) -> None:
+    _on_model(model, args)
     _check(load_library().fb_op_adapter_gemm(model, ctypes.byref(args)))
 
 

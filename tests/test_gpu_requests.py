@@ -743,3 +743,12 @@ def test_cross_no_key_at_all(model, queries, heads, kv_heads, D, sms, masked):
     finally:
         model.set_sm_budget(0)
     assert (out[:-2] == 0).all() and (out[-2:] == 7.0).all()
+
+
+def test_device_of_a_model(model):
+    assert fb.fb_model_device(model.handle) == torch.cuda.current_device()
+    args = Cross([3], [5], seed=54).args
+    assert args._device == torch.cuda.current_device()
+    args._device += 1  # as if the tensors lay on the next one
+    with pytest.raises(ValueError, match="device"):
+        model.op_cross_attention(args)

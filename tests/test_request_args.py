@@ -87,3 +87,48 @@ def test_make_functions_check_their_tensors():
         fb.make_cross(z, z, z, z, i, i, head_dim=96)
     with pytest.raises(TypeError, match="CUDA"):
         fb.make_adapters(z, z, torch.zeros(1, 8, 128), torch.zeros(1, 4, 8), i, i[:1], z)
+
+
+class _OnDevice:
+    """A tensor's device and nothing else."""
+
+    def __init__(self, index):
+        self.device = type("device", (), {"index": index})
+
+
+class _ModelOnDeviceOne:
+    """The library of a model on device 1, whose calls count."""
+    calls = 0
+
+    def fb_model_device(self, model):
+        return 1
+
+    def fb_op_cross_attention(self, model, args):
+        self.calls += 1
+        return fb.FB_OK
+
+    fb_op_adapter_gemm = fb_op_cross_attention
+
+
+@pytest.mark.parametrize("call,make", [(fb.fb_op_cross_attention, cross), (fb.fb_op_adapter_gemm, adapters)])
+def test_tensors_of_another_device_than_the_models(monkeypatch, call, make):
+    """Refused by the binding before the library reads an address."""
+    lib = _ModelOnDeviceOne()
+    monkeypatch.setattr(fb, "load_library", lambda: lib)
+    assert fb._one_device(q=_OnDevice(2), valid=None, k=_OnDevice(2)) == 2
+    with pytest.raises(ValueError, match="several devices"):
+        fb._one_device(q=_OnDevice(1), k=_OnDevice(0))
+    args = make()
+    args._device = 0
+    with pytest.raises(ValueError, match="device 0.*device 1"):
+        call(P, args)
+    assert lib.calls == 0
+    args._device = 1
+    call(P, args)
+    assert lib.calls == 1
+    call(P, make())  # (filled in by hand: taken as it is)
+    assert lib.calls == 2
+
+
+def test_null_model_has_no_device(lib):
+    assert lib.fb_model_device(None) == -1
