@@ -513,8 +513,8 @@ fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const ui
  * once as it is stored. q_offsets [seqs + 1], kv_offsets [states + 1] (each rising from 0 to at
  * most q_rows or kv_rows) and kv_of [seqs] are read on the device; rows of no sequence are not
  * written. Row strides are multiples of 8, q, k, v and out 16-byte aligned. FB_EINVAL for other
- * sizes, seqs outside [0, FB_CROSS_MAX_SEQS], states < 0 or below seqs without kv_of, heads not a
- * multiple of kv_heads, G past FB_CROSS_MAX_GROUP, rows outside [0, FB_CROSS_MAX_ROWS], or, found
+ * sizes, seqs outside [0, FB_CROSS_MAX_SEQS], states outside [0, FB_CROSS_MAX_ROWS] or below seqs
+ * without kv_of, heads not a multiple of kv_heads, G past FB_CROSS_MAX_GROUP, rows outside [0, FB_CROSS_MAX_ROWS], or, found
  * on the device, offsets that are not as above or a kv_of outside [0, states) (the outputs are
  * then not usable). The scratch for the parts of long states is the model's and grows on demand
  * (FB_ENOMEM). */

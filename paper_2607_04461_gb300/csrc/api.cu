@@ -548,9 +548,10 @@ struct DeviceScope {
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 fb_status cross_args(const fb_cross& c, CrossArgs* out) {
-  if (c.seqs < 0 || c.seqs > FB_CROSS_MAX_SEQS || c.states < 0 || (!c.kv_of && c.states < c.seqs))
-    return fail(FB_EINVAL, "seqs=%d must be in [0, %d], states=%d at least seqs without kv_of",
-                c.seqs, FB_CROSS_MAX_SEQS, c.states);
+  if (c.seqs < 0 || c.seqs > FB_CROSS_MAX_SEQS || c.states < 0 || c.states > FB_CROSS_MAX_ROWS ||
+      (!c.kv_of && c.states < c.seqs))
+    return fail(FB_EINVAL, "seqs=%d must be in [0, %d], states=%d in [0, %d], at least seqs without kv_of",
+                c.seqs, FB_CROSS_MAX_SEQS, c.states, FB_CROSS_MAX_ROWS);
   if (c.heads < 1 || c.heads > FB_CROSS_MAX_HEADS || c.kv_heads < 1 || c.heads % c.kv_heads ||
       c.heads / c.kv_heads > FB_CROSS_MAX_GROUP)
     return fail(FB_EINVAL, "heads=%d must be in [1, %d] and 1 to %d times kv_heads=%d", c.heads,

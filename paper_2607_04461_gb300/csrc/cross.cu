@@ -621,6 +621,13 @@ __global__ void __launch_bounds__(THREADS, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
 
+  // States that no sequence asks for are checked too (the others by load_seq): 32 a CTA by the mask warp
+  // before its first segment, the others, where there are more, when the segments are done.
+  auto bad_state = [&](int64_t u) {
+    if (u >= p.states) return u == 0 && p.kv_off[0] != 0;
+    const int a = p.kv_off[u], b = p.kv_off[u + 1];
+    return b < a || b > p.kv_rows || (u == 0 && a != 0);
+  };
   auto is_dual = [](const Seg& sg) { return DUAL && sg.dual; };
   uint32_t seg = 0;  // segments that this role has come to
   if (warp == 0) {
@@ -871,14 +878,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     // P of tile T - VS - 2: its mask, and those before it, have been read.
     uint32_t t = 0;                 // key tiles so far
     uint32_t land = 0;              // bit s: phase of v_land[s]
-    if (blockIdx.x == 0) {  // states that no sequence asks for are checked here, the others by load_seq
-      bool bad = p.kv_off[0] != 0;
-      for (int u = lane; u < p.states; u += 32) {
-        const int a = p.kv_off[u], b = p.kv_off[u + 1];
-        bad = bad || b < a || b > p.kv_rows;
-      }
-      if (bad) fb_report(err, FB_DEVERR_BAD_INDEX);
-    }
+    if (bad_state(blockIdx.x * 32 + lane)) fb_report(err, FB_DEVERR_BAD_INDEX);
     for (; !failed; ++seg) {
       if (!__all_sync(0xffffffffu, mbar_wait_idle(&g_full[seg % SEGS], (seg / SEGS) & 1, err))) {
         failed = true;
@@ -1204,6 +1204,11 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint64_t t0 = fb_globaltimer();
     while (fb_globaltimer() - t0 < 100000ull) __nanosleep(1000);
   }
+  bool bad = false;
+#pragma unroll 4
+  for (int64_t u = 32ll * gridDim.x + blockIdx.x * THREADS + threadIdx.x; u < p.states; u += (int64_t)gridDim.x * THREADS)
+    bad = bad_state(u) || bad;
+  if (bad) fb_report(err, FB_DEVERR_BAD_INDEX);
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem, TMEM_COLS);

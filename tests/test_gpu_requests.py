@@ -752,3 +752,41 @@ def test_device_of_a_model(model):
     args._device += 1  # as if the tensors lay on the next one
     with pytest.raises(ValueError, match="device"):
         model.op_cross_attention(args)
+
+
+@pytest.mark.parametrize("queries,sms", [([3], 0), ([300] * 40, 0), ([5, 40], 2)])
+def test_cross_bad_offset_of_a_state_that_nobody_asks_for(model, queries, sms):
+    states = 100_000
+    c = Cross(queries, [40, 100, 7], kv_of=[i % 2 for i in range(len(queries))], seed=55)
+    of = c.kv_of
+    k_at = torch.full((states + 1,), 147, dtype=I32, device="cuda")
+    k_at[:3] = whole([0, 40, 140])
+    c.args = fb.make_cross(c.q, c.k, c.v, c.out, whole(c.q_at), k_at, kv_of=of)
+    model.set_sm_budget(sms)
+    try:
+        c.check(model)
+        for at, n in ((3, 139), (31, 141), (32, 146), (33, 148 + len(c.k)), (5000, 12), (12345, -1), (99_999, 1 << 30), (states, 146)):
+            bad = k_at.clone()
+            bad[at] = n
+            with pytest.raises(fb.FlashBonError) as e:
+                model.op_cross_attention(fb.make_cross(c.q, c.k, c.v, c.out, whole(c.q_at), bad, kv_of=of))
+            assert e.value.status == fb.FB_EINVAL, (at, n)
+        c.out.fill_(7.0)
+        c.check(model)
+    finally:
+        model.set_sm_budget(0)
+
+
+def test_cross_very_many_states(model):
+    """2^24 states, two of which are asked for: no role waits for the check of the others (under a limit of
+    3 ms for each wait; one warp alone would look at them for longer)."""
+    c = Cross([3, 200], [40, 100], seed=56)
+    k_at = torch.full(((1 << 24) + 1,), 140, dtype=I32, device="cuda")
+    k_at[:2] = whole([0, 40])
+    c.args = fb.make_cross(c.q, c.k, c.v, c.out, whole(c.q_at), k_at, kv_of=whole([0, 1]))
+    torch.cuda.synchronize()
+    fb.fb_set_device_wait_limit(3_000_000)
+    try:
+        c.check(model)
+    finally:
+        fb.fb_set_device_wait_limit(0)

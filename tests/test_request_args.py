@@ -132,3 +132,9 @@ def test_tensors_of_another_device_than_the_models(monkeypatch, call, make):
 
 def test_null_model_has_no_device(lib):
     assert lib.fb_model_device(None) == -1
+
+
+def test_cross_refuses_more_states_than_rows_can_be(lib):
+    for states in ((1 << 26) + 1, (1 << 31) - 1):
+        assert lib.fb_op_cross_attention(P, ctypes.byref(cross(states=states, kv_of=P))) == fb.FB_EINVAL
+        assert b"states" in lib.fb_last_error()
