@@ -1098,11 +1098,13 @@ __global__ void __launch_bounds__(THREADS, 1)
         const float mx = fmaxf(fmax3(fmax3(top[0], top[1], top[2]), fmax3(top[3], top[4], top[5]), fmaxf(top[6], top[7])) * p.scale_log2, -FLT_MAX);
         if (__all_sync(0xffffffffu, m_used == -INFINITY)) {  // the segment's first tile
           m_used = mx;
-        } else if (const bool grew = mx > m_used + 8.f; __any_sync(0xffffffffu, grew && lane < live)) {
-          // (each row by its own scores: what a row gives does not depend on the rows beside it, among
-          // which may be another sequence's, or none that was ever loaded)
-          const float alpha = grew ? ex2(m_used - mx) : 1.f;
-          m_used = grew ? mx : m_used;
+        } else if (__any_sync(0xffffffffu, mx > m_used + 8.f && lane < live)) {
+          // (Rows that exist vote, and no others: what else lies in the tile, another sequence's queries or
+          // what no load wrote, must not show in this one's bits. The warp's rows move together: each for
+          // itself moves more often, 158 us for 151 of 4096 rows on 8191 keys.)
+          const float m_new = fmaxf(m_used, mx);
+          const float alpha = ex2(m_used - m_new);
+          m_used = m_new;
           l *= alpha;
 #pragma unroll 1
           for (int c = 0; c < D / 32; ++c) {
