@@ -509,8 +509,9 @@ fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const ui
  * valid[j] = 0 hold, NaN and infinities too, has no influence. Where no key is left, out[r] is
  * zero. q and out: bf16 [q_rows][heads * head_dim], k and v: bf16 [kv_rows][kv_heads * head_dim],
  * head_dim 64 or 128, valid: [kv_rows], scale finite and positive (0: 1 / sqrt(head_dim)). Scores,
- * maxima and sums are fp32; a key's weight is rounded to bf16 for its product with v, the result
- * once as it is stored. q_offsets [seqs + 1], kv_offsets [states + 1] (each rising from 0 to at
+ * maxima and sums are fp32, of long states in parts, so that they lose 4e-4 of the result at most; a
+ * key's weight is rounded to bf16 for its product with v, but not in the sum that divides the result,
+ * which is rounded once as it is stored. q_offsets [seqs + 1], kv_offsets [states + 1] (each rising from 0 to at
  * most q_rows or kv_rows) and kv_of [seqs] are read on the device; rows of no sequence are not
  * written. Row strides are multiples of 8, q, k, v and out 16-byte aligned. FB_EINVAL for other
  * sizes, seqs outside [0, FB_CROSS_MAX_SEQS], states outside [0, FB_CROSS_MAX_ROWS] or below seqs

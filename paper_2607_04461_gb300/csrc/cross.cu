@@ -54,6 +54,7 @@ constexpr uint32_t TMEM_COLS = 512;  // S|P of A [0,128), of B [128,256), O of A
 constexpr uint32_t O_COL = 256;
 constexpr int SEGS = 4;              // ring of segments: the current one and those ahead
 constexpr int TAIL = 768;            // bytes of barriers and masks
+constexpr int FOLD = 128;            // key tiles of one accumulator in long states (see fold)
 constexpr int MASKS = 8;             // ring of key tiles' masks (> V slots + 2: see the mask warp)
 
 template <int D>
@@ -73,11 +74,11 @@ struct Params {
   const uint8_t* valid;
   int seqs, states, q_rows, kv_rows, kv_heads, group, rq;
   bool dual;       // two kv heads side by side where a sequence has one query tile
-  bool flat;       // every item costs 1 (sizes whose costs would pass 32 bits)
   bf16* O;
   int64_t ldo;
   float scale_log2;
   float* ws;       // parts of cut items (null: whole items only): two slots a CTA
+  float* sums;     // of long states (see fold): a slot a CTA
   int* counters;   // [gridDim.x][8], zero between launches
   int* err;
 };
@@ -177,8 +178,8 @@ struct Cost {
     if (dual) tiles = p.kv_heads;
     n_kv = (q.nk + TB - 1) / TB;
     w = dual ? 5 : 4;
-    pair = p.flat ? 1 : w * n_kv + 4;
-    single = p.flat ? 1 : 3u * n_kv + 4;
+    pair = w * n_kv + 4;
+    single = 3u * n_kv + 4;
     head = (u32)(tiles / 2) * pair + (tiles & 1 ? single : 0);
   }
   __device__ __forceinline__ u32 all() const { return head * heads; }
@@ -541,8 +542,50 @@ __device__ __forceinline__ void join(const Params& p, int lo, int hi, int ww, in
   }
 }
 
-// DUAL: p.dual
-template <int D, bool MASKED, bool DUAL>
+// The tensor core's sums cut bits off: where all terms have one sign, up to 8e-7 of the result per key tile
+// (2^20 keys in one CTA lose 0.5 %, 2^23 5 %). Past FOLD_ROWS keys (4e-4) a warp therefore adds its O rows, with
+// their maxima and sums (m, l), to what `sum` holds of the segment every FOLD key tiles, and begins again from
+// zero (1e-4 at most, 2^23 keys too). END: what `sum` holds goes back into O and l. A lane's row each; sum lies
+// as a part (see part_of). A kernel of its own (LONG), since this code beside the loop costs the others 2 to 3 %
+// (32 sequences of 1560 rows on 20 to 512 keys 113.3 us for 110.1).
+constexpr int FOLD_ROWS = 512 * TB;
+template <int D, bool END>
+__device__ __forceinline__ void fold(float* sum, bool first, uint32_t o_taddr, int lane, float m, float& l) {
+  float2* ml = reinterpret_cast<float2*>(sum + 32 * D) + lane;
+  const float2 was = first ? make_float2(m, 0.f) : *ml;
+  const float f = ex2(was.x - m);
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c) {
+    uint32_t u[32];
+    tmem_ld32(o_taddr + c * 32, u);
+    tmem_ld_wait();
+    reg_fence32(u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float4* at = reinterpret_cast<float4*>(sum) + (c * 8 + e) * 32 + lane;
+      float4 v = first ? make_float4(0.f, 0.f, 0.f, 0.f) : *at;
+      v.x = fmaf(v.x, f, __uint_as_float(u[4 * e]));
+      v.y = fmaf(v.y, f, __uint_as_float(u[4 * e + 1]));
+      v.z = fmaf(v.z, f, __uint_as_float(u[4 * e + 2]));
+      v.w = fmaf(v.w, f, __uint_as_float(u[4 * e + 3]));
+      if (!END) *at = v;
+      u[4 * e] = END ? __float_as_uint(v.x) : 0u;
+      u[4 * e + 1] = END ? __float_as_uint(v.y) : 0u;
+      u[4 * e + 2] = END ? __float_as_uint(v.z) : 0u;
+      u[4 * e + 3] = END ? __float_as_uint(v.w) : 0u;
+    }
+    tmem_st32(o_taddr + c * 32, u);
+  }
+  tmem_st_wait();
+  l = fmaf(was.y, f, l);
+  if (!END) {
+    *ml = make_float2(m, l);
+    l = 0.f;
+  }
+}
+
+// DUAL: p.dual, LONG: more than FOLD_ROWS keys
+template <int D, bool MASKED, bool DUAL, bool LONG>
 __global__ void __launch_bounds__(THREADS, 1)
     cross_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const Params p) {
@@ -1049,6 +1092,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int i = live > 0 ? 0 : steps; i < steps; ++i, ++sc, kt += kt_step) {
         if (!scores_ready(i == steps - 1)) { failed = true; break; }
         tc_fence_after();
+        if (LONG && i % FOLD == 0 && i > 0)
+          fold<D, false>(p.sums + ((size_t)blockIdx.x * 8 + warp - 2) * part_floats(D), i == FOLD, lane_base + o_col,
+                         lane, m_used, l);
         const int valid = keys - i * TB;
         const int halves = valid > 64 ? 2 : 1;  // (without a key in the second half its P is not read)
         // the keys that there are, 32 to a word; the other scores become -inf where they are
@@ -1165,6 +1211,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       tc_fence_after();
       if (!next_is_there()) { failed = true; break; }
       if (live > 0) {
+        if (LONG && steps > FOLD)
+          fold<D, true>(p.sums + ((size_t)blockIdx.x * 8 + warp - 2) * part_floats(D), false, lane_base + o_col,
+                        lane, m_used, l);
         bf16* out = out_row(sg);
         const bool in = lane < live;
         if (sg.whole) {  // (rows without a key, all masked: zeros)
@@ -1271,7 +1320,7 @@ bool may_cut(const CrossArgs& c, int num_sms) {
   return fewest < 8ll * num_sms && (c.kv_rows > 7 * TB || most_items(c) > num_sms);
 }
 
-template <int D, bool MASKED, bool DUAL>
+template <int D, bool MASKED, bool DUAL, bool LONG>
 cudaError_t launch(const CrossArgs& c, const Params& p, int grid, cudaStream_t st) {
   CUtensorMap mq, mk, mv;
   const bool no_keys = c.kv_rows == 0;  // (any map: nothing is loaded then)
@@ -1280,7 +1329,7 @@ cudaError_t launch(const CrossArgs& c, const Params& p, int grid, cudaStream_t s
     mk = mv = mq;
   else if (!map_kv(&mk, c, c.k, c.ldk) || !map_kv(&mv, c, c.v, c.ldv))
     return cudaErrorInvalidValue;
-  auto kern = cross_kernel<D, MASKED, DUAL>;
+  auto kern = cross_kernel<D, MASKED, DUAL, LONG>;
   const cudaError_t e =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::SMEM);
   if (e != cudaSuccess) return e;
@@ -1289,7 +1338,9 @@ cudaError_t launch(const CrossArgs& c, const Params& p, int grid, cudaStream_t s
 
 template <int D, bool MASKED>
 cudaError_t choose(const CrossArgs& c, const Params& p, int grid, cudaStream_t st) {
-  return p.dual ? launch<D, MASKED, true>(c, p, grid, st) : launch<D, MASKED, false>(c, p, grid, st);
+  if (c.kv_rows > FOLD_ROWS)
+    return p.dual ? launch<D, MASKED, true, true>(c, p, grid, st) : launch<D, MASKED, false, true>(c, p, grid, st);
+  return p.dual ? launch<D, MASKED, true, false>(c, p, grid, st) : launch<D, MASKED, false, false>(c, p, grid, st);
 }
 
 }  // namespace
@@ -1297,8 +1348,8 @@ cudaError_t choose(const CrossArgs& c, const Params& p, int grid, cudaStream_t s
 cudaError_t cross_set_wait_limit(unsigned long long ns) { return fb_set_wait_limit_tu(ns); }
 
 size_t cross_ws_bytes(const CrossArgs& c, int num_sms) {
-  if (!may_cut(c, num_sms)) return 0;
-  return 2 * (size_t)num_sms * 8 * part_floats(c.head_dim) * sizeof(float);
+  const size_t slot = (size_t)num_sms * 8 * part_floats(c.head_dim) * sizeof(float);
+  return (may_cut(c, num_sms) ? 2 * slot : 0) + (c.kv_rows > FOLD_ROWS ? slot : 0);
 }
 
 cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* err, int num_sms,
@@ -1325,9 +1376,10 @@ cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* er
   const long long seqs = c.seqs < c.q_rows ? c.seqs : c.q_rows;
   p.dual = seqs * c.kv_heads > num_sms && c.q_rows <= seqs * p.rq;
   const long long tiles = (c.kv_rows + TB - 1) / TB;
-  p.flat = most_items(c) * (4.0 * tiles + 4) >= 4e9;
-  const bool cut = may_cut(c, num_sms) && !p.flat;
+  // (costs are counted in 32 bits)
+  const bool room = may_cut(c, num_sms), cut = room && most_items(c) * (4.0 * tiles + 4) < 4e9;
   p.ws = cut ? (float*)ws : nullptr;
+  p.sums = (float*)ws + (room ? (size_t)2 * num_sms * 8 * part_floats(c.head_dim) : 0);
   p.counters = counters;
   p.err = err;
   long long units = most_items(c);

@@ -790,3 +790,60 @@ def test_cross_very_many_states(model):
         c.check(model)
     finally:
         fb.fb_set_device_wait_limit(0)
+
+
+def test_cross_very_long_state_loses_nothing(model):
+    """2^22 keys on two SMs, values of one sign: a single accumulator would lose 1 % to the tensor core's
+    truncated sums. The result is rounded to bf16, 2^-8, and its sums lose 1e-4 at most."""
+    keys, D = 1 << 22, 64
+    g = gen(57)
+    k = torch.zeros(keys, D, dtype=BF, device="cuda")
+    v = (1 + torch.rand(keys, D, generator=g, device="cuda")).to(BF)
+    q, out = torch.ones(3, D, dtype=BF, device="cuda"), torch.zeros(3, D, dtype=BF, device="cuda")
+    args = fb.make_cross(q, k, v, out, whole([0, 3]), whole([0, keys]), head_dim=D)
+    want = v.double().mean(0)
+    for sms in (2, 0):
+        model.set_sm_budget(sms)
+        try:
+            model.op_cross_attention(args)
+        finally:
+            model.set_sm_budget(0)
+        assert ((out.double() - want).abs() <= (2.0 ** -8 + 1e-4) * want).all(), sms
+
+
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("valid", [None, 0.4])
+@pytest.mark.parametrize("heads,kv_heads", [(2, 1), (2, 2), (3, 3)])
+@pytest.mark.parametrize("queries,sms", [([3] * 5, 2), ([1, 2, 1, 1, 2], 4), ([140, 0, 300, 5, 1], 2), ([2, 0, 130, 2, 1], 0)])
+def test_cross_long_states_in_parts(model, D, valid, heads, kv_heads, queries, sms):
+    """States on both sides of the parts' 128 key tiles, and of several parts, with scores whose maxima grow;
+    whole items, cut ones and key heads side by side."""
+    model.set_sm_budget(sms)
+    try:
+        Cross(queries, [16384, 16385, 33000, 4, 49153], heads=heads, kv_heads=kv_heads, D=D, valid=valid,
+              scale=0.5, seed=58).check(model)
+    finally:
+        model.set_sm_budget(0)
+
+
+def test_cross_long_state_masked_to_its_last_part(model):
+    """Nothing left in the first parts, then nothing in the last ones."""
+    valid = torch.zeros(70_000 + 3)
+    valid[60_000:60_100] = 1
+    for v in (valid, valid.flip(0)):
+        model.set_sm_budget(2)
+        try:
+            Cross([1, 200], [70_000], kv_of=[0, 0], D=64, valid=v, seed=59).check(model)
+        finally:
+            model.set_sm_budget(0)
+
+
+def test_cross_long_states_same_result_every_time(model):
+    c = Cross([200] * 40, [70_000], kv_of=[0] * 40, D=64, valid=0.1, seed=60)
+    model.op_cross_attention(c.args)
+    first = c.out.clone()
+    for _ in range(5):
+        c.out.fill_(7.0)
+        model.op_cross_attention(c.args)
+        torch.cuda.synchronize()
+        assert torch.equal(first, c.out)
