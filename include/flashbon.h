@@ -496,9 +496,12 @@ fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const ui
  * (engineering entry points: the paper drafts the candidates of one prompt at a time. A pool
  * that serves several requests has a prompt of its own length and an adapter of its own for
  * each.) Inference only. The op calls follow the ones above: DEVICE pointers of the model's
- * device, enqueued on the model's stream, waited for; grids are sized to the model's SM budget;
- * a matrix is row-major with a row stride in elements, elements behind its width are neither
- * read nor written; inputs and outputs do not overlap unless said so; fb_set_op_repeat applies.
+ * device, enqueued on the model's stream, waited for. The attention and the products in tiles size
+ * their grids to the model's SM budget; two kernels of the adapters, the product of few rows by
+ * streamed weights and the low-rank part of short segments, launch a block for every so many weight
+ * rows or rows, on whatever SMs the stream has. A matrix is row-major with a row stride in elements,
+ * elements behind its width are neither read nor written; inputs and outputs do not overlap unless
+ * said so; fb_set_op_repeat applies.
  *
  * fb_op_cross_attention: attention to encoder states of another length. Sequence s has the query
  * rows q_offsets[s] .. q_offsets[s + 1] - 1 and attends to the keys and values kv_offsets[u] ..
@@ -509,16 +512,16 @@ fb_status fb_moe_forward(fb_model* m, const fb_moe* moe, const void* a, const ui
  * valid[j] = 0 hold, NaN and infinities too, has no influence. Where no key is left, out[r] is
  * zero. q and out: bf16 [q_rows][heads * head_dim], k and v: bf16 [kv_rows][kv_heads * head_dim],
  * head_dim 64 or 128, valid: [kv_rows], scale finite and positive (0: 1 / sqrt(head_dim)). Scores,
- * maxima and sums are fp32, of long states in parts, so that they lose 4e-4 of the result at most; a
- * key's weight is rounded to bf16 for its product with v, but not in the sum that divides the result,
- * which is rounded once as it is stored. q_offsets [seqs + 1], kv_offsets [states + 1] (each rising from 0 to at
- * most q_rows or kv_rows) and kv_of [seqs] are read on the device; rows of no sequence are not
- * written. Row strides are multiples of 8, q, k, v and out 16-byte aligned. FB_EINVAL for other
- * sizes, seqs outside [0, FB_CROSS_MAX_SEQS], states outside [0, FB_CROSS_MAX_ROWS] or below seqs
- * without kv_of, heads not a multiple of kv_heads, G past FB_CROSS_MAX_GROUP, rows outside [0, FB_CROSS_MAX_ROWS], or, found
- * on the device, offsets that are not as above or a kv_of outside [0, states) (the outputs are
- * then not usable). The scratch for the parts of long states is the model's and grows on demand
- * (FB_ENOMEM). */
+ * maxima and sums are fp32, of long states in parts, so that they lose 4e-4 of the result at most;
+ * a key's weight is rounded to bf16 for its product with v, but not in the sum that divides the
+ * result, which is rounded once as it is stored. q_offsets [seqs + 1], kv_offsets [states + 1]
+ * (each rising from 0 to at most q_rows or kv_rows) and kv_of [seqs] are read on the device; rows
+ * of no sequence are not written. Row strides are multiples of 8, q, k, v and out 16-byte aligned.
+ * FB_EINVAL for other sizes, seqs outside [0, FB_CROSS_MAX_SEQS], states outside [0,
+ * FB_CROSS_MAX_ROWS] or below seqs without kv_of, heads not a multiple of kv_heads, G past
+ * FB_CROSS_MAX_GROUP, rows outside [0, FB_CROSS_MAX_ROWS], or, found on the device, offsets that
+ * are not as above or a kv_of outside [0, states) (the outputs are then not usable). The scratch
+ * for the parts of long states is the model's and grows on demand (FB_ENOMEM). */
 #define FB_CROSS_MAX_SEQS 4096
 #define FB_CROSS_MAX_GROUP 128
 #define FB_CROSS_MAX_HEADS 4096
@@ -551,7 +554,7 @@ fb_status fb_op_cross_attention(fb_model* m, const fb_cross* c);
  * they are stored; x a_e^T passes through the tensor cores as a sum of bf16 values, two of them
  * for bf16 results and three for fp32 ones. offsets [segments + 1] (rising from 0 to at most rows)
  * and adapter [segments] are read on the device; rows from offsets[segments] on are not written.
- * n, k, rank and the row strides are multiples of 8; x, w, a, b and out are 16-byte aligned.
+ * n, k, rank and the row strides are multiples of 8; x, w, a, b, resid and out are 16-byte aligned.
  * FB_EINVAL for other sizes, segments outside [0, FB_ADAPTER_MAX_SEGMENTS], adapters < 1, rank past
  * FB_ADAPTER_MAX_RANK, rows outside [0, FB_ADAPTER_MAX_ROWS], n or k past FB_EXPERT_MAX_SIZE, or,
  * found on the device, offsets that are not as above or an adapter outside [-1, adapters) (the

@@ -847,3 +847,43 @@ def test_cross_long_states_same_result_every_time(model):
         model.op_cross_attention(c.args)
         torch.cuda.synchronize()
         assert torch.equal(first, c.out)
+
+
+def test_both_on_sm_partitions_side_by_side():
+    """A model on each part of the GPU, with its budget, two threads at once: the results of the whole one
+    within the tolerance, the same bits every time."""
+    import threading
+    with fb.Model(synth.TINY, synth.make_weights(synth.TINY)) as one, \
+            fb.Model(synth.TINY, synth.make_weights(synth.TINY)) as two, fb.SmSplit(40) as sp:
+        work = [(m, part, Cross([3, 300, 5], [6000, 700, 70_000], seed=61 + part),
+                 [Adapters(*a, N=1536, K=1544, rank=16, seed=63 + part) for a in (LONG, MANY, ([6], [0]))])
+                for part, m in enumerate((one, two))]
+        torch.cuda.synchronize()
+        failures = []
+
+        def run(m, part, c, adapters):
+            try:
+                m.set_stream(sp.streams[part])
+                m.set_sm_budget(sp.sms[part])
+                for _ in range(10):
+                    m.op_cross_attention(c.args)
+                    for a in adapters:
+                        m.op_adapter_gemm(a.args)
+            except Exception as e:  # noqa: BLE001
+                failures.append(e)
+
+        threads = [threading.Thread(target=run, args=w) for w in work]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert not failures
+        for m, _, c, adapters in work:
+            first = c.out.clone()
+            c.check(m)
+            assert torch.equal(first, c.out)
+            for a in adapters:
+                first = a.out.clone()
+                a.check(m)
+                assert torch.equal(first, a.out)
+            m.set_stream(None)
