@@ -22,8 +22,9 @@
 // adds up (the tensor core's sums lose about 6e-8 of the result per K block of 64). So do results of
 // a K past 2^17.
 // Bounds: with many rows the tensor pipe under the power cap (24960 rows, 8960 x 1536, rank 64: 430 us, 1.6
-// PFLOP/s, t's 26 among them); with one round of tiles the SM's operand rate, some 45 bytes a clock (1560
-// rows, 1536 x 8960, rank 32, fp32: 58 us, K blocks of 256 x 192 590 clocks); with few rows latency (see
+// PFLOP/s, t's 26 among them). With one round of tiles a K block of 256 x 192 takes 590 clocks (1560 rows,
+// 1536 x 8960, rank 32, fp32: 58 us), where the tensor pipe needs 384 and operands, 256 + 192 clocks, 448;
+// what the others go to is not known, and other widths took no less in all. With few rows latency (see
 // adapter_delta_kernel).
 // Every wait is bounded (mbar_wait): a role that gives up records it and the kernel ends.
 #include <atomic>

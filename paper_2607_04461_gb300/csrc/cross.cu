@@ -16,9 +16,11 @@
 //    TMEM, V MN-major); the order PV_A(j), S_A(j+1), PV_B(j), S_B(j+1) lets each group's softmax run
 //    beside the other group's MMAs.
 //  * warps 2-9: softmax, one row per thread, warps 2-5 tile A, 6-9 tile B: running maximum and
-//    sum in fp32 registers, P = exp2(scale log2(e) s - m) as bf16 over S in TMEM (its rounding is
-//    random from key to key and averages out in O, at most 2^-8 of a term), O rescaled in TMEM
-//    only when the maximum grew by more than 2^8. The sum is of the unrounded values. Its code is kept
+//    sum in fp32 registers, P = exp2(scale log2(e) s - m) as bf16 over S in TMEM, O rescaled in TMEM
+//    only when the maximum grew by more than 2^8. P's rounding is 2^-8 of a term at most; the sum is of the
+//    unrounded values, so that where few keys count it stays in the result (32 sequences of 1560 rows on 512
+//    keys: 2.03e-3 off, rounding the result alone gives 1.66e-3). A sum of the rounded values would give
+//    1.83e-3 and take 158 us for 153 (added half a tile later, beside the next load, 159). Its code is kept
 //    short, since an item's end and the next one's start run as fast as their instructions arrive: masked
 //    scores become -inf in TMEM by a loop over 32 at a time, and exponentials are taken 64 at a time from a
 //    second read (both unrolled over the 128 registers of the first read: 128 us for those 110).
@@ -31,9 +33,10 @@
 // The last key tile's MMAs cover ceil16 of its keys. Every wait is bounded (mbar_wait): a role
 // that gives up records it and the kernel ends.
 //
-// Bounds: with many queries for each key the tensor pipe and the exponentials, 2 x 128 x 128 of both
-// in about 2600 clocks (32 candidates of 1560 rows, 12 heads of 128: 149 us, 1.05 PFLOP/s, for 512 shared
-// keys, 388 us, 1.23 PFLOP/s, for 1560 own ones; 4096 rows on 8191 keys in cut items: 147 us, 1.40), with
+// Bounds: with many queries for each key the hand-over between softmax and issuer: a step of 2 x 128 x 128
+// takes about 2600 clocks, of which the tensor pipe needs 2049 and the exponentials 1056 (31 a clock); it waits
+// for the arithmetic around them (32 candidates of 1560 rows, 12 heads of 128: 153 us, 1.03 PFLOP/s, for 512
+// shared keys, 388 us, 1.23 PFLOP/s, for 1560 own ones; 4096 rows on 8191 keys in cut items: 150 us, 1.37). With
 // tokens on long states the bytes of K and V (64 requests, 4 kv heads of 128, 32 to 4096 keys, 92 MB:
 // 28.3 us, half of it at the rate of a copy). What is left beside them: 4 to 5 us from launch to the first
 // scores, some 3000 clocks at an item's end until the next one's scores are looked at (tried without gain:
@@ -1370,9 +1373,9 @@ cudaError_t cross_attention(const CrossArgs& c, void* ws, int* counters, int* er
   p.ldo = c.ldo;
   p.scale_log2 = c.scale * 1.4426950408889634f;
   // Two kv heads side by side keep twice as much of K and V on its way (64 tokens of 4 kv heads on 32 to
-  // 4096 keys: 28.3 us for 30.9), but a step of both takes 3500 clocks for one's 2600: only where every CTA
-  // has more than one to do. With longer sequences the items have two query tiles for the most part, and
-  // the kernel without that takes 149 us for 161 (32 of 1560 rows on 512 keys).
+  // 4096 keys: 28.3 us for 30.9), but a step of both takes 3500 clocks for one's 2600: only where there are
+  // more heads of sequences than SMs (as pairs they may be fewer). With longer sequences the items have two query tiles for the most part, and
+  // the kernel without that took 149 us for 161 (32 of 1560 rows on 512 keys).
   const long long seqs = c.seqs < c.q_rows ? c.seqs : c.q_rows;
   p.dual = seqs * c.kv_heads > num_sms && c.q_rows <= seqs * p.rq;
   const long long tiles = (c.kv_rows + TB - 1) / TB;
