@@ -755,9 +755,10 @@ def _one_device(**tensors):
 
 def _on_model(model, args):
     """Refuses tensors of another device than the model's, whose addresses mean nothing there.
-    (Structures filled in by hand say nothing about their device.)"""
+    (Structures filled in by hand say nothing about their device, and no model is the library's to
+    refuse.)"""
     device = getattr(args, "_device", None)
-    if device is not None and device != load_library().fb_model_device(model):
+    if model and device is not None and device != load_library().fb_model_device(model):
         raise ValueError(f"tensors on device {device}, the model on device "
                          f"{load_library().fb_model_device(model)}")
 

@@ -138,3 +138,13 @@ def test_cross_refuses_more_states_than_rows_can_be(lib):
     for states in ((1 << 26) + 1, (1 << 31) - 1):
         assert lib.fb_op_cross_attention(P, ctypes.byref(cross(states=states, kv_of=P))) == fb.FB_EINVAL
         assert b"states" in lib.fb_last_error()
+
+
+@pytest.mark.parametrize("call,make", [(fb.fb_op_cross_attention, cross), (fb.fb_op_adapter_gemm, adapters)])
+def test_no_model_is_refused_by_the_library(lib, call, make):
+    """As before the tensors' device was looked at (a closed Model has no handle)."""
+    args = make()
+    args._device = 0
+    with pytest.raises(fb.FlashBonError) as e:
+        call(None, args)
+    assert e.value.status == fb.FB_EINVAL
