@@ -21,7 +21,7 @@
 // fp32 results take K in parts of 4 blocks, each in an accumulator of its own, which the epilogue
 // adds up (the tensor core's sums lose about 6e-8 of the result per K block of 64). So do results of
 // a K past 2^17.
-// Bounds: with many rows the tensor pipe under the power cap (24960 rows, 8960 x 1536, rank 64: 430 us, 1.6
+// Bounds: with many rows the tensor pipe under the power cap (24960 rows, 8960 x 1536, rank 64: 421 us, 1.7
 // PFLOP/s, t's 26 among them). With one round of tiles a K block of 256 x 192 takes 590 clocks (1560 rows,
 // 1536 x 8960, rank 32, fp32: 58 us), where the tensor pipe needs 384 and operands, 256 + 192 clocks, 448;
 // what the others go to is not known, and other widths took no less in all. With few rows latency (see
